@@ -4,4 +4,4 @@
 The HIP library (libdla.so) is loaded on first use by paper_2606_10650_amd.dla;
 importing the package does not touch the GPU.
 """
-__all__ = ["dla", "workloads", "build"]
+__all__ = ["dla", "train", "workloads", "build"]

@@ -125,6 +125,10 @@ static dla_status ret(dla_status s) {
   return s;
 }
 
+namespace dla {
+dla_status remember(dla_status s) { return ret(s); }
+}  // namespace dla
+
 static dla_status check_desc(const dla_cache_desc* d) {
   if (!d) return DLA_ERR_INVALID_ARG;
   if (d->B < 1 || d->H < 1 || d->C < 1) return DLA_ERR_INVALID_ARG;

@@ -1,0 +1,82 @@
+// Launches of the single-state recurrence and its backward pass (recurrence.hip,
+// recurrence_adjoint.hip, recurrence_step.hip).
+#pragma once
+#include "dla_common.h"
+#include "dla_train.h"
+
+namespace dla {
+
+// Rows of one tensor: element (b, h, t, i) lies at p + b sb + (h / hdiv) sh + t st + i,
+// in elements.
+struct Rows {
+  void* p = nullptr;
+  int64_t sb = 0, sh = 0, st = 0;
+  int hdiv = 1;
+};
+
+inline Rows rows_of(const dla_rows* r, int hdiv) {
+  Rows x;
+  if (r) {
+    x.p = r->data;
+    x.sb = r->stride_b;
+    x.sh = r->stride_h;
+    x.st = r->stride_t;
+    x.hdiv = hdiv;
+  }
+  return x;
+}
+
+template <typename T>
+__device__ __forceinline__ T* row_base(const Rows& r, int b, int h) {
+  return static_cast<T*>(r.p) + (b * r.sb + (h / r.hdiv) * r.sh);
+}
+
+// What every kernel of a call is given.  Heads are numbered b * H + h.
+struct RecArgs {
+  int B, H, Hk, T, dk, dv;
+  float scale;
+  const int32_t* lengths;
+  Rows gate;           // float32
+  int nseg, seg_len;   // segments of seg_len tokens (a multiple of the chunk)
+  float* seg_state;    // [heads][nseg][dk][dv], the state before each segment
+  float* seg_adj;      // [heads][nseg][dk][dv], the adjoint behind each segment
+  float* seg_decay;    // [heads][nseg]
+};
+
+// Tokens per chunk: what a workgroup takes at a time.
+inline int rec_chunk(int dtype) { return dtype == DLA_BF16 ? 64 : 32; }
+
+// Forward over segments: out (and the last state).
+hipError_t launch_recurrence_forward(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
+                                     const Rows& v, const Rows& out, const float* s0, float* s_out,
+                                     hipStream_t st);
+// dq, by the forward kernel with do, v, k in the places of q, k, v and the state
+// transposed; qdot[head][t] = q_t . (the part of dq_t that came from before the chunk);
+// end_dot[head] = <dstate, last state> where dstate is given.
+hipError_t launch_recurrence_dq(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
+                                const Rows& v, const Rows& dout, const Rows& dq, bool dq_f32,
+                                const float* s0, const float* dstate, float* qdot, float* end_dot,
+                                hipStream_t st);
+// dk, dv, dstate0, and per token what its pairs inside the chunk and behind it add to dg.
+hipError_t launch_recurrence_adjoint(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
+                                     const Rows& v, const Rows& dout, const Rows& dk, bool dk_f32,
+                                     const Rows& dv, const float* dstate, float* ds0, float* kdot,
+                                     hipStream_t st);
+// Each segment's own contribution to the state (or, reverse, to the adjoint), and from
+// them the state before (the adjoint behind) each segment.
+hipError_t launch_recurrence_segments(const RecArgs& a, int dtype, bool reverse, const Rows& x,
+                                      const Rows& y, const float* first, hipStream_t st);
+// Token by token, for short sequences.
+hipError_t launch_recurrence_step(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
+                                  const Rows& v, const Rows& out, const float* s0, float* s_out,
+                                  hipStream_t st);
+// dg from the per-token sums: dg_t = end_dot + sum over s >= t of (qdot_s - kdot_s).
+hipError_t launch_recurrence_dgate(const RecArgs& a, int dtype, const float* qdot, const float* kdot,
+                                   const float* end_dot, double* block_sum, int* block_cut,
+                                   const Rows& dg, hipStream_t st);
+constexpr int kDgateBlock = 1024;   // tokens per workgroup of the gate's gradient
+// Sums the heads that share a key head: [B][H][T][d] float32 -> rows of B * Hk heads.
+hipError_t launch_head_sum(const RecArgs& a, int dtype, const float* part, const Rows& out,
+                           hipStream_t st);
+
+}  // namespace dla

@@ -1,0 +1,366 @@
+// The single-state recurrence over long sequences, and dq of its backward pass.
+//
+// A workgroup takes one head's segment of tokens, a chunk at a time (recurrence_tile.h
+// has the chunk's formulas).  Wave w holds columns 32 w .. 32 w + 31 of the state, all
+// d_k rows of them, in the accumulators of the products that update it; their layout is
+// that of the first operand of the product that reads them, so the state never leaves
+// the registers.  The chunk's scores are formed with keys as the first operand, which
+// makes them, too, the operand of the product with the values; every wave forms them for
+// itself, which costs a quarter more products and saves a barrier and a pass through LDS.
+//
+// dq_t = sum_{s <= t} e^{a_t - a_s} (do_t . v_s) k_s + e^{a_t} S do_t is the same with do,
+// v and k in the places of q, k and v and the state transposed.
+#include "recurrence_tile.h"
+
+namespace dla {
+namespace {
+
+struct FwdArgs {
+  RecArgs a;
+  Rows q, k, v, out;       // in the kernel's roles
+  const float* s0;         // state before the first token, or null
+  int64_t s_rs, s_cs;      // strides of a state's rows and columns, in the kernel's roles
+  const float* seg_state;  // state before each segment, or null: one segment
+  float* s_out;            // state behind the last token, or null
+  const float* dstate;     // dq only, or null
+  Rows x;                  // dq only: q, whose products with dq's carried part go to qdot
+  float* qdot;
+  float* end_dot;
+  int out_f32;
+};
+
+template <typename Tin, int DK, int DV, bool DQ>
+__global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
+  constexpr int CH = kChunk<Tin>, NT = 2 * DV, NW = DV / 32, TT = CH / 32, ST = DK / 32;
+  using F = typename Frag<Tin>::T;
+  using TK = Tile<Tin, DK>;
+  using TV = Tile<Tin, DV>;
+  __shared__ __align__(16) Tin sq[CH * DK], sk[CH * DK], sv[CH * DV];
+  __shared__ __align__(16) Decays<CH> dec;
+  __shared__ float dots[DQ ? NW * CH : 1];
+  const RecArgs& a = f.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5;
+  const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
+  const int b = head / a.H, h = head % a.H, c0 = 32 * wave;
+  const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
+  const Tin* q = row_base<const Tin>(f.q, b, h);
+  const Tin* k = row_base<const Tin>(f.k, b, h);
+  const Tin* v = row_base<const Tin>(f.v, b, h);
+  const float* gate = row_base<const float>(a.gate, b, h);
+  const int64_t D = (int64_t)DK * DV;
+
+  f32x16 S[ST];
+  const float* first = f.seg_state ? f.seg_state + ((int64_t)head * a.nseg + seg) * D
+                                   : (f.s0 ? f.s0 + head * D : nullptr);
+  if (first) {
+    load_state(S, first, f.s_rs, f.s_cs, c0, lane);
+  } else {
+#pragma unroll
+    for (int i = 0; i < ST; ++i) S[i] = zero16();
+  }
+
+  Stage<Tin, DK, NT> gq, gk;
+  Stage<Tin, DV, NT> gv;
+  float gg = 0.f;
+  auto request = [&](int t0) {
+    gq.load(q, f.q.st, t0, lim, tid);
+    gk.load(k, f.k.st, t0, lim, tid);
+    gv.load(v, f.v.st, t0, lim, tid);
+    if (wave == 0) gg = (lane < CH && t0 + lane < lim) ? gate[(t0 + lane) * a.gate.st] : 0.f;
+  };
+  request(begin);
+  for (int t0 = begin; t0 < end; t0 += CH) {
+    __syncthreads();   // the last chunk's tiles are read
+    gq.store(sq, tid);
+    gk.store(sk, tid);
+    gv.store(sv, tid);
+    if (wave == 0) form_decays<CH>(&dec, gg, lane);
+    __syncthreads();
+    if (t0 + CH < end) request(t0 + CH);
+
+    F vf[2 * TT];
+#pragma unroll
+    for (int kk = 0; kk < 2 * TT; ++kk) vf[kk] = TV::template col_frag<false>(sv, c0, kk, lane);
+#pragma unroll
+    for (int tt = 0; tt < TT; ++tt) {
+      const int tl = 32 * tt + (lane & 31), t = t0 + tl;
+      F qf[DK / 16];
+#pragma unroll
+      for (int kk = 0; kk < DK / 16; ++kk) qf[kk] = TK::row_frag(sq, tl, kk, lane);
+      const float hi = dec.hi[tl], lo = dec.lo[tl];
+      f32x16 o = zero16();
+#pragma unroll
+      for (int st = 0; st <= tt; ++st) {
+        f32x16 p = zero16();
+#pragma unroll
+        for (int kk = 0; kk < DK / 16; ++kk)
+          Frag<Tin>::mma(p, TK::row_frag(sk, 32 * st + perm_row(lane & 31), kk, lane), qf[kk]);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          float hs[8], ls[8], x[8];
+          weights8(dec.hi, 2 * st + kk, lane, hs);
+          weights8(dec.lo, 2 * st + kk, lane, ls);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int s = 32 * st + 16 * kk + 8 * g + e;
+            x[e] = s <= tl ? p[8 * kk + e] * decay2(hi, lo, hs[e], ls[e]) : 0.f;
+          }
+          Frag<Tin>::mma(o, vf[2 * st + kk], Frag<Tin>::from_floats(x));
+        }
+      }
+      f32x16 c = zero16();
+#pragma unroll
+      for (int i = 0; i < ST; ++i)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          const F s = state_frag<Tin>(S[i], kk);
+          // qdot adds up along the sequence, so what the rounding left counts there
+          if constexpr (DQ && sizeof(Tin) == 2)
+            Frag<Tin>::mma(c, state_frag_low(S[i], kk, s), qf[2 * i + kk]);
+          Frag<Tin>::mma(c, s, qf[2 * i + kk]);
+        }
+      const float in = dec.in[tl];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        c[r] *= in * a.scale;
+        o[r] = o[r] * a.scale + c[r];
+        if (t >= lim) o[r] = 0.f;
+      }
+      if constexpr (DQ) {
+        float dot = 0.f;
+        if (t < lim) {
+          const Tin* x = row_base<const Tin>(f.x, b, h) + t * f.x.st + c0;
+#pragma unroll
+          for (int bb = 0; bb < 4; ++bb) {
+            float y[4];
+            load4f(x + 8 * bb + 4 * g, y);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) dot += c[4 * bb + j] * y[j];
+          }
+        }
+        dot += __shfl_xor(dot, 32);
+        if (g == 0) dots[wave * CH + tl] = dot;
+      }
+      if (t < end) {
+        if (f.out_f32) store_out(row_base<float>(f.out, b, h) + t * f.out.st, c0, o, lane);
+        else store_out(row_base<Tin>(f.out, b, h) + t * f.out.st, c0, o, lane);
+      }
+    }
+    const float total = dec.total;
+#pragma unroll
+    for (int i = 0; i < ST; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[i][r] *= total;
+#pragma unroll
+    for (int kk = 0; kk < 2 * TT; ++kk) {
+      float w[8];
+      weights8(dec.out, kk, lane, w);
+      const Scaled<Tin> y(vf[kk], w);
+#pragma unroll
+      for (int i = 0; i < ST; ++i) y.mma_b(S[i], TK::template col_frag<true>(sk, 32 * i, kk, lane));
+    }
+    if constexpr (DQ) {
+      __syncthreads();
+      if (tid < CH && t0 + tid < end) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) x += dots[w * CH + tid];
+        f.qdot[(int64_t)head * a.T + t0 + tid] = x;
+      }
+    }
+  }
+  if (seg == a.nseg - 1) {
+    if (f.s_out) store_state(S, f.s_out + head * D, f.s_rs, f.s_cs, c0, lane);
+    if constexpr (DQ) {
+      if (f.dstate) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < ST; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            x += S[i][r] * f.dstate[head * D + (32 * i + held_row(r, lane)) * f.s_rs + (c0 + (lane & 31)) * f.s_cs];
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+        __syncthreads();
+        if (lane == 0) dots[wave] = x;
+        __syncthreads();
+        if (tid == 0) {
+          float y = 0.f;
+          for (int w = 0; w < NW; ++w) y += dots[w];
+          f.end_dot[head] = y;
+        }
+      }
+    }
+  }
+}
+
+// A segment's own part of the state behind it, sum over its tokens of (decay to the
+// segment's end) k_s v_s^T; reverse: of the adjoint before it, sum of scale (decay from
+// the segment's start) q_s do_s^T.
+template <typename Tin, int DK, int DV, bool REV>
+__global__ __launch_bounds__(2 * DV, 2) void segment_kernel(RecArgs a, Rows xr, Rows yr, float* dst) {
+  constexpr int CH = kChunk<Tin>, NT = 2 * DV, TT = CH / 32, ST = DK / 32;
+  using TK = Tile<Tin, DK>;
+  using TV = Tile<Tin, DV>;
+  __shared__ __align__(16) Tin sk[CH * DK], sv[CH * DV];
+  __shared__ __align__(16) Decays<CH> dec;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
+  const int b = head / a.H, h = head % a.H, c0 = 32 * wave;
+  const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
+  const Tin* x = row_base<const Tin>(xr, b, h);
+  const Tin* y = row_base<const Tin>(yr, b, h);
+  const float* gate = row_base<const float>(a.gate, b, h);
+  f32x16 S[ST];
+#pragma unroll
+  for (int i = 0; i < ST; ++i) S[i] = zero16();
+  float decay = 1.f;
+  Stage<Tin, DK, NT> gx;
+  Stage<Tin, DV, NT> gy;
+  float gg = 0.f;
+  auto request = [&](int t0) {
+    gx.load(x, xr.st, t0, lim, tid);
+    gy.load(y, yr.st, t0, lim, tid);
+    if (wave == 0) gg = (lane < CH && t0 + lane < lim) ? gate[(t0 + lane) * a.gate.st] : 0.f;
+  };
+  const int n = (end - begin + CH - 1) / CH;
+  auto chunk_at = [&](int c) { return begin + (REV ? n - 1 - c : c) * CH; };
+  request(chunk_at(0));
+  for (int c = 0; c < n; ++c) {
+    __syncthreads();
+    gx.store(sk, tid);
+    gy.store(sv, tid);
+    if (wave == 0) form_decays<CH>(&dec, gg, lane);
+    __syncthreads();
+    if (c + 1 < n) request(chunk_at(c + 1));
+    const float total = dec.total;
+    decay *= total;
+#pragma unroll
+    for (int i = 0; i < ST; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[i][r] *= total;
+#pragma unroll
+    for (int kk = 0; kk < 2 * TT; ++kk) {
+      float w[8];
+      weights8(REV ? dec.in : dec.out, kk, lane, w);
+      if constexpr (REV) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] *= a.scale;
+      }
+      const Scaled<Tin> z(TV::template col_frag<false>(sv, c0, kk, lane), w);
+#pragma unroll
+      for (int i = 0; i < ST; ++i) z.mma_b(S[i], TK::template col_frag<true>(sk, 32 * i, kk, lane));
+    }
+  }
+  store_state(S, dst + ((int64_t)head * a.nseg + seg) * DK * DV, DV, 1, c0, lane);
+  if (tid == 0) a.seg_decay[(int64_t)head * a.nseg + seg] = decay;
+}
+
+// The segments' own parts become the states before them (reverse: the adjoints behind
+// them), one element of a head's state per thread.
+template <bool REV>
+__global__ __launch_bounds__(256) void prefix_kernel(RecArgs a, float* part, const float* first) {
+  const int64_t D = (int64_t)a.dk * a.dv;
+  const int head = blockIdx.y;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;   // D is a multiple of 256
+  float* p = part + (int64_t)head * a.nseg * D + i;
+  const float* decay = a.seg_decay + (int64_t)head * a.nseg;
+  float cur = first ? first[head * D + i] : 0.f;
+  for (int j = 0; j < a.nseg; ++j) {
+    const int s = REV ? a.nseg - 1 - j : j;
+    const float own = p[s * D];
+    p[s * D] = cur;
+    cur = decay[s] * cur + own;
+  }
+}
+
+template <typename Tin, int DK, int DV, bool DQ>
+hipError_t run_forward(const FwdArgs& f, hipStream_t st) {
+  const int grid = f.a.B * f.a.H * f.a.nseg;
+  hipLaunchKernelGGL((forward_kernel<Tin, DK, DV, DQ>), dim3(grid), dim3(2 * DV), 0, st, f);
+  return hipGetLastError();
+}
+
+template <bool DQ>
+hipError_t pick_forward(const FwdArgs& f, int dtype, int dk, int dv, hipStream_t st) {
+  if (dtype == DLA_BF16) {
+    if (dk == 128) return dv == 128 ? run_forward<bf16_t, 128, 128, DQ>(f, st) : run_forward<bf16_t, 128, 64, DQ>(f, st);
+    return dv == 128 ? run_forward<bf16_t, 64, 128, DQ>(f, st) : run_forward<bf16_t, 64, 64, DQ>(f, st);
+  }
+  if (dk == 128) return dv == 128 ? run_forward<float, 128, 128, DQ>(f, st) : run_forward<float, 128, 64, DQ>(f, st);
+  return dv == 128 ? run_forward<float, 64, 128, DQ>(f, st) : run_forward<float, 64, 64, DQ>(f, st);
+}
+
+template <typename Tin, int DK, int DV>
+hipError_t run_segments(const RecArgs& a, bool rev, const Rows& x, const Rows& y, const float* first,
+                        hipStream_t st) {
+  const dim3 grid(a.B * a.H * a.nseg), block(2 * DV), pg(DK * DV / 256, a.B * a.H);
+  float* dst = rev ? a.seg_adj : a.seg_state;
+  if (rev) {
+    hipLaunchKernelGGL((segment_kernel<Tin, DK, DV, true>), grid, block, 0, st, a, x, y, dst);
+    hipLaunchKernelGGL((prefix_kernel<true>), pg, dim3(256), 0, st, a, dst, first);
+  } else {
+    hipLaunchKernelGGL((segment_kernel<Tin, DK, DV, false>), grid, block, 0, st, a, x, y, dst);
+    hipLaunchKernelGGL((prefix_kernel<false>), pg, dim3(256), 0, st, a, dst, first);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_recurrence_segments(const RecArgs& a, int dtype, bool reverse, const Rows& x,
+                                      const Rows& y, const float* first, hipStream_t st) {
+  if (dtype == DLA_BF16) {
+    if (a.dk == 128) return a.dv == 128 ? run_segments<bf16_t, 128, 128>(a, reverse, x, y, first, st) : run_segments<bf16_t, 128, 64>(a, reverse, x, y, first, st);
+    return a.dv == 128 ? run_segments<bf16_t, 64, 128>(a, reverse, x, y, first, st) : run_segments<bf16_t, 64, 64>(a, reverse, x, y, first, st);
+  }
+  if (a.dk == 128) return a.dv == 128 ? run_segments<float, 128, 128>(a, reverse, x, y, first, st) : run_segments<float, 128, 64>(a, reverse, x, y, first, st);
+  return a.dv == 128 ? run_segments<float, 64, 128>(a, reverse, x, y, first, st) : run_segments<float, 64, 64>(a, reverse, x, y, first, st);
+}
+
+hipError_t launch_recurrence_forward(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
+                                     const Rows& v, const Rows& out, const float* s0, float* s_out,
+                                     hipStream_t st) {
+  FwdArgs f;
+  f.a = a;
+  f.q = q;
+  f.k = k;
+  f.v = v;
+  f.out = out;
+  f.s0 = s0;
+  f.s_rs = a.dv;
+  f.s_cs = 1;
+  f.seg_state = a.nseg > 1 ? a.seg_state : nullptr;
+  f.s_out = s_out;
+  f.dstate = nullptr;
+  f.qdot = f.end_dot = nullptr;
+  f.out_f32 = 0;
+  return pick_forward<false>(f, dtype, a.dk, a.dv, st);
+}
+
+hipError_t launch_recurrence_dq(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
+                                const Rows& v, const Rows& dout, const Rows& dq, bool dq_f32,
+                                const float* s0, const float* dstate, float* qdot, float* end_dot,
+                                hipStream_t st) {
+  FwdArgs f;
+  f.a = a;
+  f.q = dout;
+  f.k = v;
+  f.v = k;
+  f.out = dq;
+  f.s0 = s0;
+  f.s_rs = 1;
+  f.s_cs = a.dv;
+  f.seg_state = a.nseg > 1 ? a.seg_state : nullptr;
+  f.s_out = nullptr;
+  f.dstate = dstate;
+  f.x = q;
+  f.qdot = qdot;
+  f.end_dot = end_dot;
+  f.out_f32 = dq_f32 ? 1 : 0;
+  return pick_forward<true>(f, dtype, a.dv, a.dk, st);
+}
+
+}  // namespace dla

@@ -1,0 +1,415 @@
+// The part of the recurrence's backward pass that runs from the last token back: dk, dv,
+// the adjoint of the state, and the gate's gradient.
+//
+// With R the adjoint of the state behind a chunk (what later tokens and the last state's
+// gradient ask of it), a chunk gives
+//   dv_s = e^{a_end - a_s} R^T k_s + scale sum_{u >= s} e^{a_u - a_s} (q_u . k_s) do_u
+//   dk_s = e^{a_end - a_s} R v_s   + scale sum_{u >= s} e^{a_u - a_s} (do_u . v_s) q_u
+//   R   <- e^{a_end} R + scale sum_u e^{a_u} q_u do_u^T.
+// dv contracts R over its rows and dk over its columns.  A wave holds 32 columns of R and
+// 32 columns of R^T, both in accumulators, which are the operands of those products as
+// they are; keeping R twice costs the products that update it and no pass through LDS.
+//
+// The gate's gradient: e^{g_t} scales what every token s < t leaves for every token u >= t,
+// so dg_t is the sum over those pairs of A_us = scale e^{a_u - a_s} (q_u . k_s)(do_u . v_s),
+// with the state before all tokens and the gradient of the last one as further ends.  With
+// x_u the sum of A_us over s < u and y_s that over u > s, dg_t = <dstate, last state> + sum
+// over s >= t of (x_s - y_s).  No pair (t, t) enters either, so nothing large cancels where
+// the gates are steep.  This kernel adds up the pairs inside a chunk and those from a
+// chunk's token to what is behind the chunk; the pairs with what is before it come from
+// the dq pass.
+#include "recurrence_tile.h"
+
+namespace dla {
+namespace {
+
+struct AdjArgs {
+  RecArgs a;
+  Rows q, k, v, dout, dk, dv;
+  const float* dstate;
+  float* ds0;
+  float* kdot;   // [heads][T]: y_s - (the in-chunk part of x_s)
+  int dk_f32;
+};
+
+// sum over the 32 lanes of each half
+__device__ __forceinline__ float half_sum(float x) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+template <typename Tin, int DK, int DV>
+__global__ __launch_bounds__(2 * (DK > DV ? DK : DV), 1) void adjoint_kernel(AdjArgs f) {
+  constexpr int CH = kChunk<Tin>, NT = 2 * (DK > DV ? DK : DV), NW = NT / 64, TT = CH / 32;
+  constexpr int KT = DK / 32, VT = DV / 32;
+  using F = typename Frag<Tin>::T;
+  using TK = Tile<Tin, DK>;
+  using TV = Tile<Tin, DV>;
+  __shared__ __align__(16) Tin sq[CH * DK], sk[CH * DK], sv[CH * DV], so[CH * DV];
+  __shared__ __align__(16) Decays<CH> dec;
+  __shared__ float dots[(NW + 1) * CH];   // waves' parts of k . dk; then the rows' sums
+  const RecArgs& a = f.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5;
+  const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
+  const int b = head / a.H, h = head % a.H, c0 = 32 * wave;
+  const bool has_v = c0 < DV, has_k = c0 < DK;   // wave-uniform
+  const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
+  const Tin* q = row_base<const Tin>(f.q, b, h);
+  const Tin* k = row_base<const Tin>(f.k, b, h);
+  const Tin* v = row_base<const Tin>(f.v, b, h);
+  const Tin* dout = row_base<const Tin>(f.dout, b, h);
+  const float* gate = row_base<const float>(a.gate, b, h);
+  const int64_t D = (int64_t)DK * DV;
+
+  f32x16 R[KT], Rt[VT];   // columns c0.. of R [DK][DV], and of its transpose
+#pragma unroll
+  for (int i = 0; i < KT; ++i) R[i] = zero16();
+#pragma unroll
+  for (int i = 0; i < VT; ++i) Rt[i] = zero16();
+  const float* last = a.nseg > 1 ? a.seg_adj + ((int64_t)head * a.nseg + seg) * D
+                                 : (f.dstate ? f.dstate + head * D : nullptr);
+  if (last) {
+    if (has_v) load_state(R, last, DV, 1, c0, lane);
+    if (has_k) load_state(Rt, last, 1, DV, c0, lane);
+  }
+
+  Stage<Tin, DK, NT> gq, gk;
+  Stage<Tin, DV, NT> gv, go;
+  float gg = 0.f;
+  auto request = [&](int t0) {
+    gq.load(q, f.q.st, t0, lim, tid);
+    gk.load(k, f.k.st, t0, lim, tid);
+    gv.load(v, f.v.st, t0, lim, tid);
+    go.load(dout, f.dout.st, t0, lim, tid);
+    if (wave == 0) gg = (lane < CH && t0 + lane < lim) ? gate[(t0 + lane) * a.gate.st] : 0.f;
+  };
+  const int n = (end - begin + CH - 1) / CH;
+  request(begin + (n - 1) * CH);
+  for (int t0 = begin + (n - 1) * CH; t0 >= begin; t0 -= CH) {
+    __syncthreads();
+    gq.store(sq, tid);
+    gk.store(sk, tid);
+    gv.store(sv, tid);
+    go.store(so, tid);
+    for (int i = tid; i < (NW + 1) * CH; i += NT) dots[i] = 0.f;
+    if (wave == 0) form_decays<CH>(&dec, gg, lane);
+    __syncthreads();
+    if (t0 > begin) request(t0 - CH);
+
+    F qc[2 * TT], oc[2 * TT];   // the wave's columns of q and do, tokens along k
+#pragma unroll
+    for (int kk = 0; kk < 2 * TT; ++kk) {
+      qc[kk] = Frag<Tin>::zero();
+      oc[kk] = Frag<Tin>::zero();
+      if (has_k) qc[kk] = TK::template col_frag<false>(sq, c0, kk, lane);
+      if (has_v) oc[kk] = TV::template col_frag<false>(so, c0, kk, lane);
+    }
+#pragma unroll
+    for (int st = 0; st < TT; ++st) {
+      const int sl = 32 * st + (lane & 31), s = t0 + sl;
+      F kf[DK / 16], vf[DV / 16];
+#pragma unroll
+      for (int kk = 0; kk < DK / 16; ++kk) kf[kk] = TK::row_frag(sk, sl, kk, lane);
+#pragma unroll
+      for (int kk = 0; kk < DV / 16; ++kk) vf[kk] = TV::row_frag(sv, sl, kk, lane);
+      const float hi = dec.hi[sl], lo = dec.lo[sl];
+      f32x16 dv = zero16(), dk = zero16();
+#pragma unroll
+      for (int ut = st; ut < TT; ++ut) {
+        f32x16 p = zero16(), z = zero16();
+#pragma unroll
+        for (int kk = 0; kk < DK / 16; ++kk)
+          Frag<Tin>::mma(p, TK::row_frag(sq, 32 * ut + perm_row(lane & 31), kk, lane), kf[kk]);
+#pragma unroll
+        for (int kk = 0; kk < DV / 16; ++kk)
+          Frag<Tin>::mma(z, TV::row_frag(so, 32 * ut + perm_row(lane & 31), kk, lane), vf[kk]);
+        // the waves share out the score tiles' sums of A_us
+        const bool mine = (st * TT + ut) % NW == wave;
+        float col = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          float hu[8], lu[8], x[8], y[8], pair[8];
+          weights8(dec.hi, 2 * ut + kk, lane, hu);
+          weights8(dec.lo, 2 * ut + kk, lane, lu);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int u = 32 * ut + 16 * kk + 8 * g + e;
+            const float d = decay2(hu[e], lu[e], hi, lo) * a.scale;
+            x[e] = u >= sl ? p[8 * kk + e] * d : 0.f;
+            y[e] = u >= sl ? z[8 * kk + e] * d : 0.f;
+            pair[e] = u > sl ? x[e] * z[8 * kk + e] : 0.f;
+          }
+          Frag<Tin>::mma(dv, oc[2 * ut + kk], Frag<Tin>::from_floats(x));
+          Frag<Tin>::mma(dk, qc[2 * ut + kk], Frag<Tin>::from_floats(y));
+          if (mine) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              col += pair[e];
+              const float row = half_sum(pair[e]);
+              if ((lane & 31) == 0) atomicAdd(&dots[NW * CH + 32 * ut + 16 * kk + 8 * g + e], row);
+            }
+          }
+        }
+        if (mine) {
+          col += __shfl_xor(col, 32);
+          if (g == 0) dots[wave * CH + sl] += col;
+        }
+      }
+      const float w = dec.out[sl];
+      if (has_v) {
+        f32x16 c = zero16();
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) Frag<Tin>::mma(c, state_frag<Tin>(R[i], kk), kf[2 * i + kk]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dv[r] = s < lim ? dv[r] + c[r] * w : 0.f;
+        if (s < end) store_out(row_base<Tin>(f.dv, b, h) + s * f.dv.st, c0, dv, lane);
+      }
+      if (has_k) {
+        f32x16 c = zero16();
+#pragma unroll
+        for (int i = 0; i < VT; ++i)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            const F x = state_frag<Tin>(Rt[i], kk);
+            // what adds up along the sequence: see the dq pass
+            if constexpr (sizeof(Tin) == 2) Frag<Tin>::mma(c, state_frag_low(Rt[i], kk, x), vf[2 * i + kk]);
+            Frag<Tin>::mma(c, x, vf[2 * i + kk]);
+          }
+        float dot = 0.f;
+#pragma unroll
+        for (int bb = 0; bb < 4; ++bb) {
+          float y[4];
+          load4f(sk + TK::at(sl, c0 + 8 * bb + 4 * g), y);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = 4 * bb + j;
+            c[r] *= w;
+            dot += c[r] * y[j];
+            dk[r] = s < lim ? dk[r] + c[r] : 0.f;
+          }
+        }
+        dot += __shfl_xor(dot, 32);
+        if (g == 0) dots[wave * CH + sl] += dot;
+        if (s < end) {
+          if (f.dk_f32) store_out(row_base<float>(f.dk, b, h) + s * f.dk.st, c0, dk, lane);
+          else store_out(row_base<Tin>(f.dk, b, h) + s * f.dk.st, c0, dk, lane);
+        }
+      }
+    }
+    const float total = dec.total;
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) R[i][r] *= total;
+#pragma unroll
+    for (int i = 0; i < VT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) Rt[i][r] *= total;
+#pragma unroll
+    for (int kk = 0; kk < 2 * TT; ++kk) {
+      float w[8];
+      weights8(dec.in, kk, lane, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] *= a.scale;
+      if (has_v) {
+        const Scaled<Tin> y(oc[kk], w);
+#pragma unroll
+        for (int i = 0; i < KT; ++i) y.mma_b(R[i], TK::template col_frag<true>(sq, 32 * i, kk, lane));
+      }
+      if (has_k) {
+        const Scaled<Tin> y(qc[kk], w);
+#pragma unroll
+        for (int i = 0; i < VT; ++i) y.mma_b(Rt[i], TV::template col_frag<true>(so, 32 * i, kk, lane));
+      }
+    }
+    __syncthreads();
+    if (tid < CH && t0 + tid < end) {
+      float x = -dots[NW * CH + tid];
+#pragma unroll
+      for (int w = 0; w < NW; ++w) x += dots[w * CH + tid];
+      f.kdot[(int64_t)head * a.T + t0 + tid] = t0 + tid < lim ? x : 0.f;
+    }
+  }
+  if (seg == 0 && f.ds0 && has_v) store_state(R, f.ds0 + head * D, DV, 1, c0, lane);
+}
+
+// dg from the tokens' sums, from the last token back, in float64: what is added up spans
+// the sequence, what is left may be small.  A cut gate lets nothing through: dg is zero
+// there and the sum starts anew, exactly.  Two passes over blocks of tokens: each block's
+// sum back to its first cut, then the tokens.
+struct DgArgs {
+  RecArgs a;
+  const float* qdot;
+  const float* kdot;
+  const float* end_dot;
+  double* block_sum;
+  int* block_cut;
+  Rows dg;
+  int dtype;
+};
+
+constexpr int kPer = kDgateBlock / 256;
+
+__device__ __forceinline__ void later(double& x, int& cut, double y, int ycut) {
+  // x, cut: the part before; y, ycut: the part behind it
+  if (!cut) x += y;
+  cut |= ycut;
+}
+
+template <bool LAST>
+__global__ __launch_bounds__(256) void dgate_kernel(DgArgs f) {
+  const RecArgs& a = f.a;
+  const int nb = gridDim.x, block = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
+  const int lane = tid & 63, wave = tid >> 6;
+  const int b = head / a.H, h = head % a.H;
+  const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const float* gate = row_base<const float>(a.gate, b, h);
+  __shared__ double sums[4];
+  __shared__ int cuts[4];
+  const int64_t t0 = (int64_t)block * kDgateBlock + tid * kPer;
+  double x[kPer];
+  int cut[kPer];
+  double sum = 0.0;   // of the thread's tokens, from the last back to the first cut
+  int any = 0;
+#pragma unroll
+  for (int i = kPer - 1; i >= 0; --i) {
+    const int64_t t = t0 + i;
+    x[i] = 0.0;
+    cut[i] = 0;
+    if (t < lim) {
+      x[i] = (double)f.qdot[(int64_t)head * a.T + t] - (double)f.kdot[(int64_t)head * a.T + t];
+      cut[i] = gate[t * a.gate.st] < kCutGate;
+    }
+    // a cut at t: what is at t and behind it counts for no earlier token
+    double s = x[i];
+    int c = cut[i];
+    if (c) s = 0.0;
+    later(s, c, sum, any);
+    sum = s;
+    any = c;
+  }
+  // this thread's sum and those of the threads behind it in the wave
+  double ws = sum;
+  int wc = any;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_down(ws, o);
+    const int c = __shfl_down(wc, o);
+    if (lane + o < 64) later(ws, wc, y, c);
+  }
+  if (lane == 0) {
+    sums[wave] = ws;
+    cuts[wave] = wc;
+  }
+  __syncthreads();
+  if constexpr (!LAST) {
+    if (tid == 0) {
+      double s = sums[0];
+      int c = cuts[0];
+      for (int w = 1; w < 4; ++w) later(s, c, sums[w], cuts[w]);
+      f.block_sum[(int64_t)head * nb + block] = s;
+      f.block_cut[(int64_t)head * nb + block] = c;
+    }
+  } else {
+    // what is behind this thread: the rest of its wave, the waves and blocks behind
+    double s = __shfl_down(ws, 1);
+    int c = __shfl_down(wc, 1);
+    if (lane == 63) {
+      s = 0.0;
+      c = 0;
+    }
+    for (int w = wave + 1; w < 4; ++w) later(s, c, sums[w], cuts[w]);
+    for (int i = block + 1; i < nb && !c; ++i)
+      later(s, c, f.block_sum[(int64_t)head * nb + i], f.block_cut[(int64_t)head * nb + i]);
+    if (!c && f.end_dot) s += (double)f.end_dot[head];
+#pragma unroll
+    for (int i = kPer - 1; i >= 0; --i) {
+      const int64_t t = t0 + i;
+      s = cut[i] ? 0.0 : s + x[i];
+      if (t < a.T) {
+        const float y = t < lim ? (float)s : 0.f;
+        const int64_t at = b * f.dg.sb + h * f.dg.sh + t * f.dg.st;
+        if (f.dtype == DLA_BF16) static_cast<__bf16*>(f.dg.p)[at] = (__bf16)y;
+        else static_cast<float*>(f.dg.p)[at] = y;
+      }
+    }
+  }
+}
+
+// [B][H][T][d] float32 -> the sum over the H / Hk heads of each key head, four columns a
+// thread, heads in order.
+template <typename Tin>
+__global__ __launch_bounds__(256) void head_sum_kernel(RecArgs a, const float* part, Rows out) {
+  const int n4 = a.dk / 4, G = a.H / a.Hk;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)a.T * n4;
+  if (i >= per) return;
+  const int64_t t = i / n4, c = 4 * (i % n4);
+  const int b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk;
+  const float* p = part + (((int64_t)b * a.H + hk * G) * a.T + t) * a.dk + c;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int j = 0; j < G; ++j) {
+    const float4 x = *reinterpret_cast<const float4*>(p + (int64_t)j * a.T * a.dk);
+    s.x += x.x;
+    s.y += x.y;
+    s.z += x.z;
+    s.w += x.w;
+  }
+  store4(static_cast<Tin*>(out.p) + b * out.sb + hk * out.sh + t * out.st + c, s.x, s.y, s.z, s.w);
+}
+
+template <typename Tin, int DK, int DV>
+hipError_t run_adjoint(const AdjArgs& f, hipStream_t st) {
+  hipLaunchKernelGGL((adjoint_kernel<Tin, DK, DV>), dim3(f.a.B * f.a.H * f.a.nseg),
+                     dim3(2 * (DK > DV ? DK : DV)), 0, st, f);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_recurrence_adjoint(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
+                                     const Rows& v, const Rows& dout, const Rows& dk, bool dk_f32,
+                                     const Rows& dv, const float* dstate, float* ds0, float* kdot,
+                                     hipStream_t st) {
+  AdjArgs f;
+  f.a = a;
+  f.q = q;
+  f.k = k;
+  f.v = v;
+  f.dout = dout;
+  f.dk = dk;
+  f.dv = dv;
+  f.dstate = dstate;
+  f.ds0 = ds0;
+  f.kdot = kdot;
+  f.dk_f32 = dk_f32 ? 1 : 0;
+  if (dtype == DLA_BF16) {
+    if (a.dk == 128) return a.dv == 128 ? run_adjoint<bf16_t, 128, 128>(f, st) : run_adjoint<bf16_t, 128, 64>(f, st);
+    return a.dv == 128 ? run_adjoint<bf16_t, 64, 128>(f, st) : run_adjoint<bf16_t, 64, 64>(f, st);
+  }
+  if (a.dk == 128) return a.dv == 128 ? run_adjoint<float, 128, 128>(f, st) : run_adjoint<float, 128, 64>(f, st);
+  return a.dv == 128 ? run_adjoint<float, 64, 128>(f, st) : run_adjoint<float, 64, 64>(f, st);
+}
+
+hipError_t launch_recurrence_dgate(const RecArgs& a, int dtype, const float* qdot, const float* kdot,
+                                   const float* end_dot, double* block_sum, int* block_cut,
+                                   const Rows& dg, hipStream_t st) {
+  DgArgs f{a, qdot, kdot, end_dot, block_sum, block_cut, dg, dtype};
+  const dim3 grid((a.T + kDgateBlock - 1) / kDgateBlock, a.B * a.H);
+  if (grid.x > 1) hipLaunchKernelGGL((dgate_kernel<false>), grid, dim3(256), 0, st, f);
+  hipLaunchKernelGGL((dgate_kernel<true>), grid, dim3(256), 0, st, f);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_sum(const RecArgs& a, int dtype, const float* part, const Rows& out,
+                           hipStream_t st) {
+  const dim3 grid((unsigned)(((int64_t)a.T * a.dk / 4 + 255) / 256), a.B * a.Hk);
+  if (dtype == DLA_BF16) hipLaunchKernelGGL((head_sum_kernel<bf16_t>), grid, dim3(256), 0, st, a, part, out);
+  else hipLaunchKernelGGL((head_sum_kernel<float>), grid, dim3(256), 0, st, a, part, out);
+  return hipGetLastError();
+}
+
+}  // namespace dla

@@ -1,0 +1,32 @@
+// Launches of the root-mean-square norm (rms_norm.hip).
+#pragma once
+#include "dla_common.h"
+
+namespace dla {
+
+struct NormRows {
+  void* p = nullptr;
+  int64_t st = 0;   // elements from row to row
+};
+
+struct NormArgs {
+  int64_t rows;
+  int D;
+  float eps;
+  const void* w;
+  int w_f32;
+  // forward: x, residual, h = x + residual, y; backward: dx, dres, h, dy
+  NormRows x, res, h, y;
+  float* rstd;
+  float* y_scale;
+  float* dw_part;   // [slots][D]
+  int slots;
+};
+
+int norm_threads(int64_t rows, int pieces);
+int norm_slots(int64_t rows, int pieces);
+// kind 0: forward; 1: forward with 8-bit output; 2: backward
+hipError_t launch_norm(const NormArgs& a, int dtype, int kind, hipStream_t st);
+hipError_t launch_norm_dw(const NormArgs& a, float* dw, hipStream_t st);
+
+}  // namespace dla

@@ -1,0 +1,318 @@
+// Root-mean-square norm of a residual stream: h = x + residual, y = w h / rms(h), with y in
+// the inputs' type or in 8 bits with a scale per row; and its backward pass.
+//
+// A row lies in the registers of NT threads, NP pieces of 16 bytes each: one wave per row
+// where that holds it (no LDS, no barrier) and rows are many, a workgroup otherwise.  Rows
+// are read once and written once, so bytes bound the forward pass, and the backward pass
+// but for dw: a workgroup goes over many rows with dw's sums of its columns in registers,
+// leaves one partial sum per column, and a second kernel adds those up in a fixed order.
+// Rows may start at any element: a piece is read as it lies, whatever its alignment.
+#include "dla_common.h"
+#include "dla_train.h"
+#include "rms_norm.h"
+
+namespace dla {
+namespace {
+
+template <typename T>
+struct Piece {
+  static constexpr int N = 16 / (int)sizeof(T);
+  struct __attribute__((packed, aligned(sizeof(T)))) Raw {
+    uint32_t w[4];
+  };
+  __device__ static __forceinline__ void load(const T* p, int n, float (&x)[N]) {
+    if (n >= N) {
+      const Raw r = *reinterpret_cast<const Raw*>(p);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if constexpr (sizeof(T) == 2) x[i] = __uint_as_float(i & 1 ? r.w[i >> 1] & 0xFFFF0000u : r.w[i >> 1] << 16);
+        else x[i] = __uint_as_float(r.w[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = i < n ? to_f32(p[i]) : 0.f;
+    }
+  }
+  __device__ static __forceinline__ void store(T* p, int n, const float (&x)[N]) {
+    if constexpr (sizeof(T) == 2) {
+      if (n >= N) {
+        Raw r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+          bf16x2 y;
+          y[0] = (__bf16)x[2 * i];
+          y[1] = (__bf16)x[2 * i + 1];
+          r.w[i] = __builtin_bit_cast(uint32_t, y);
+        }
+        *reinterpret_cast<Raw*>(p) = r;
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (i < n) reinterpret_cast<__bf16*>(p)[i] = (__bf16)x[i];
+      }
+    } else {
+      if (n >= N) {
+        Raw r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = __float_as_uint(x[i]);
+        *reinterpret_cast<Raw*>(p) = r;
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (i < n) p[i] = x[i];
+      }
+    }
+  }
+};
+
+// Eight-bit floating point (4 exponent, 3 mantissa bits, no infinity), round to nearest
+// even; |x| <= 448 or NaN.
+template <int N>
+__device__ __forceinline__ void store_f8(uint8_t* p, int n, const float (&x)[N]) {
+  struct __attribute__((packed, aligned(1))) Raw {
+    uint32_t w[N / 4];
+  } r;
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    uint32_t u = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], 0, false);
+    r.w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], u, true);
+  }
+  if (n >= N) {
+    *reinterpret_cast<Raw*>(p) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = (uint8_t)(r.w[i >> 2] >> (8 * (i & 3)));
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void load_weight(const NormArgs& a, int i, int n, float (&w)[Piece<T>::N]) {
+  if (sizeof(T) == 4 || a.w_f32) {
+#pragma unroll
+    for (int j = 0; j < Piece<T>::N; ++j) w[j] = j < n ? static_cast<const float*>(a.w)[i + j] : 0.f;
+  } else {
+    Piece<T>::load(static_cast<const T*>(a.w) + i, n, w);
+  }
+}
+
+// A sum (or, with MAX, a maximum that lets a NaN through) over the NT threads of a row.
+template <int NT, bool MAX>
+__device__ __forceinline__ float over_row(float x, float* lds) {
+  auto both = [](float p, float q) { return MAX ? (q > p || q != q ? q : p) : p + q; };
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x = both(x, __shfl_xor(x, o));
+  if constexpr (NT > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) x = both(x, lds[i]);
+  }
+  return x;
+}
+
+template <typename T, int NT, int NP, bool F8>
+__global__ __launch_bounds__(NT > 256 ? NT : 256) void norm_kernel(NormArgs a) {
+  constexpr int N = Piece<T>::N, PER = NT > 256 ? 1 : 256 / NT;
+  __shared__ float lds[NT / 64];
+  const int tid = threadIdx.x % NT;
+  const int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / NT;
+  if (row >= a.rows) return;   // whole waves, and whole workgroups where they share a row
+  float h[NP][N], w[NP][N], sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int c = (i * NT + tid) * N, n = a.D - c;
+#pragma unroll
+    for (int j = 0; j < N; ++j) h[i][j] = 0.f;
+    if (n > 0) {
+      Piece<T>::load(static_cast<const T*>(a.x.p) + row * a.x.st + c, n, h[i]);
+      if (a.res.p) {
+        float r[N];
+        Piece<T>::load(static_cast<const T*>(a.res.p) + row * a.res.st + c, n, r);
+#pragma unroll
+        for (int j = 0; j < N; ++j) h[i][j] += r[j];
+      }
+      load_weight<T>(a, c, n, w[i]);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum += h[i][j] * h[i][j];
+  }
+  sum = over_row<NT, false>(sum, lds);
+  const float rstd = 1.f / sqrtf(sum / (float)a.D + a.eps);
+  if (a.rstd && tid == 0) a.rstd[row] = rstd;
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int c = (i * NT + tid) * N, n = a.D - c;
+    if (n > 0) {
+      if (a.h.p) Piece<T>::store(static_cast<T*>(a.h.p) + row * a.h.st + c, n, h[i]);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        h[i][j] = h[i][j] * rstd * w[i][j];
+        if constexpr (F8) {
+          const float y = j < n ? fabsf(h[i][j]) : 0.f;
+          top = y > top || y != y ? y : top;
+        }
+      }
+      if constexpr (!F8) Piece<T>::store(static_cast<T*>(a.y.p) + row * a.y.st + c, n, h[i]);
+    }
+  }
+  if constexpr (F8) {
+    top = over_row<NT, true>(top, lds);
+    if (tid == 0) a.y_scale[row] = top / 448.f;
+    const float inv = top > 0.f ? 448.f / top : (top == 0.f ? 0.f : top);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (i * NT + tid) * N, n = a.D - c;
+      if (n > 0) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          // past 448 by rounding only
+          const float y = h[i][j] * inv;
+          h[i][j] = y > 448.f ? 448.f : (y < -448.f ? -448.f : y);
+        }
+        store_f8(static_cast<uint8_t*>(a.y.p) + row * a.y.st + c, n, h[i]);
+      }
+    }
+  }
+}
+
+// dx = (dn - n mean(dn n)) / rms + dres with n = h / rms and dn = dy w; dw = sum of dy n
+template <typename T, int NT, int NP>
+__global__ __launch_bounds__(NT > 256 ? NT : 256) void norm_backward_kernel(NormArgs a) {
+  constexpr int N = Piece<T>::N, PER = NT > 256 ? 1 : 256 / NT;
+  __shared__ float lds[NT / 64];
+  const int tid = threadIdx.x % NT, slot = blockIdx.x * PER + threadIdx.x / NT;
+  const int slots = gridDim.x * PER;
+  float w[NP][N], dw[NP][N];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int c = (i * NT + tid) * N, n = a.D - c;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      dw[i][j] = 0.f;
+      w[i][j] = 0.f;
+    }
+    if (n > 0) load_weight<T>(a, c, n, w[i]);
+  }
+  // slots is a whole number of workgroups' rows, so a workgroup's waves end together
+  for (int64_t row = slot; row < a.rows; row += slots) {
+    const float rstd = a.rstd[row];
+    float dy[NP][N], n_[NP][N], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (i * NT + tid) * N, n = a.D - c;
+#pragma unroll
+      for (int j = 0; j < N; ++j) dy[i][j] = n_[i][j] = 0.f;
+      if (n > 0) {
+        Piece<T>::load(static_cast<const T*>(a.y.p) + row * a.y.st + c, n, dy[i]);
+        Piece<T>::load(static_cast<const T*>(a.h.p) + row * a.h.st + c, n, n_[i]);
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        n_[i][j] *= rstd;
+        dw[i][j] += dy[i][j] * n_[i][j];
+        dy[i][j] *= w[i][j];
+        sum += dy[i][j] * n_[i][j];
+      }
+    }
+    const float mean = over_row<NT, false>(sum, lds) / (float)a.D;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (i * NT + tid) * N, n = a.D - c;
+      if (n > 0) {
+        float r[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) r[j] = 0.f;
+        if (a.res.p) Piece<T>::load(static_cast<const T*>(a.res.p) + row * a.res.st + c, n, r);
+#pragma unroll
+        for (int j = 0; j < N; ++j) r[j] += (dy[i][j] - n_[i][j] * mean) * rstd;
+        Piece<T>::store(static_cast<T*>(a.x.p) + row * a.x.st + c, n, r);
+      }
+    }
+  }
+  if (!a.dw_part) return;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int c = (i * NT + tid) * N;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (c + j < a.D) a.dw_part[(int64_t)slot * a.D + c + j] = dw[i][j];
+  }
+}
+
+// dw[c] = sum over the slots' parts, 16 rows of 64 columns a workgroup
+__global__ __launch_bounds__(1024) void dw_kernel(const float* part, int slots, int D, float* dw) {
+  __shared__ float sums[16][64];
+  const int col = threadIdx.x & 63, r = threadIdx.x >> 6, c = blockIdx.x * 64 + col;
+  float s = 0.f;
+  if (c < D)
+    for (int i = r; i < slots; i += 16) s += part[(int64_t)i * D + c];
+  sums[r][col] = s;
+  __syncthreads();
+  if (r == 0 && c < D) {
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x += sums[i][col];
+    dw[c] = x;
+  }
+}
+
+template <typename T, int NT, int NP>
+hipError_t go(const NormArgs& a, int kind, hipStream_t st) {
+  constexpr int PER = NT > 256 ? 1 : 256 / NT, BLOCK = NT > 256 ? NT : 256;
+  const dim3 grid((unsigned)((a.rows + PER - 1) / PER)), block(BLOCK);
+  if (kind == 0) hipLaunchKernelGGL((norm_kernel<T, NT, NP, false>), grid, block, 0, st, a);
+  else if (kind == 1) hipLaunchKernelGGL((norm_kernel<T, NT, NP, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((norm_backward_kernel<T, NT, NP>), dim3(a.slots / PER), block, 0, st, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t pick(const NormArgs& a, int kind, hipStream_t st) {
+  const int pieces = (a.D + Piece<T>::N - 1) / Piece<T>::N;
+  switch (norm_threads(a.rows, pieces)) {
+    case 64:
+      if (pieces <= 64) return go<T, 64, 1>(a, kind, st);
+      if (pieces <= 128) return go<T, 64, 2>(a, kind, st);
+      return go<T, 64, 4>(a, kind, st);
+    case 256:
+      if (pieces <= 256) return go<T, 256, 1>(a, kind, st);
+      if (pieces <= 512) return go<T, 256, 2>(a, kind, st);
+      if (pieces <= 1024) return go<T, 256, 4>(a, kind, st);
+      return go<T, 256, 8>(a, kind, st);
+    default:   // float32 rows of more than 8192 values
+      if constexpr (sizeof(T) == 4) return go<T, 1024, 4>(a, kind, st);
+      return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+// Threads that share a row: a wave where it holds the row in 4 pieces a lane and there are
+// rows enough to fill the chip, else 256, past 2048 pieces 1024.
+int norm_threads(int64_t rows, int pieces) {
+  if (pieces <= 64 || (pieces <= 256 && rows >= 1024)) return 64;
+  return pieces <= 2048 ? 256 : 1024;
+}
+
+// Rows that the backward pass works on at a time, each leaving one partial dw.
+int norm_slots(int64_t rows, int pieces) {
+  const int nt = norm_threads(rows, pieces), per = nt > 256 ? 1 : 256 / nt;
+  const int64_t groups = (rows + per - 1) / per;
+  return (int)(groups < 512 ? groups : 512) * per;
+}
+
+hipError_t launch_norm(const NormArgs& a, int dtype, int kind, hipStream_t st) {
+  return dtype == DLA_BF16 ? pick<bf16_t>(a, kind, st) : pick<float>(a, kind, st);
+}
+
+hipError_t launch_norm_dw(const NormArgs& a, float* dw, hipStream_t st) {
+  hipLaunchKernelGGL(dw_kernel, dim3((a.D + 63) / 64), dim3(1024), 0, st, a.dw_part, a.slots, a.D, dw);
+  return hipGetLastError();
+}
+
+}  // namespace dla

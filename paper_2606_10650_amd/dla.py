@@ -29,7 +29,11 @@ EXPORTED = ("dla_cache_layout_of", "dla_state_cache_alloc", "dla_cache_flags",
             "dla_cache_header_check", "dla_prefill_workspace_size", "dla_prefill_segment_count",
             "dla_prefill_segment_starts", "dla_prefill", "dla_prefill_static", "dla_decode_step",
             "dla_decode_step_delta", "dla_prefill_delta_workspace_size", "dla_prefill_delta",
-            "dla_status_string", "dla_get_last_error", "dla_peak_mfma_bf16", "dla_peak_hbm_read")
+            "dla_status_string", "dla_get_last_error", "dla_peak_mfma_bf16", "dla_peak_hbm_read",
+            # bound by paper_2606_10650_amd.train
+            "dla_recurrence_workspace_size", "dla_recurrence_forward", "dla_recurrence_backward",
+            "dla_rms_norm", "dla_rms_norm_fp8", "dla_rms_norm_workspace_size",
+            "dla_rms_norm_backward", "dla_adamw_step")
 STATIC_SCRATCH_BYTES = 128 << 20   # DLA_STATIC_SCRATCH_BYTES
 
 

@@ -1,0 +1,346 @@
+"""Python binding of libdla's training operators (include/dla_train.h): the
+single-state recurrence of the base model with its backward pass, the
+root-mean-square norm of the residual stream, and AdamW.  Argument marshalling
+only: the work is the library's, torch provides device memory and the current
+stream.
+
+Below the calls, the same as differentiable functions (`Recurrence`, `RMSNorm`)
+for a model written in torch.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import dla
+from .dla import DLA_BF16, DLA_F32, _check, _dtype_code, _ptr, _stream
+
+DLA_STATE_FP8 = 2
+FP8 = torch.float8_e4m3fn
+FP8_BLOCK = 256          # elements per scale of 8-bit optimizer states
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64)]
+
+
+class RecurrenceDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32),
+                ("T", ctypes.c_int32), ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("lengths", ctypes.c_void_p)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class NormRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p),
+                ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float)]
+
+
+class AdamWParams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64),
+                ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("state_format", ctypes.c_int32), ("seed", ctypes.c_uint32),
+                ("grad_scale", ctypes.c_void_p)]
+
+
+_bound = False
+
+
+def lib():
+    """libdla.so with the training entry points declared."""
+    global _bound
+    L = dla.lib()
+    if not _bound:
+        P, S, I = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
+        ref = ctypes.POINTER
+        R, N = ref(Rows), ref(NormRows)
+        L.dla_recurrence_workspace_size.argtypes = [ref(RecurrenceDesc), I, ref(S)]
+        L.dla_recurrence_forward.argtypes = [ref(RecurrenceDesc), R, R, R, R, P, R, P, P, S, P]
+        L.dla_recurrence_backward.argtypes = [ref(RecurrenceDesc), R, R, R, R, P, R, P, R, R, R, R,
+                                              P, P, S, P]
+        L.dla_rms_norm.argtypes = [ref(NormDesc), N, N, P, N, N, P, P]
+        L.dla_rms_norm_fp8.argtypes = [ref(NormDesc), N, N, P, N, N, P, P]
+        L.dla_rms_norm_workspace_size.argtypes = [ref(NormDesc), ref(S)]
+        L.dla_rms_norm_backward.argtypes = [ref(NormDesc), N, N, P, P, N, N, P, P, S, P]
+        L.dla_adamw_step.argtypes = [ref(AdamWTensor), I, ref(AdamWParams), P]
+        for name in dla.EXPORTED:
+            if name.startswith(("dla_recurrence", "dla_rms_norm", "dla_adamw")):
+                getattr(L, name).restype = ctypes.c_int
+        _bound = True
+    return L
+
+
+# ---------------------------------------------------------------------------
+# recurrence
+# ---------------------------------------------------------------------------
+def _rows(t, name, d=None):
+    """dla_rows of a [B, heads, T, d] tensor, or of a [B, H, T] one (d None)."""
+    if t is None:
+        return None
+    if t.dim() != (3 if d is None else 4):
+        raise ValueError(f"{name}: {t.dim()} dimensions")
+    if d is not None and (t.shape[3] != d or (d > 1 and t.numel() and t.stride(3) != 1)):
+        raise ValueError(f"{name}: the last axis must be {d} contiguous values")
+    return ctypes.byref(Rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)))
+
+
+def _rec_desc(B, H, Hk, T, d_k, d_v, dtype, scale=1.0, lengths=None):
+    return RecurrenceDesc(B, H, Hk, T, d_k, d_v, _dtype_code(dtype), float(scale),
+                          None if lengths is None else lengths.data_ptr())
+
+
+def recurrence_workspace_bytes(B: int, H: int, Hk: int, T: int, d_k: int, d_v: int, dtype, *,
+                               backward: bool = False) -> int:
+    """Workspace of a forward (or backward) pass; 0 where none is needed."""
+    n = ctypes.c_size_t(0)
+    _check(lib().dla_recurrence_workspace_size(
+        ctypes.byref(_rec_desc(B, H, Hk, T, d_k, d_v, dtype)), int(backward), ctypes.byref(n)),
+        "dla_recurrence_workspace_size")
+    return int(n.value)
+
+
+def _checked(q, k, v, g, lengths, more):
+    """Shapes, types and devices of a call; (B, H, Hk, T, d_k, d_v)."""
+    B, Hk, T, d_k = q.shape
+    H, d_v = v.shape[1], v.shape[3]
+    if k.shape != q.shape or v.shape != (B, H, T, d_v) or g.shape != (B, H, T):
+        raise ValueError(f"shapes {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}, {tuple(g.shape)}")
+    if g.dtype != torch.float32:
+        raise ValueError("gates must be float32")
+    if lengths is not None and (lengths.shape != (B,) or lengths.dtype != torch.int32 or
+                                not lengths.is_contiguous()):
+        raise ValueError("lengths must be int32 [B], contiguous")
+    state = (B, H, d_k, d_v)
+    for t, shape, dtype in [(k, None, q.dtype), (v, None, q.dtype), (g, None, None), (lengths, None, None)] + more:
+        if t is None:
+            continue
+        if t.device != q.device or (dtype is not None and t.dtype != dtype):
+            raise ValueError(f"a tensor of type {t.dtype} on {t.device}, with q {q.dtype} on {q.device}")
+        if shape == "state":
+            if t.shape != state or t.dtype != torch.float32 or not t.is_contiguous():
+                raise ValueError(f"states must be float32 {state}, contiguous")
+        elif shape is not None and tuple(t.shape) != shape:
+            raise ValueError(f"shape {tuple(t.shape)}, not {shape}")
+    return B, H, Hk, T, d_k, d_v
+
+
+def _space(workspace, need, device):
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _token_major(B, heads, T, d, dtype, device):
+    """[B, heads, T, d], laid out [B][T][heads][d] as projections read it."""
+    return torch.empty((B, T, heads, d), dtype=dtype, device=device).transpose(1, 2)
+
+
+def recurrence(q, k, v, g, *, scale: float = 1.0, state=None, lengths=None, out=None,
+               state_out=None, want_state: bool = False, workspace=None):
+    """S_t = exp(g_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t (dla_recurrence_forward).
+    q, k: [B, Hk, T, d_k]; v: [B, H, T, d_v]; g: [B, H, T] float32, in any layout with the
+    last axis of q, k and v contiguous and its rows 16-byte aligned.  state: [B, H, d_k,
+    d_v] float32 or None; state_out may be the same tensor.  Returns (out, state_out); out
+    is laid out [B][T][H][d_v] unless given."""
+    B, H, Hk, T, d_k, d_v = _checked(q, k, v, g, lengths,
+                                     [(state, "state", None), (state_out, "state", None),
+                                      (out, tuple(v.shape), q.dtype)])
+    if out is None:
+        out = _token_major(B, H, T, d_v, v.dtype, v.device)
+    if state_out is None and want_state:
+        state_out = torch.empty((B, H, d_k, d_v), dtype=torch.float32, device=v.device)
+    need = recurrence_workspace_bytes(B, H, Hk, T, d_k, d_v, q.dtype)
+    workspace, size = _space(workspace, need, q.device) if need else (None, 0)
+    desc = _rec_desc(B, H, Hk, T, d_k, d_v, q.dtype, scale, lengths)
+    _check(lib().dla_recurrence_forward(
+        ctypes.byref(desc), _rows(q, "q", d_k), _rows(k, "k", d_k), _rows(v, "v", d_v),
+        _rows(g, "g"), _ptr(state), _rows(out, "out", d_v), _ptr(state_out), _ptr(workspace), size,
+        _stream(q.device)), "dla_recurrence_forward")
+    return out, state_out
+
+
+def recurrence_backward(q, k, v, g, dout, *, scale: float = 1.0, state=None, dstate=None,
+                        lengths=None, want_dstate: Optional[bool] = None, workspace=None):
+    """Gradients of `recurrence` (dla_recurrence_backward) from those of its outputs, dout
+    and dstate (None: zero).  Returns dq, dk, dv, dg, all of the inputs' type, and the
+    gradient of `state` (float32; None without one, unless want_dstate)."""
+    B, H, Hk, T, d_k, d_v = _checked(q, k, v, g, lengths,
+                                     [(state, "state", None), (dstate, "state", None),
+                                      (dout, tuple(v.shape), q.dtype)])
+    dq = _token_major(B, Hk, T, d_k, q.dtype, q.device)
+    dk = _token_major(B, Hk, T, d_k, q.dtype, q.device)
+    dv = _token_major(B, H, T, d_v, q.dtype, q.device)
+    dg = torch.empty((B, T, H), dtype=q.dtype, device=q.device).transpose(1, 2)
+    ds0 = None
+    if state is not None if want_dstate is None else want_dstate:
+        ds0 = torch.empty((B, H, d_k, d_v), dtype=torch.float32, device=q.device)
+    need = recurrence_workspace_bytes(B, H, Hk, T, d_k, d_v, q.dtype, backward=True)
+    workspace, size = _space(workspace, need, q.device) if need else (None, 0)
+    desc = _rec_desc(B, H, Hk, T, d_k, d_v, q.dtype, scale, lengths)
+    _check(lib().dla_recurrence_backward(
+        ctypes.byref(desc), _rows(q, "q", d_k), _rows(k, "k", d_k), _rows(v, "v", d_v),
+        _rows(g, "g"), _ptr(state), _rows(dout, "dout", d_v), _ptr(dstate), _rows(dq, "dq", d_k),
+        _rows(dk, "dk", d_k), _rows(dv, "dv", d_v), _rows(dg, "dg"), _ptr(ds0), _ptr(workspace),
+        size, _stream(q.device)), "dla_recurrence_backward")
+    return dq, dk, dv, dg, ds0
+
+
+# ---------------------------------------------------------------------------
+# norm
+# ---------------------------------------------------------------------------
+def _norm_rows(t, shape, dtype, device, name):
+    if t is None:
+        return None
+    if tuple(t.shape) != shape or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, not {dtype} {shape} on {device}")
+    if shape[1] > 1 and t.numel() and t.stride(1) != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return ctypes.byref(NormRows(t.data_ptr(), t.stride(0)))
+
+
+def _norm_desc(x, weight, eps):
+    if x.dim() != 2 or weight.shape != (x.shape[1],) or not weight.is_contiguous() or \
+            weight.device != x.device:
+        raise ValueError(f"shapes {tuple(x.shape)}, {tuple(weight.shape)}: rows [N, D] and a weight [D] are wanted")
+    return NormDesc(x.shape[0], x.shape[1], _dtype_code(x.dtype), _dtype_code(weight.dtype), float(eps))
+
+
+def _norm_forward(call, x, weight, residual, eps, y, last):
+    shape, dev = tuple(x.shape), x.device
+    h = torch.empty(shape, dtype=x.dtype, device=dev) if residual is not None else None
+    desc = _norm_desc(x, weight, eps)
+    _check(getattr(lib(), call)(
+        ctypes.byref(desc), _norm_rows(x, shape, x.dtype, dev, "x"),
+        _norm_rows(residual, shape, x.dtype, dev, "residual"), _ptr(weight),
+        _norm_rows(h, shape, x.dtype, dev, "h"), _norm_rows(y, shape, y.dtype, dev, "y"),
+        _ptr(last), _stream(dev)), call)
+    return x if h is None else h
+
+
+def rms_norm(x, weight, residual=None, *, eps: float = 1e-6):
+    """h = x + residual, y = weight h / sqrt(mean(h^2) + eps) (dla_rms_norm).  x, residual:
+    [N, D].  Returns (y, h, rstd); h is x itself without a residual."""
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    rstd = torch.empty(x.shape[:1], dtype=torch.float32, device=x.device)
+    return y, _norm_forward("dla_rms_norm", x, weight, residual, eps, y, rstd), rstd
+
+
+def rms_norm_fp8(x, weight, residual=None, *, eps: float = 1e-6):
+    """The same with y in 8 bits (dla_rms_norm_fp8): returns (y float8_e4m3fn, h, scale),
+    y times its row's scale being the norm's output."""
+    y = torch.empty(x.shape, dtype=FP8, device=x.device)
+    scale = torch.empty(x.shape[:1], dtype=torch.float32, device=x.device)
+    return y, _norm_forward("dla_rms_norm_fp8", x, weight, residual, eps, y, scale), scale
+
+
+def rms_norm_workspace_bytes(rows: int, D: int, dtype=torch.bfloat16) -> int:
+    """Workspace of rms_norm_backward for rows of D values."""
+    n = ctypes.c_size_t(0)
+    code = _dtype_code(dtype)
+    _check(lib().dla_rms_norm_workspace_size(ctypes.byref(NormDesc(rows, D, code, code, 0.0)),
+                                             ctypes.byref(n)), "dla_rms_norm_workspace_size")
+    return int(n.value)
+
+
+def rms_norm_backward(dy, h, weight, rstd, dres=None, *, workspace=None):
+    """Gradients of rms_norm from dy and dres, those of its outputs y and h (None: zero):
+    (dx, which is also the residual's, and dweight in float32)."""
+    shape, dev, dt = tuple(h.shape), h.device, h.dtype
+    desc = _norm_desc(h, weight, 0.0)
+    if rstd.shape != shape[:1] or rstd.dtype != torch.float32 or not rstd.is_contiguous() or rstd.device != dev:
+        raise ValueError("rstd must be float32 [N], contiguous")
+    dx = torch.empty(shape, dtype=dt, device=dev)
+    dw = torch.empty(shape[1:], dtype=torch.float32, device=dev)
+    workspace, size = _space(workspace, rms_norm_workspace_bytes(*shape, dt), dev)
+    _check(lib().dla_rms_norm_backward(
+        ctypes.byref(desc), _norm_rows(dy, shape, dt, dev, "dy"), _norm_rows(h, shape, dt, dev, "h"),
+        _ptr(weight), _ptr(rstd), _norm_rows(dres, shape, dt, dev, "dres"),
+        _norm_rows(dx, shape, dt, dev, "dx"), _ptr(dw), _ptr(workspace), size, _stream(dev)),
+        "dla_rms_norm_backward")
+    return dx, dw
+
+
+# ---------------------------------------------------------------------------
+# AdamW
+# ---------------------------------------------------------------------------
+class AdamW:
+    """AdamW over many tensors at once (dla_adamw_step).  `add` names a tensor and its
+    buffers, which the caller keeps; `step` updates all of them in place on the current
+    stream.  Without m and v, `add` makes their states, zeroed, in the given format.
+    Tensors may differ in type; those of a kind go in the same launches."""
+
+    def __init__(self, states: str = "f32"):
+        if states not in ("f32", "fp8"):
+            raise ValueError(f"states {states!r}: f32 or fp8")
+        self.states = states
+        self.kept = []       # the tensors of each entry
+        self._groups = {}    # (param, grad type, format) -> entries
+        self._arrays = None
+
+    def add(self, param, grad, m=None, v=None, *, master=None, m_scale=None, v_scale=None,
+            weight_decay: float = 0.0):
+        n, dev = param.numel(), param.device
+        if m is None and v is None:
+            if self.states == "fp8":
+                m, v = (torch.zeros(n, dtype=torch.uint8, device=dev).view(FP8) for _ in range(2))
+                m_scale, v_scale = (torch.zeros(-(-n // FP8_BLOCK), device=dev) for _ in range(2))
+            else:
+                m, v = (torch.zeros(n, device=dev) for _ in range(2))
+        fp8 = m.dtype == FP8
+        if v.dtype != m.dtype or m.dtype not in (torch.float32, FP8):
+            raise ValueError(f"states of types {m.dtype}, {v.dtype}")
+        if fp8 and (m_scale is None or v_scale is None):
+            raise ValueError("8-bit states need their scales")
+        sizes = [(param, n, None), (grad, n, None), (m, n, None), (v, n, None),
+                 (master, n, torch.float32)]
+        if fp8:
+            sizes += [(t, -(-n // FP8_BLOCK), torch.float32) for t in (m_scale, v_scale)]
+        for t, size, dtype in sizes:
+            if t is not None and (t.numel() != size or not t.is_contiguous() or t.device != dev or
+                                  (dtype is not None and t.dtype != dtype)):
+                raise ValueError(f"a buffer of {t.numel()} {t.dtype} on {t.device} where {size} "
+                                 f"contiguous elements on {dev} are wanted")
+        key = (_dtype_code(param.dtype), _dtype_code(grad.dtype), DLA_STATE_FP8 if fp8 else DLA_F32, dev)
+        self._groups.setdefault(key, []).append(
+            (param, master, grad, m, v, m_scale if fp8 else None, v_scale if fp8 else None, n,
+             float(weight_decay)))
+        self.kept.append({"param": param, "master": master, "m": m, "v": v, "m_scale": m_scale,
+                          "v_scale": v_scale})
+        self._arrays = None
+
+    def _marshal(self):
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._arrays = [(key, (AdamWTensor * len(ts))(*[AdamWTensor(*map(ptr, t[:7]), *t[7:]) for t in ts]))
+                        for key, ts in self._groups.items()]
+
+    def step(self, step: int, *, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, seed: int = 0,
+             grad_scale=None):
+        """The step-th update (from 1).  seed: of 8-bit states' rounding, 0 for nearest.
+        grad_scale: a float32 tensor of one element, or None; the step changes nothing where
+        it is not finite."""
+        if self._arrays is None:
+            self._marshal()
+        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+            raise ValueError("grad_scale must be one float32")
+        for (p, g, fmt, dev), arr in self._arrays:
+            if grad_scale is not None and grad_scale.device != dev:
+                raise ValueError(f"grad_scale on {grad_scale.device}, tensors on {dev}")
+            args = AdamWParams(lr, betas[0], betas[1], eps, step, p, g, fmt, seed & 0xFFFFFFFF,
+                               None if grad_scale is None else grad_scale.data_ptr())
+            _check(lib().dla_adamw_step(arr, len(arr), ctypes.byref(args), _stream(dev)),
+                   "dla_adamw_step")
