@@ -41,10 +41,14 @@ struct RecArgs {
   float* seg_state;    // [heads][nseg][dk][dv], the state before each segment
   float* seg_adj;      // [heads][nseg][dk][dv], the adjoint behind each segment
   float* seg_decay;    // [heads][nseg]
+  float4* decays;      // [heads][chunks * kRecChunk], see recurrence_tile.h
 };
 
-// Tokens per chunk: what a workgroup takes at a time.
-inline int rec_chunk(int dtype) { return dtype == DLA_BF16 ? 64 : 32; }
+constexpr int kRecChunk = 32;   // tokens a workgroup takes at a time
+__host__ __device__ inline int64_t rec_padded(int T) { return ((int64_t)T + kRecChunk - 1) / kRecChunk * kRecChunk; }
+
+// Every token's decays within its chunk, for the chunk kernels of a call.
+hipError_t launch_recurrence_decays(const RecArgs& a, hipStream_t st);
 
 // Forward over segments: out (and the last state).
 hipError_t launch_recurrence_forward(const RecArgs& a, int dtype, const Rows& q, const Rows& k,

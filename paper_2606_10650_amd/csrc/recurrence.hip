@@ -29,15 +29,52 @@ struct FwdArgs {
   int out_f32;
 };
 
+// Decays of a chunk's tokens, a half-wave per chunk.
+__global__ __launch_bounds__(256) void decays_kernel(RecArgs a) {
+  const int64_t padded = rec_padded(a.T), chunks = padded / kChunk;
+  const int lane = threadIdx.x & 31;
+  const int64_t c = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int head = blockIdx.y, b = head / a.H, h = head % a.H;
+  const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int64_t t = c * kChunk + lane;
+  const float gate = t < lim ? row_base<const float>(a.gate, b, h)[t * a.gate.st] : 0.f;
+  const bool cut = gate < kCutGate;
+  double x = cut ? 0.0 : (double)gate * 1.4426950408889634;
+  int n = cut ? 1 : 0;
+#pragma unroll
+  for (int o = 1; o < kChunk; o <<= 1) {
+    const double y = __shfl_up(x, o, kChunk);
+    const int m = __shfl_up(n, o, kChunk);
+    if (lane >= o) {
+      x += y;
+      n += m;
+    }
+  }
+  const double w = rint(x);
+  const float hi = (float)w - 131072.f * (float)n, lo = (float)(x - w);
+  const float eh = __shfl(hi, kChunk - 1, kChunk), el = __shfl(lo, kChunk - 1, kChunk);
+  if (c < chunks)
+    a.decays[head * padded + t] = make_float4(hi, lo, decay2(hi, lo, 0.f, 0.f), decay2(eh, el, hi, lo));
+}
+
+// A lane's 16 columns of its token's row, as floats (see store_out)
+__device__ __forceinline__ void load16(const bf16_t* p, u32x4 (&x)[4]) {
+  x[0] = *reinterpret_cast<const u32x4*>(p);
+  x[1] = *reinterpret_cast<const u32x4*>(p + 16);
+}
+__device__ __forceinline__ void load16(const float* p, u32x4 (&x)[4]) {
+  x[0] = *reinterpret_cast<const u32x4*>(p);
+  x[1] = *reinterpret_cast<const u32x4*>(p + 4);
+  x[2] = *reinterpret_cast<const u32x4*>(p + 16);
+  x[3] = *reinterpret_cast<const u32x4*>(p + 20);
+}
+
 template <typename Tin, int DK, int DV, bool DQ>
 __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
-  constexpr int CH = kChunk<Tin>, NT = 2 * DV, NW = DV / 32, TT = CH / 32, ST = DK / 32;
-  using F = typename Frag<Tin>::T;
-  using TK = Tile<Tin, DK>;
-  using TV = Tile<Tin, DV>;
-  __shared__ __align__(16) Tin sq[CH * DK], sk[CH * DK], sv[CH * DV];
-  __shared__ __align__(16) Decays<CH> dec;
-  __shared__ float dots[DQ ? NW * CH : 1];
+  constexpr int NT = 2 * DV, NW = DV / 32, ST = DK / 32;
+  __shared__ __align__(16) Tin sq[kChunk * DK], sk[kChunk * DK], sv[kChunk * DV];
+  __shared__ __align__(16) Decays dec;
+  __shared__ float dots[DQ ? NW * kChunk : 1];
   const RecArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5;
   const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
@@ -47,7 +84,8 @@ __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
   const Tin* q = row_base<const Tin>(f.q, b, h);
   const Tin* k = row_base<const Tin>(f.k, b, h);
   const Tin* v = row_base<const Tin>(f.v, b, h);
-  const float* gate = row_base<const float>(a.gate, b, h);
+  const Tin* x = DQ ? row_base<const Tin>(f.x, b, h) + c0 + 8 * g : nullptr;
+  const float4* decays = a.decays + head * rec_padded(a.T);
   const int64_t D = (int64_t)DK * DV;
 
   f32x16 S[ST];
@@ -62,111 +100,54 @@ __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
 
   Stage<Tin, DK, NT> gq, gk;
   Stage<Tin, DV, NT> gv;
-  float gg = 0.f;
+  float4 gd;
+  u32x4 gx[4];
   auto request = [&](int t0) {
     gq.load(q, f.q.st, t0, lim, tid);
     gk.load(k, f.k.st, t0, lim, tid);
     gv.load(v, f.v.st, t0, lim, tid);
-    if (wave == 0) gg = (lane < CH && t0 + lane < lim) ? gate[(t0 + lane) * a.gate.st] : 0.f;
+    if (tid < kChunk) gd = decays[t0 + tid];
   };
   request(begin);
-  for (int t0 = begin; t0 < end; t0 += CH) {
+  for (int t0 = begin; t0 < end; t0 += kChunk) {
     __syncthreads();   // the last chunk's tiles are read
     gq.store(sq, tid);
     gk.store(sk, tid);
     gv.store(sv, tid);
-    if (wave == 0) form_decays<CH>(&dec, gg, lane);
+    if (tid < kChunk) dec.store(gd, tid);
     __syncthreads();
-    if (t0 + CH < end) request(t0 + CH);
-
-    F vf[2 * TT];
+    const int t = t0 + (lane & 31);
+    if constexpr (DQ) {
 #pragma unroll
-    for (int kk = 0; kk < 2 * TT; ++kk) vf[kk] = TV::template col_frag<false>(sv, c0, kk, lane);
-#pragma unroll
-    for (int tt = 0; tt < TT; ++tt) {
-      const int tl = 32 * tt + (lane & 31), t = t0 + tl;
-      F qf[DK / 16];
-#pragma unroll
-      for (int kk = 0; kk < DK / 16; ++kk) qf[kk] = TK::row_frag(sq, tl, kk, lane);
-      const float hi = dec.hi[tl], lo = dec.lo[tl];
-      f32x16 o = zero16();
-#pragma unroll
-      for (int st = 0; st <= tt; ++st) {
-        f32x16 p = zero16();
-#pragma unroll
-        for (int kk = 0; kk < DK / 16; ++kk)
-          Frag<Tin>::mma(p, TK::row_frag(sk, 32 * st + perm_row(lane & 31), kk, lane), qf[kk]);
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          float hs[8], ls[8], x[8];
-          weights8(dec.hi, 2 * st + kk, lane, hs);
-          weights8(dec.lo, 2 * st + kk, lane, ls);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int s = 32 * st + 16 * kk + 8 * g + e;
-            x[e] = s <= tl ? p[8 * kk + e] * decay2(hi, lo, hs[e], ls[e]) : 0.f;
-          }
-          Frag<Tin>::mma(o, vf[2 * st + kk], Frag<Tin>::from_floats(x));
-        }
-      }
-      f32x16 c = zero16();
-#pragma unroll
-      for (int i = 0; i < ST; ++i)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          const F s = state_frag<Tin>(S[i], kk);
-          // qdot adds up along the sequence, so what the rounding left counts there
-          if constexpr (DQ && sizeof(Tin) == 2)
-            Frag<Tin>::mma(c, state_frag_low(S[i], kk, s), qf[2 * i + kk]);
-          Frag<Tin>::mma(c, s, qf[2 * i + kk]);
-        }
-      const float in = dec.in[tl];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        c[r] *= in * a.scale;
-        o[r] = o[r] * a.scale + c[r];
-        if (t >= lim) o[r] = 0.f;
-      }
-      if constexpr (DQ) {
-        float dot = 0.f;
-        if (t < lim) {
-          const Tin* x = row_base<const Tin>(f.x, b, h) + t * f.x.st + c0;
-#pragma unroll
-          for (int bb = 0; bb < 4; ++bb) {
-            float y[4];
-            load4f(x + 8 * bb + 4 * g, y);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) dot += c[4 * bb + j] * y[j];
-          }
-        }
-        dot += __shfl_xor(dot, 32);
-        if (g == 0) dots[wave * CH + tl] = dot;
-      }
-      if (t < end) {
-        if (f.out_f32) store_out(row_base<float>(f.out, b, h) + t * f.out.st, c0, o, lane);
-        else store_out(row_base<Tin>(f.out, b, h) + t * f.out.st, c0, o, lane);
-      }
+      for (int i = 0; i < 4; ++i) gx[i] = u32x4{0u, 0u, 0u, 0u};
+      if (t < lim) load16(x + t * f.x.st, gx);
     }
-    const float total = dec.total;
+    if (t0 + kChunk < end) request(t0 + kChunk);
+    const float in = dec.in[lane & 31] * a.scale;
+    f32x16 p, c, o;
+    chunk_step<Tin, DK, DV, false, DQ>(sq, sk, sv, dec, 1.f, c0, lane, S, p, c, o);
 #pragma unroll
-    for (int i = 0; i < ST; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) S[i][r] *= total;
-#pragma unroll
-    for (int kk = 0; kk < 2 * TT; ++kk) {
-      float w[8];
-      weights8(dec.out, kk, lane, w);
-      const Scaled<Tin> y(vf[kk], w);
-#pragma unroll
-      for (int i = 0; i < ST; ++i) y.mma_b(S[i], TK::template col_frag<true>(sk, 32 * i, kk, lane));
+    for (int r = 0; r < 16; ++r) {
+      c[r] *= in;
+      o[r] = t < lim ? o[r] * a.scale + c[r] : 0.f;
+    }
+    if (t < end) {
+      if (DQ && f.out_f32) store_out(row_base<float>(f.out, b, h) + t * f.out.st, c0, o, lane);
+      else store_out(row_base<Tin>(f.out, b, h) + t * f.out.st, c0, o, lane);
     }
     if constexpr (DQ) {
-      __syncthreads();
-      if (tid < CH && t0 + tid < end) {
-        float x = 0.f;
+      constexpr int PE = 16 / (int)sizeof(Tin);
+      float dot = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) x += dots[w * CH + tid];
-        f.qdot[(int64_t)head * a.T + t0 + tid] = x;
+      for (int r = 0; r < 16; ++r) dot += c[r] * to_f32(piece_elem<Tin>(gx[r / PE], r % PE));
+      dot += __shfl_xor(dot, 32);
+      if (g == 0) dots[wave * kChunk + lane] = dot;
+      __syncthreads();
+      if (tid < kChunk && t0 + tid < end) {
+        float y = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) y += dots[w * kChunk + tid];
+        f.qdot[(int64_t)head * a.T + t0 + tid] = t0 + tid < lim ? y : 0.f;
       }
     }
   }
@@ -174,21 +155,22 @@ __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
     if (f.s_out) store_state(S, f.s_out + head * D, f.s_rs, f.s_cs, c0, lane);
     if constexpr (DQ) {
       if (f.dstate) {
-        float x = 0.f;
+        float y = 0.f;
 #pragma unroll
         for (int i = 0; i < ST; ++i)
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            x += S[i][r] * f.dstate[head * D + (32 * i + held_row(r, lane)) * f.s_rs + (c0 + (lane & 31)) * f.s_cs];
+            y += S[i][r] * f.dstate[head * D + (32 * i + held_row(r, lane)) * f.s_rs +
+                                    (c0 + perm_row(lane & 31)) * f.s_cs];
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+        for (int o = 1; o < 64; o <<= 1) y += __shfl_xor(y, o);
         __syncthreads();
-        if (lane == 0) dots[wave] = x;
+        if (lane == 0) dots[wave] = y;
         __syncthreads();
         if (tid == 0) {
-          float y = 0.f;
-          for (int w = 0; w < NW; ++w) y += dots[w];
-          f.end_dot[head] = y;
+          float z = 0.f;
+          for (int w = 0; w < NW; ++w) z += dots[w];
+          f.end_dot[head] = z;
         }
       }
     }
@@ -200,11 +182,9 @@ __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
 // the segment's start) q_s do_s^T.
 template <typename Tin, int DK, int DV, bool REV>
 __global__ __launch_bounds__(2 * DV, 2) void segment_kernel(RecArgs a, Rows xr, Rows yr, float* dst) {
-  constexpr int CH = kChunk<Tin>, NT = 2 * DV, TT = CH / 32, ST = DK / 32;
-  using TK = Tile<Tin, DK>;
-  using TV = Tile<Tin, DV>;
-  __shared__ __align__(16) Tin sk[CH * DK], sv[CH * DV];
-  __shared__ __align__(16) Decays<CH> dec;
+  constexpr int NT = 2 * DV, ST = DK / 32;
+  __shared__ __align__(16) Tin sk[kChunk * DK], sv[kChunk * DV];
+  __shared__ __align__(16) Decays dec;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
   const int b = head / a.H, h = head % a.H, c0 = 32 * wave;
@@ -212,46 +192,46 @@ __global__ __launch_bounds__(2 * DV, 2) void segment_kernel(RecArgs a, Rows xr, 
   const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
   const Tin* x = row_base<const Tin>(xr, b, h);
   const Tin* y = row_base<const Tin>(yr, b, h);
-  const float* gate = row_base<const float>(a.gate, b, h);
+  const float4* decays = a.decays + head * rec_padded(a.T);
   f32x16 S[ST];
 #pragma unroll
   for (int i = 0; i < ST; ++i) S[i] = zero16();
   float decay = 1.f;
   Stage<Tin, DK, NT> gx;
   Stage<Tin, DV, NT> gy;
-  float gg = 0.f;
+  float4 gd;
   auto request = [&](int t0) {
     gx.load(x, xr.st, t0, lim, tid);
     gy.load(y, yr.st, t0, lim, tid);
-    if (wave == 0) gg = (lane < CH && t0 + lane < lim) ? gate[(t0 + lane) * a.gate.st] : 0.f;
+    if (tid < kChunk) gd = decays[t0 + tid];
   };
-  const int n = (end - begin + CH - 1) / CH;
-  auto chunk_at = [&](int c) { return begin + (REV ? n - 1 - c : c) * CH; };
+  const int n = (end - begin + kChunk - 1) / kChunk;
+  auto chunk_at = [&](int c) { return begin + (REV ? n - 1 - c : c) * kChunk; };
   request(chunk_at(0));
   for (int c = 0; c < n; ++c) {
     __syncthreads();
     gx.store(sk, tid);
     gy.store(sv, tid);
-    if (wave == 0) form_decays<CH>(&dec, gg, lane);
+    if (tid < kChunk) dec.store(gd, tid);
     __syncthreads();
     if (c + 1 < n) request(chunk_at(c + 1));
-    const float total = dec.total;
+    const float total = dec.total();
     decay *= total;
 #pragma unroll
     for (int i = 0; i < ST; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) S[i][r] *= total;
 #pragma unroll
-    for (int kk = 0; kk < 2 * TT; ++kk) {
+    for (int kk = 0; kk < 2; ++kk) {
       float w[8];
       weights8(REV ? dec.in : dec.out, kk, lane, w);
       if constexpr (REV) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] *= a.scale;
       }
-      const Scaled<Tin> z(TV::template col_frag<false>(sv, c0, kk, lane), w);
+      const Scaled<Tin> z(Tile<Tin, DV>::col_frag(sv, c0, kk, lane), w);
 #pragma unroll
-      for (int i = 0; i < ST; ++i) z.mma_b(S[i], TK::template col_frag<true>(sk, 32 * i, kk, lane));
+      for (int i = 0; i < ST; ++i) z.mma_b(S[i], Tile<Tin, DK>::col_frag(sk, 32 * i, kk, lane));
     }
   }
   store_state(S, dst + ((int64_t)head * a.nseg + seg) * DK * DV, DV, 1, c0, lane);
@@ -309,6 +289,12 @@ hipError_t run_segments(const RecArgs& a, bool rev, const Rows& x, const Rows& y
 }
 
 }  // namespace
+
+hipError_t launch_recurrence_decays(const RecArgs& a, hipStream_t st) {
+  const int64_t chunks = rec_padded(a.T) / kChunk;
+  hipLaunchKernelGGL(decays_kernel, dim3((unsigned)((chunks + 7) / 8), a.B * a.H), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
 
 hipError_t launch_recurrence_segments(const RecArgs& a, int dtype, bool reverse, const Rows& x,
                                       const Rows& y, const float* first, hipStream_t st) {

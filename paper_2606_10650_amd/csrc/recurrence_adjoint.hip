@@ -6,9 +6,10 @@
 //   dv_s = e^{a_end - a_s} R^T k_s + scale sum_{u >= s} e^{a_u - a_s} (q_u . k_s) do_u
 //   dk_s = e^{a_end - a_s} R v_s   + scale sum_{u >= s} e^{a_u - a_s} (do_u . v_s) q_u
 //   R   <- e^{a_end} R + scale sum_u e^{a_u} q_u do_u^T.
-// dv contracts R over its rows and dk over its columns.  A wave holds 32 columns of R and
-// 32 columns of R^T, both in accumulators, which are the operands of those products as
-// they are; keeping R twice costs the products that update it and no pass through LDS.
+// dv contracts R over its rows and dk over its columns.  Half of the workgroup's waves hold
+// 32 columns each of R, the others 32 columns each of R^T, in accumulators that are the
+// operands of those products as they are; keeping R twice costs the products that update it
+// and no pass through LDS.  Both halves run recurrence_tile.h's chunk step, back in time.
 //
 // The gate's gradient: e^{g_t} scales what every token s < t leaves for every token u >= t,
 // so dg_t is the sum over those pairs of A_us = scale e^{a_u - a_s} (q_u . k_s)(do_u . v_s),
@@ -39,202 +40,137 @@ __device__ __forceinline__ float half_sum(float x) {
   return x;
 }
 
+// What the waves of a workgroup pass each other for the gate's gradient.
+template <int KW>
+struct PairSums {
+  float qk[16][64];            // q_u . k_s, element and lane of a score tile
+  float col[KW][kChunk];       // per wave of dk: y_s, and the carried k_s . dk_s
+  float row[KW][kChunk];       // per wave: its rows' x_u, else zero
+};
+
+// Waves 0 .. DV / 32 - 1 hold 32 columns each of R [DK][DV] and give dv; the others hold
+// those of its transpose and give dk.
 template <typename Tin, int DK, int DV>
-__global__ __launch_bounds__(2 * (DK > DV ? DK : DV), 1) void adjoint_kernel(AdjArgs f) {
-  constexpr int CH = kChunk<Tin>, NT = 2 * (DK > DV ? DK : DV), NW = NT / 64, TT = CH / 32;
-  constexpr int KT = DK / 32, VT = DV / 32;
-  using F = typename Frag<Tin>::T;
-  using TK = Tile<Tin, DK>;
-  using TV = Tile<Tin, DV>;
-  __shared__ __align__(16) Tin sq[CH * DK], sk[CH * DK], sv[CH * DV], so[CH * DV];
-  __shared__ __align__(16) Decays<CH> dec;
-  __shared__ float dots[(NW + 1) * CH];   // waves' parts of k . dk; then the rows' sums
+__global__ __launch_bounds__(2 * (DK + DV), 1) void adjoint_kernel(AdjArgs f) {
+  constexpr int NT = 2 * (DK + DV), KW = DK / 32, VW = DV / 32, PER = 16 / KW;
+  __shared__ __align__(16) Tin sq[kChunk * DK], sk[kChunk * DK], sv[kChunk * DV], so[kChunk * DV];
+  __shared__ __align__(16) Decays dec;
+  __shared__ PairSums<KW> pairs;
   const RecArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5;
   const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
-  const int b = head / a.H, h = head % a.H, c0 = 32 * wave;
-  const bool has_v = c0 < DV, has_k = c0 < DK;   // wave-uniform
+  const int b = head / a.H, h = head % a.H;
+  const bool of_v = wave < VW;
+  const int kw = wave - VW, c0 = 32 * (of_v ? wave : kw);
   const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
   const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
   const Tin* q = row_base<const Tin>(f.q, b, h);
   const Tin* k = row_base<const Tin>(f.k, b, h);
   const Tin* v = row_base<const Tin>(f.v, b, h);
   const Tin* dout = row_base<const Tin>(f.dout, b, h);
-  const float* gate = row_base<const float>(a.gate, b, h);
+  const float4* decays = a.decays + head * rec_padded(a.T);
   const int64_t D = (int64_t)DK * DV;
-
-  f32x16 R[KT], Rt[VT];   // columns c0.. of R [DK][DV], and of its transpose
-#pragma unroll
-  for (int i = 0; i < KT; ++i) R[i] = zero16();
-#pragma unroll
-  for (int i = 0; i < VT; ++i) Rt[i] = zero16();
-  const float* last = a.nseg > 1 ? a.seg_adj + ((int64_t)head * a.nseg + seg) * D
-                                 : (f.dstate ? f.dstate + head * D : nullptr);
-  if (last) {
-    if (has_v) load_state(R, last, DV, 1, c0, lane);
-    if (has_k) load_state(Rt, last, 1, DV, c0, lane);
-  }
 
   Stage<Tin, DK, NT> gq, gk;
   Stage<Tin, DV, NT> gv, go;
-  float gg = 0.f;
+  float4 gd;
   auto request = [&](int t0) {
     gq.load(q, f.q.st, t0, lim, tid);
     gk.load(k, f.k.st, t0, lim, tid);
     gv.load(v, f.v.st, t0, lim, tid);
     go.load(dout, f.dout.st, t0, lim, tid);
-    if (wave == 0) gg = (lane < CH && t0 + lane < lim) ? gate[(t0 + lane) * a.gate.st] : 0.f;
+    if (tid < kChunk) gd = decays[t0 + tid];
   };
-  const int n = (end - begin + CH - 1) / CH;
-  request(begin + (n - 1) * CH);
-  for (int t0 = begin + (n - 1) * CH; t0 >= begin; t0 -= CH) {
-    __syncthreads();
+  auto stage = [&](int t0) {
+    __syncthreads();   // the last chunk's tiles are read
     gq.store(sq, tid);
     gk.store(sk, tid);
     gv.store(sv, tid);
     go.store(so, tid);
-    for (int i = tid; i < (NW + 1) * CH; i += NT) dots[i] = 0.f;
-    if (wave == 0) form_decays<CH>(&dec, gg, lane);
+    if (tid < kChunk) dec.store(gd, tid);
     __syncthreads();
-    if (t0 > begin) request(t0 - CH);
-
-    F qc[2 * TT], oc[2 * TT];   // the wave's columns of q and do, tokens along k
+    if (t0 > begin) request(t0 - kChunk);
+  };
+  const float* last = a.nseg > 1 ? a.seg_adj + ((int64_t)head * a.nseg + seg) * D
+                                 : (f.dstate ? f.dstate + head * D : nullptr);
+  const int t_last = begin + (end - begin - 1) / kChunk * kChunk;
+  request(t_last);
+  if (of_v) {
+    f32x16 R[DK / 32];
 #pragma unroll
-    for (int kk = 0; kk < 2 * TT; ++kk) {
-      qc[kk] = Frag<Tin>::zero();
-      oc[kk] = Frag<Tin>::zero();
-      if (has_k) qc[kk] = TK::template col_frag<false>(sq, c0, kk, lane);
-      if (has_v) oc[kk] = TV::template col_frag<false>(so, c0, kk, lane);
+    for (int i = 0; i < DK / 32; ++i) R[i] = zero16();
+    if (last) load_state(R, last, DV, 1, c0, lane);
+    for (int t0 = t_last; t0 >= begin; t0 -= kChunk) {
+      stage(t0);
+      const int s = t0 + (lane & 31);
+      const float w = dec.out[lane & 31];
+      f32x16 p, c, o;
+      chunk_step<Tin, DK, DV, true, false>(sk, sq, so, dec, a.scale, c0, lane, R, p, c, o);
+      // the first wave's scores, for the waves of dk
+      if (wave == 0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) pairs.qk[r][lane] = p[r];
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[r] = s < lim ? o[r] * a.scale + c[r] * w : 0.f;
+      if (s < end) store_out(row_base<Tin>(f.dv, b, h) + s * f.dv.st, c0, o, lane);
+      __syncthreads();
+      __syncthreads();
     }
+    if (seg == 0 && f.ds0) store_state(R, f.ds0 + head * D, DV, 1, c0, lane);
+  } else {
+    f32x16 R[DV / 32];
 #pragma unroll
-    for (int st = 0; st < TT; ++st) {
-      const int sl = 32 * st + (lane & 31), s = t0 + sl;
-      F kf[DK / 16], vf[DV / 16];
+    for (int i = 0; i < DV / 32; ++i) R[i] = zero16();
+    if (last) load_state(R, last, 1, DV, c0, lane);
+    for (int t0 = t_last; t0 >= begin; t0 -= kChunk) {
+      stage(t0);
+      const int sl = lane & 31, s = t0 + sl;
+      const float w = dec.out[sl], hi = dec.hi[sl], lo = dec.lo[sl];
+      f32x16 p, c, o;
+      chunk_step<Tin, DV, DK, true, true>(sv, so, sq, dec, a.scale, c0, lane, R, p, c, o);
+      float dot = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < DK / 16; ++kk) kf[kk] = TK::row_frag(sk, sl, kk, lane);
+      for (int e = 0; e < 4; ++e) {
+        float y[4];
+        load4f(sk + Tile<Tin, DK>::at(sl, c0 + held_row(4 * e, lane)), y);
 #pragma unroll
-      for (int kk = 0; kk < DV / 16; ++kk) vf[kk] = TV::row_frag(sv, sl, kk, lane);
-      const float hi = dec.hi[sl], lo = dec.lo[sl];
-      f32x16 dv = zero16(), dk = zero16();
-#pragma unroll
-      for (int ut = st; ut < TT; ++ut) {
-        f32x16 p = zero16(), z = zero16();
-#pragma unroll
-        for (int kk = 0; kk < DK / 16; ++kk)
-          Frag<Tin>::mma(p, TK::row_frag(sq, 32 * ut + perm_row(lane & 31), kk, lane), kf[kk]);
-#pragma unroll
-        for (int kk = 0; kk < DV / 16; ++kk)
-          Frag<Tin>::mma(z, TV::row_frag(so, 32 * ut + perm_row(lane & 31), kk, lane), vf[kk]);
-        // the waves share out the score tiles' sums of A_us
-        const bool mine = (st * TT + ut) % NW == wave;
-        float col = 0.f;
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          float hu[8], lu[8], x[8], y[8], pair[8];
-          weights8(dec.hi, 2 * ut + kk, lane, hu);
-          weights8(dec.lo, 2 * ut + kk, lane, lu);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int u = 32 * ut + 16 * kk + 8 * g + e;
-            const float d = decay2(hu[e], lu[e], hi, lo) * a.scale;
-            x[e] = u >= sl ? p[8 * kk + e] * d : 0.f;
-            y[e] = u >= sl ? z[8 * kk + e] * d : 0.f;
-            pair[e] = u > sl ? x[e] * z[8 * kk + e] : 0.f;
-          }
-          Frag<Tin>::mma(dv, oc[2 * ut + kk], Frag<Tin>::from_floats(x));
-          Frag<Tin>::mma(dk, qc[2 * ut + kk], Frag<Tin>::from_floats(y));
-          if (mine) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              col += pair[e];
-              const float row = half_sum(pair[e]);
-              if ((lane & 31) == 0) atomicAdd(&dots[NW * CH + 32 * ut + 16 * kk + 8 * g + e], row);
-            }
-          }
-        }
-        if (mine) {
-          col += __shfl_xor(col, 32);
-          if (g == 0) dots[wave * CH + sl] += col;
+        for (int j = 0; j < 4; ++j) {
+          c[4 * e + j] *= w;
+          dot += c[4 * e + j] * y[j];
         }
       }
-      const float w = dec.out[sl];
-      if (has_v) {
-        f32x16 c = zero16();
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) Frag<Tin>::mma(c, state_frag<Tin>(R[i], kk), kf[2 * i + kk]);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dv[r] = s < lim ? dv[r] + c[r] * w : 0.f;
-        if (s < end) store_out(row_base<Tin>(f.dv, b, h) + s * f.dv.st, c0, dv, lane);
+      for (int r = 0; r < 16; ++r) o[r] = s < lim ? o[r] * a.scale + c[r] : 0.f;
+      if (s < end) {
+        if (f.dk_f32) store_out(row_base<float>(f.dk, b, h) + s * f.dk.st, c0, o, lane);
+        else store_out(row_base<Tin>(f.dk, b, h) + s * f.dk.st, c0, o, lane);
       }
-      if (has_k) {
-        f32x16 c = zero16();
+      __syncthreads();   // the scores of q and k are there
+      // The waves share out the pairs' sums, PER elements of the tile each: element r of a
+      // lane is the pair of its token s and token u = held_row(r).
 #pragma unroll
-        for (int i = 0; i < VT; ++i)
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {
-            const F x = state_frag<Tin>(Rt[i], kk);
-            // what adds up along the sequence: see the dq pass
-            if constexpr (sizeof(Tin) == 2) Frag<Tin>::mma(c, state_frag_low(Rt[i], kk, x), vf[2 * i + kk]);
-            Frag<Tin>::mma(c, x, vf[2 * i + kk]);
-          }
-        float dot = 0.f;
-#pragma unroll
-        for (int bb = 0; bb < 4; ++bb) {
-          float y[4];
-          load4f(sk + TK::at(sl, c0 + 8 * bb + 4 * g), y);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = 4 * bb + j;
-            c[r] *= w;
-            dot += c[r] * y[j];
-            dk[r] = s < lim ? dk[r] + c[r] : 0.f;
-          }
-        }
-        dot += __shfl_xor(dot, 32);
-        if (g == 0) dots[wave * CH + sl] += dot;
-        if (s < end) {
-          if (f.dk_f32) store_out(row_base<float>(f.dk, b, h) + s * f.dk.st, c0, dk, lane);
-          else store_out(row_base<Tin>(f.dk, b, h) + s * f.dk.st, c0, dk, lane);
-        }
+      for (int r = 0; r < 16; ++r) {
+        if (r / PER != kw) continue;
+        const int u = held_row(r, lane);
+        const float d = decay2(dec.hi[u], dec.lo[u], hi, lo) * a.scale;
+        const float pair = u > sl ? pairs.qk[r][lane] * p[r] * d : 0.f;
+        dot += pair;
+        const float row = half_sum(pair);
+        if (sl == 0) pairs.row[kw][u] = row;
       }
-    }
-    const float total = dec.total;
+      dot += __shfl_xor(dot, 32);
+      if (g == 0) pairs.col[kw][sl] = dot;
+      __syncthreads();
+      if (kw == 0 && lane < kChunk && s < end) {
+        float x = 0.f;
 #pragma unroll
-    for (int i = 0; i < KT; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) R[i][r] *= total;
-#pragma unroll
-    for (int i = 0; i < VT; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) Rt[i][r] *= total;
-#pragma unroll
-    for (int kk = 0; kk < 2 * TT; ++kk) {
-      float w[8];
-      weights8(dec.in, kk, lane, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] *= a.scale;
-      if (has_v) {
-        const Scaled<Tin> y(oc[kk], w);
-#pragma unroll
-        for (int i = 0; i < KT; ++i) y.mma_b(R[i], TK::template col_frag<true>(sq, 32 * i, kk, lane));
+        for (int i = 0; i < KW; ++i) x += pairs.col[i][lane];
+        x -= pairs.row[((lane & 7) + 8 * (lane >> 4)) / PER][lane];   // the wave that has element r of row u
+        f.kdot[(int64_t)head * a.T + s] = s < lim ? x : 0.f;
       }
-      if (has_k) {
-        const Scaled<Tin> y(qc[kk], w);
-#pragma unroll
-        for (int i = 0; i < VT; ++i) y.mma_b(Rt[i], TV::template col_frag<true>(so, 32 * i, kk, lane));
-      }
-    }
-    __syncthreads();
-    if (tid < CH && t0 + tid < end) {
-      float x = -dots[NW * CH + tid];
-#pragma unroll
-      for (int w = 0; w < NW; ++w) x += dots[w * CH + tid];
-      f.kdot[(int64_t)head * a.T + t0 + tid] = t0 + tid < lim ? x : 0.f;
     }
   }
-  if (seg == 0 && f.ds0 && has_v) store_state(R, f.ds0 + head * D, DV, 1, c0, lane);
 }
 
 // dg from the tokens' sums, from the last token back, in float64: what is added up spans
@@ -358,13 +294,24 @@ __global__ __launch_bounds__(256) void head_sum_kernel(RecArgs a, const float* p
     s.z += x.z;
     s.w += x.w;
   }
-  store4(static_cast<Tin*>(out.p) + b * out.sb + hk * out.sh + t * out.st + c, s.x, s.y, s.z, s.w);
+  Tin* dst = static_cast<Tin*>(out.p) + b * out.sb + hk * out.sh + t * out.st + c;
+  if constexpr (sizeof(Tin) == 2) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    bf16x4 y;
+    y[0] = (__bf16)s.x;
+    y[1] = (__bf16)s.y;
+    y[2] = (__bf16)s.z;
+    y[3] = (__bf16)s.w;
+    *reinterpret_cast<bf16x4*>(dst) = y;
+  } else {
+    *reinterpret_cast<float4*>(dst) = s;
+  }
 }
 
 template <typename Tin, int DK, int DV>
 hipError_t run_adjoint(const AdjArgs& f, hipStream_t st) {
   hipLaunchKernelGGL((adjoint_kernel<Tin, DK, DV>), dim3(f.a.B * f.a.H * f.a.nseg),
-                     dim3(2 * (DK > DV ? DK : DV)), 0, st, f);
+                     dim3(2 * (DK + DV)), 0, st, f);
   return hipGetLastError();
 }
 

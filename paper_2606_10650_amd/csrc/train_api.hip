@@ -29,12 +29,12 @@ struct Plan {
 Plan plan_of(const dla_recurrence_desc& d, bool backward) {
   Plan p;
   p.step = !backward && d.T <= kStepTokens;
-  const int chunk = rec_chunk(d.dtype), heads = d.B * d.H;
+  const int chunk = kRecChunk, heads = d.B * d.H;
   const int chunks = (d.T + chunk - 1) / chunk;
   int n = 1;
   if (heads < 256) {
     n = (512 + heads - 1) / heads;
-    if (n > chunks / 4) n = chunks / 4;
+    if (n > chunks / 8) n = chunks / 8;
     if (n > 64) n = 64;
     if (n < 1) n = 1;
   }
@@ -46,7 +46,7 @@ Plan plan_of(const dla_recurrence_desc& d, bool backward) {
 }
 
 struct Space {
-  size_t seg_state, seg_adj, seg_decay, qdot, kdot, end_dot, block_sum, block_cut, dq_part, dk_part, total;
+  size_t decays, seg_state, seg_adj, seg_decay, qdot, kdot, end_dot, block_sum, block_cut, dq_part, dk_part, total;
 };
 
 Space space_of(const dla_recurrence_desc& d, const Plan& p, bool backward) {
@@ -60,6 +60,7 @@ Space space_of(const dla_recurrence_desc& d, const Plan& p, bool backward) {
   };
   const size_t heads = (size_t)d.B * d.H, D = (size_t)d.d_k * d.d_v, tokens = heads * d.T;
   if (p.step || d.T == 0 || heads == 0) return s;
+  s.decays = take(heads * rec_padded(d.T) * 16);
   if (p.nseg > 1) {
     s.seg_state = take(heads * p.nseg * D * 4);
     if (backward) s.seg_adj = take(heads * p.nseg * D * 4);
@@ -121,6 +122,7 @@ RecArgs args_of(const dla_recurrence_desc& d, const Plan& p, const dla_rows* gat
   a.seg_state = (float*)(ws + s.seg_state);
   a.seg_adj = (float*)(ws + s.seg_adj);
   a.seg_decay = (float*)(ws + s.seg_decay);
+  a.decays = (float4*)(ws + s.decays);
   return a;
 }
 
@@ -239,7 +241,8 @@ dla_status dla_recurrence_forward(const dla_recurrence_desc* desc, const dla_row
   if (p.step) {
     r = launch_recurrence_step(a, d.dtype, qr, kr, vr, outr, state, state_out, st);
   } else {
-    if (p.nseg > 1) r = launch_recurrence_segments(a, d.dtype, false, kr, vr, state, st);
+    r = launch_recurrence_decays(a, st);
+    if (r == hipSuccess && p.nseg > 1) r = launch_recurrence_segments(a, d.dtype, false, kr, vr, state, st);
     if (r == hipSuccess) r = launch_recurrence_forward(a, d.dtype, qr, kr, vr, outr, state, state_out, st);
   }
   return remember(r == hipSuccess ? DLA_OK : DLA_ERR_HIP);
@@ -286,8 +289,8 @@ dla_status dla_recurrence_backward(const dla_recurrence_desc* desc, const dla_ro
   float* qdot = (float*)(ws + sp.qdot);
   float* kdot = (float*)(ws + sp.kdot);
   float* end_dot = (float*)(ws + sp.end_dot);
-  hipError_t r = hipSuccess;
-  if (p.nseg > 1) {
+  hipError_t r = launch_recurrence_decays(a, st);
+  if (r == hipSuccess && p.nseg > 1) {
     r = launch_recurrence_segments(a, d.dtype, false, kr, vr, state, st);
     if (r == hipSuccess) r = launch_recurrence_segments(a, d.dtype, true, qr, dor, dstate_out, st);
   }
