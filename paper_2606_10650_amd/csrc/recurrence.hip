@@ -9,7 +9,8 @@
 // itself, which costs a quarter more products and saves a barrier and a pass through LDS.
 //
 // dq_t = sum_{s <= t} e^{a_t - a_s} (do_t . v_s) k_s + e^{a_t} S do_t is the same with do,
-// v and k in the places of q, k and v and the state transposed.
+// v and k in the places of q, k and v and the state transposed.  That pass also leaves
+// qdot_t, what the pairs (s < t, t) give to the gates between them (recurrence_adjoint.hip).
 #include "recurrence_tile.h"
 
 namespace dla {
@@ -23,7 +24,7 @@ struct FwdArgs {
   const float* seg_state;  // state before each segment, or null: one segment
   float* s_out;            // state behind the last token, or null
   const float* dstate;     // dq only, or null
-  Rows x;                  // dq only: q, whose products with dq's carried part go to qdot
+  Rows x;                  // dq only: q
   float* qdot;
   float* end_dot;
   int out_f32;
@@ -57,24 +58,19 @@ __global__ __launch_bounds__(256) void decays_kernel(RecArgs a) {
     a.decays[head * padded + t] = make_float4(hi, lo, decay2(hi, lo, 0.f, 0.f), decay2(eh, el, hi, lo));
 }
 
-// A lane's 16 columns of its token's row, as floats (see store_out)
-__device__ __forceinline__ void load16(const bf16_t* p, u32x4 (&x)[4]) {
-  x[0] = *reinterpret_cast<const u32x4*>(p);
-  x[1] = *reinterpret_cast<const u32x4*>(p + 16);
-}
-__device__ __forceinline__ void load16(const float* p, u32x4 (&x)[4]) {
-  x[0] = *reinterpret_cast<const u32x4*>(p);
-  x[1] = *reinterpret_cast<const u32x4*>(p + 4);
-  x[2] = *reinterpret_cast<const u32x4*>(p + 16);
-  x[3] = *reinterpret_cast<const u32x4*>(p + 20);
-}
+// A chunk's tiles; two of them, so that the next chunk is stored while one is read and a
+// chunk takes one barrier.
+template <typename Tin, int DK, int DV, bool DQ>
+struct FwdTiles {
+  Tin q[kChunk * DK], k[kChunk * DK], v[kChunk * DV], x[DQ ? kChunk * DV : 8];
+  Decays dec;
+  float dots[DQ ? DV / 32 : 1][kChunk];
+};
 
 template <typename Tin, int DK, int DV, bool DQ>
-__global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
+__global__ __launch_bounds__(2 * DV, sizeof(Tin) == 2 ? 2 : 1) void forward_kernel(FwdArgs f) {
   constexpr int NT = 2 * DV, NW = DV / 32, ST = DK / 32;
-  __shared__ __align__(16) Tin sq[kChunk * DK], sk[kChunk * DK], sv[kChunk * DV];
-  __shared__ __align__(16) Decays dec;
-  __shared__ float dots[DQ ? NW * kChunk : 1];
+  __shared__ __align__(16) FwdTiles<Tin, DK, DV, DQ> tiles[2];
   const RecArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5;
   const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
@@ -84,10 +80,28 @@ __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
   const Tin* q = row_base<const Tin>(f.q, b, h);
   const Tin* k = row_base<const Tin>(f.k, b, h);
   const Tin* v = row_base<const Tin>(f.v, b, h);
-  const Tin* x = DQ ? row_base<const Tin>(f.x, b, h) + c0 + 8 * g : nullptr;
+  const Tin* x = DQ ? row_base<const Tin>(f.x, b, h) : nullptr;
   const float4* decays = a.decays + head * rec_padded(a.T);
   const int64_t D = (int64_t)DK * DV;
 
+  Stage<Tin, DK, NT> gq, gk;
+  Stage<Tin, DV, NT> gv, gx;
+  float4 gd;
+  auto request = [&](int t0) {
+    gq.load(q, f.q.st, t0, lim, tid);
+    gk.load(k, f.k.st, t0, lim, tid);
+    gv.load(v, f.v.st, t0, lim, tid);
+    if constexpr (DQ) gx.load(x, f.x.st, t0, lim, tid);
+    if (tid < kChunk) gd = decays[t0 + tid];
+  };
+  auto store = [&](FwdTiles<Tin, DK, DV, DQ>& to) {
+    gq.store(to.q, tid);
+    gk.store(to.k, tid);
+    gv.store(to.v, tid);
+    if constexpr (DQ) gx.store(to.x, tid);
+    if (tid < kChunk) to.dec.store(gd, tid);
+  };
+  request(begin);
   f32x16 S[ST];
   const float* first = f.seg_state ? f.seg_state + ((int64_t)head * a.nseg + seg) * D
                                    : (f.s0 ? f.s0 + head * D : nullptr);
@@ -97,60 +111,39 @@ __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
 #pragma unroll
     for (int i = 0; i < ST; ++i) S[i] = zero16();
   }
-
-  Stage<Tin, DK, NT> gq, gk;
-  Stage<Tin, DV, NT> gv;
-  float4 gd;
-  u32x4 gx[4];
-  auto request = [&](int t0) {
-    gq.load(q, f.q.st, t0, lim, tid);
-    gk.load(k, f.k.st, t0, lim, tid);
-    gv.load(v, f.v.st, t0, lim, tid);
-    if (tid < kChunk) gd = decays[t0 + tid];
-  };
-  request(begin);
-  for (int t0 = begin; t0 < end; t0 += kChunk) {
-    __syncthreads();   // the last chunk's tiles are read
-    gq.store(sq, tid);
-    gk.store(sk, tid);
-    gv.store(sv, tid);
-    if (tid < kChunk) dec.store(gd, tid);
-    __syncthreads();
-    const int t = t0 + (lane & 31);
-    if constexpr (DQ) {
+  store(tiles[0]);
+  __syncthreads();
+  int at = 0;
+  // the waves' parts of a chunk's dots, added up by the chunk's successor
+  auto sum_dots = [&](const FwdTiles<Tin, DK, DV, DQ>& from, int t0) {
+    if (tid < kChunk && t0 + tid < end) {
+      float y = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) gx[i] = u32x4{0u, 0u, 0u, 0u};
-      if (t < lim) load16(x + t * f.x.st, gx);
+      for (int w = 0; w < NW; ++w) y += from.dots[w][tid];
+      f.qdot[(int64_t)head * a.T + t0 + tid] = t0 + tid < lim ? y : 0.f;
+    }
+  };
+  for (int t0 = begin; t0 < end; t0 += kChunk, at ^= 1) {
+    FwdTiles<Tin, DK, DV, DQ>& now = tiles[at];
+    if constexpr (DQ) {
+      if (t0 > begin) sum_dots(tiles[at ^ 1], t0 - kChunk);
     }
     if (t0 + kChunk < end) request(t0 + kChunk);
-    const float in = dec.in[lane & 31] * a.scale;
-    f32x16 p, c, o;
-    chunk_step<Tin, DK, DV, false, DQ>(sq, sk, sv, dec, 1.f, c0, lane, S, p, c, o);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      c[r] *= in;
-      o[r] = t < lim ? o[r] * a.scale + c[r] : 0.f;
+    const int t = t0 + (lane & 31);
+    f32x16 o;
+    const float dot = chunk_step<Tin, DK, DV, false, DQ>(now.q, now.k, now.v, now.x, now.dec, a.scale, c0, lane, S, o);
+    if constexpr (DQ) {
+      if (g == 0) now.dots[wave][lane] = dot;
     }
+    if (t >= lim) o = zero16();
     if (t < end) {
       if (DQ && f.out_f32) store_out(row_base<float>(f.out, b, h) + t * f.out.st, c0, o, lane);
       else store_out(row_base<Tin>(f.out, b, h) + t * f.out.st, c0, o, lane);
     }
-    if constexpr (DQ) {
-      constexpr int PE = 16 / (int)sizeof(Tin);
-      float dot = 0.f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dot += c[r] * to_f32(piece_elem<Tin>(gx[r / PE], r % PE));
-      dot += __shfl_xor(dot, 32);
-      if (g == 0) dots[wave * kChunk + lane] = dot;
-      __syncthreads();
-      if (tid < kChunk && t0 + tid < end) {
-        float y = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) y += dots[w * kChunk + tid];
-        f.qdot[(int64_t)head * a.T + t0 + tid] = t0 + tid < lim ? y : 0.f;
-      }
-    }
+    if (t0 + kChunk < end) store(tiles[at ^ 1]);
+    __syncthreads();
   }
+  if constexpr (DQ) sum_dots(tiles[at ^ 1], begin + (end - begin - 1) / kChunk * kChunk);
   if (seg == a.nseg - 1) {
     if (f.s_out) store_state(S, f.s_out + head * D, f.s_rs, f.s_cs, c0, lane);
     if constexpr (DQ) {
@@ -164,12 +157,11 @@ __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
                                     (c0 + perm_row(lane & 31)) * f.s_cs];
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) y += __shfl_xor(y, o);
-        __syncthreads();
-        if (lane == 0) dots[wave] = y;
+        if (lane == 0) tiles[at].dots[wave][0] = y;
         __syncthreads();
         if (tid == 0) {
           float z = 0.f;
-          for (int w = 0; w < NW; ++w) z += dots[w];
+          for (int w = 0; w < NW; ++w) z += tiles[at].dots[w][0];
           f.end_dot[head] = z;
         }
       }
@@ -180,11 +172,16 @@ __global__ __launch_bounds__(2 * DV, 2) void forward_kernel(FwdArgs f) {
 // A segment's own part of the state behind it, sum over its tokens of (decay to the
 // segment's end) k_s v_s^T; reverse: of the adjoint before it, sum of scale (decay from
 // the segment's start) q_s do_s^T.
+template <typename Tin, int DK, int DV>
+struct SegTiles {
+  Tin k[kChunk * DK], v[kChunk * DV];
+  Decays dec;
+};
+
 template <typename Tin, int DK, int DV, bool REV>
-__global__ __launch_bounds__(2 * DV, 2) void segment_kernel(RecArgs a, Rows xr, Rows yr, float* dst) {
+__global__ __launch_bounds__(2 * DV, sizeof(Tin) == 2 ? 2 : 1) void segment_kernel(RecArgs a, Rows xr, Rows yr, float* dst) {
   constexpr int NT = 2 * DV, ST = DK / 32;
-  __shared__ __align__(16) Tin sk[kChunk * DK], sv[kChunk * DV];
-  __shared__ __align__(16) Decays dec;
+  __shared__ __align__(16) SegTiles<Tin, DK, DV> tiles[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
   const int b = head / a.H, h = head % a.H, c0 = 32 * wave;
@@ -205,17 +202,20 @@ __global__ __launch_bounds__(2 * DV, 2) void segment_kernel(RecArgs a, Rows xr, 
     gy.load(y, yr.st, t0, lim, tid);
     if (tid < kChunk) gd = decays[t0 + tid];
   };
+  auto store = [&](SegTiles<Tin, DK, DV>& to) {
+    gx.store(to.k, tid);
+    gy.store(to.v, tid);
+    if (tid < kChunk) to.dec.store(gd, tid);
+  };
   const int n = (end - begin + kChunk - 1) / kChunk;
   auto chunk_at = [&](int c) { return begin + (REV ? n - 1 - c : c) * kChunk; };
   request(chunk_at(0));
+  store(tiles[0]);
+  __syncthreads();
   for (int c = 0; c < n; ++c) {
-    __syncthreads();
-    gx.store(sk, tid);
-    gy.store(sv, tid);
-    if (tid < kChunk) dec.store(gd, tid);
-    __syncthreads();
+    const SegTiles<Tin, DK, DV>& now = tiles[c & 1];
     if (c + 1 < n) request(chunk_at(c + 1));
-    const float total = dec.total();
+    const float total = now.dec.total();
     decay *= total;
 #pragma unroll
     for (int i = 0; i < ST; ++i)
@@ -224,15 +224,17 @@ __global__ __launch_bounds__(2 * DV, 2) void segment_kernel(RecArgs a, Rows xr, 
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
       float w[8];
-      weights8(REV ? dec.in : dec.out, kk, lane, w);
+      weights8(REV ? now.dec.in : now.dec.out, kk, lane, w);
       if constexpr (REV) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] *= a.scale;
       }
-      const Scaled<Tin> z(Tile<Tin, DV>::col_frag(sv, c0, kk, lane), w);
+      const Scaled<Tin> z(Tile<Tin, DV>::col_frag(now.v, c0, kk, lane), w);
 #pragma unroll
-      for (int i = 0; i < ST; ++i) z.mma_b(S[i], Tile<Tin, DK>::col_frag(sk, 32 * i, kk, lane));
+      for (int i = 0; i < ST; ++i) z.mma_b(S[i], Tile<Tin, DK>::col_frag(now.k, 32 * i, kk, lane));
     }
+    if (c + 1 < n) store(tiles[(c + 1) & 1]);
+    __syncthreads();
   }
   store_state(S, dst + ((int64_t)head * a.nseg + seg) * DK * DV, DV, 1, c0, lane);
   if (tid == 0) a.seg_decay[(int64_t)head * a.nseg + seg] = decay;

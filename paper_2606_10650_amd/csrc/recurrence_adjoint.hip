@@ -16,9 +16,9 @@
 // with the state before all tokens and the gradient of the last one as further ends.  With
 // x_u the sum of A_us over s < u and y_s that over u > s, dg_t = <dstate, last state> + sum
 // over s >= t of (x_s - y_s).  No pair (t, t) enters either, so nothing large cancels where
-// the gates are steep.  This kernel adds up the pairs inside a chunk and those from a
-// chunk's token to what is behind the chunk; the pairs with what is before it come from
-// the dq pass.
+// the gates are steep.  The dq pass leaves x (a lane holds a token u and its pairs' scores
+// of do and v; each wave adds the products with its own 32 columns of q and k), this
+// kernel y, the other way round.
 #include "recurrence_tile.h"
 
 namespace dla {
@@ -29,33 +29,24 @@ struct AdjArgs {
   Rows q, k, v, dout, dk, dv;
   const float* dstate;
   float* ds0;
-  float* kdot;   // [heads][T]: y_s - (the in-chunk part of x_s)
+  float* kdot;   // [heads][T]: y_s
   int dk_f32;
 };
 
-// sum over the 32 lanes of each half
-__device__ __forceinline__ float half_sum(float x) {
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) x += __shfl_xor(x, o);
-  return x;
-}
-
-// What the waves of a workgroup pass each other for the gate's gradient.
-template <int KW>
-struct PairSums {
-  float qk[16][64];            // q_u . k_s, element and lane of a score tile
-  float col[KW][kChunk];       // per wave of dk: y_s, and the carried k_s . dk_s
-  float row[KW][kChunk];       // per wave: its rows' x_u, else zero
+template <typename Tin, int DK, int DV>
+struct AdjTiles {
+  Tin q[kChunk * DK], k[kChunk * DK], v[kChunk * DV], o[kChunk * DV];
+  Decays dec;
+  float dots[DK / 32][kChunk];
 };
 
 // Waves 0 .. DV / 32 - 1 hold 32 columns each of R [DK][DV] and give dv; the others hold
 // those of its transpose and give dk.
 template <typename Tin, int DK, int DV>
 __global__ __launch_bounds__(2 * (DK + DV), 1) void adjoint_kernel(AdjArgs f) {
-  constexpr int NT = 2 * (DK + DV), KW = DK / 32, VW = DV / 32, PER = 16 / KW;
-  __shared__ __align__(16) Tin sq[kChunk * DK], sk[kChunk * DK], sv[kChunk * DV], so[kChunk * DV];
-  __shared__ __align__(16) Decays dec;
-  __shared__ PairSums<KW> pairs;
+  constexpr int NT = 2 * (DK + DV), KW = DK / 32, VW = DV / 32;
+  using Tiles = AdjTiles<Tin, DK, DV>;
+  __shared__ __align__(16) Tiles tiles[2];
   const RecArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5;
   const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
@@ -81,40 +72,34 @@ __global__ __launch_bounds__(2 * (DK + DV), 1) void adjoint_kernel(AdjArgs f) {
     go.load(dout, f.dout.st, t0, lim, tid);
     if (tid < kChunk) gd = decays[t0 + tid];
   };
-  auto stage = [&](int t0) {
-    __syncthreads();   // the last chunk's tiles are read
-    gq.store(sq, tid);
-    gk.store(sk, tid);
-    gv.store(sv, tid);
-    go.store(so, tid);
-    if (tid < kChunk) dec.store(gd, tid);
-    __syncthreads();
-    if (t0 > begin) request(t0 - kChunk);
+  auto store = [&](Tiles& to) {
+    gq.store(to.q, tid);
+    gk.store(to.k, tid);
+    gv.store(to.v, tid);
+    go.store(to.o, tid);
+    if (tid < kChunk) to.dec.store(gd, tid);
   };
   const float* last = a.nseg > 1 ? a.seg_adj + ((int64_t)head * a.nseg + seg) * D
                                  : (f.dstate ? f.dstate + head * D : nullptr);
   const int t_last = begin + (end - begin - 1) / kChunk * kChunk;
   request(t_last);
+  int at = 0;
   if (of_v) {
     f32x16 R[DK / 32];
 #pragma unroll
     for (int i = 0; i < DK / 32; ++i) R[i] = zero16();
     if (last) load_state(R, last, DV, 1, c0, lane);
-    for (int t0 = t_last; t0 >= begin; t0 -= kChunk) {
-      stage(t0);
+    store(tiles[0]);
+    __syncthreads();
+    for (int t0 = t_last; t0 >= begin; t0 -= kChunk, at ^= 1) {
+      const Tiles& now = tiles[at];
+      if (t0 > begin) request(t0 - kChunk);
       const int s = t0 + (lane & 31);
-      const float w = dec.out[lane & 31];
-      f32x16 p, c, o;
-      chunk_step<Tin, DK, DV, true, false>(sk, sq, so, dec, a.scale, c0, lane, R, p, c, o);
-      // the first wave's scores, for the waves of dk
-      if (wave == 0) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) pairs.qk[r][lane] = p[r];
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[r] = s < lim ? o[r] * a.scale + c[r] * w : 0.f;
+      f32x16 o;
+      chunk_step<Tin, DK, DV, true, false>(now.k, now.q, now.o, nullptr, now.dec, a.scale, c0, lane, R, o);
+      if (s >= lim) o = zero16();
       if (s < end) store_out(row_base<Tin>(f.dv, b, h) + s * f.dv.st, c0, o, lane);
-      __syncthreads();
+      if (t0 > begin) store(tiles[at ^ 1]);
       __syncthreads();
     }
     if (seg == 0 && f.ds0) store_state(R, f.ds0 + head * D, DV, 1, c0, lane);
@@ -123,53 +108,34 @@ __global__ __launch_bounds__(2 * (DK + DV), 1) void adjoint_kernel(AdjArgs f) {
 #pragma unroll
     for (int i = 0; i < DV / 32; ++i) R[i] = zero16();
     if (last) load_state(R, last, 1, DV, c0, lane);
-    for (int t0 = t_last; t0 >= begin; t0 -= kChunk) {
-      stage(t0);
-      const int sl = lane & 31, s = t0 + sl;
-      const float w = dec.out[sl], hi = dec.hi[sl], lo = dec.lo[sl];
-      f32x16 p, c, o;
-      chunk_step<Tin, DV, DK, true, true>(sv, so, sq, dec, a.scale, c0, lane, R, p, c, o);
-      float dot = 0.f;
+    // the waves' parts of a chunk's dots, added up by the chunk's successor
+    auto sum_dots = [&](const Tiles& from, int t0) {
+      if (kw == 0 && lane < kChunk && t0 + lane < end) {
+        float x = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float y[4];
-        load4f(sk + Tile<Tin, DK>::at(sl, c0 + held_row(4 * e, lane)), y);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          c[4 * e + j] *= w;
-          dot += c[4 * e + j] * y[j];
-        }
+        for (int i = 0; i < KW; ++i) x += from.dots[i][lane];
+        f.kdot[(int64_t)head * a.T + t0 + lane] = t0 + lane < lim ? x : 0.f;
       }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[r] = s < lim ? o[r] * a.scale + c[r] : 0.f;
+    };
+    store(tiles[0]);
+    __syncthreads();
+    for (int t0 = t_last; t0 >= begin; t0 -= kChunk, at ^= 1) {
+      Tiles& now = tiles[at];
+      if (t0 < t_last) sum_dots(tiles[at ^ 1], t0 + kChunk);
+      if (t0 > begin) request(t0 - kChunk);
+      const int s = t0 + (lane & 31);
+      f32x16 o;
+      const float dot = chunk_step<Tin, DV, DK, true, true>(now.v, now.o, now.q, now.k, now.dec, a.scale, c0, lane, R, o);
+      if (g == 0) now.dots[kw][lane] = dot;
+      if (s >= lim) o = zero16();
       if (s < end) {
         if (f.dk_f32) store_out(row_base<float>(f.dk, b, h) + s * f.dk.st, c0, o, lane);
         else store_out(row_base<Tin>(f.dk, b, h) + s * f.dk.st, c0, o, lane);
       }
-      __syncthreads();   // the scores of q and k are there
-      // The waves share out the pairs' sums, PER elements of the tile each: element r of a
-      // lane is the pair of its token s and token u = held_row(r).
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (r / PER != kw) continue;
-        const int u = held_row(r, lane);
-        const float d = decay2(dec.hi[u], dec.lo[u], hi, lo) * a.scale;
-        const float pair = u > sl ? pairs.qk[r][lane] * p[r] * d : 0.f;
-        dot += pair;
-        const float row = half_sum(pair);
-        if (sl == 0) pairs.row[kw][u] = row;
-      }
-      dot += __shfl_xor(dot, 32);
-      if (g == 0) pairs.col[kw][sl] = dot;
+      if (t0 > begin) store(tiles[at ^ 1]);
       __syncthreads();
-      if (kw == 0 && lane < kChunk && s < end) {
-        float x = 0.f;
-#pragma unroll
-        for (int i = 0; i < KW; ++i) x += pairs.col[i][lane];
-        x -= pairs.row[((lane & 7) + 8 * (lane >> 4)) / PER][lane];   // the wave that has element r of row u
-        f.kdot[(int64_t)head * a.T + s] = s < lim ? x : 0.f;
-      }
     }
+    sum_dots(tiles[at ^ 1], begin);
   }
 }
 

@@ -201,55 +201,83 @@ __device__ __forceinline__ void store_state(const f32x16 (&s)[N], float* p, int6
 }
 
 // One chunk, for a wave's 32 columns of a state of R rows.  Lane l % 32 is token t; the
-// elements of o and c are columns c0 + held_row(r).
+// elements of c and o are columns c0 + held_row(r).
 //   p[r] = q_t . k_s with s = held_row(r)
-//   c = S^T q_t
-//   o = sum over s of p masked and decayed, times v_s
-// and the state takes up the chunk.  REV: time runs back, so s >= t; LOW: c also takes
-// what the state's rounding to bfloat16 leaves.
-template <typename Tin, int R, int C, bool REV, bool LOW>
-__device__ __forceinline__ void chunk_step(const Tin* sq, const Tin* sk, const Tin* sv, const Decays& dec,
-                                           float update_scale, int c0, int lane, f32x16 (&S)[R / 32], f32x16& p,
-                                           f32x16& c, f32x16& o) {
+//   c = carry_t S^T q_t
+//   o = c + scale sum over s of p masked and decayed, times v_s
+// and the state takes up the chunk.  REV: time runs back, so s >= t.  PAIR: c also
+// takes what the state's rounding to bfloat16 leaves, and the lane's part of
+//   dot_t = y_t . c + scale sum over s != t of p masked and decayed, times (y_t . v_s)
+// is returned, with the rows y_t (32 columns of them a wave) in sy: what the pairs (s, t)
+// give to the gates between them.
+template <typename Tin, int R, int C, bool REV, bool PAIR>
+__device__ __forceinline__ float chunk_step(const Tin* sq, const Tin* sk, const Tin* sv, const Tin* sy,
+                                            const Decays& dec, float scale, int c0, int lane,
+                                            f32x16 (&S)[R / 32], f32x16& o) {
   using F = typename Frag<Tin>::T;
   using TR = Tile<Tin, R>;
   using TC = Tile<Tin, C>;
   const int t = lane & 31, g = lane >> 5, kr = perm_row(t);
-  p = zero16();
-  c = zero16();
+  const float hi = dec.hi[t], lo = dec.lo[t], total = dec.total();
+  f32x16 p = zero16();
   o = zero16();
 #pragma unroll
   for (int kk = 0; kk < R / 16; ++kk) {
     const F q = TR::row_frag(sq, t, kk, lane);
     Frag<Tin>::mma(p, TR::row_frag(sk, kr, kk, lane), q);
     const F s = state_frag<Tin>(S[kk >> 1], kk & 1);
-    if constexpr (LOW && sizeof(Tin) == 2) Frag<Tin>::mma(c, state_frag_low(S[kk >> 1], kk & 1, s), q);
-    Frag<Tin>::mma(c, s, q);
+    if constexpr (PAIR && sizeof(Tin) == 2) Frag<Tin>::mma(o, state_frag_low(S[kk >> 1], kk & 1, s), q);
+    Frag<Tin>::mma(o, s, q);
   }
-  const float hi = dec.hi[t], lo = dec.lo[t], total = dec.total();
+  // the scores, masked and decayed
+  float w[2][8];
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    float hs[8], ls[8];
+    weights8(dec.hi, kk, lane, hs);
+    weights8(dec.lo, kk, lane, ls);
+    weights8(REV ? dec.in : dec.out, kk, lane, w[kk]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int s = 16 * kk + 8 * g + e;
+      const float d = REV ? decay2(hs[e], ls[e], hi, lo) : decay2(hi, lo, hs[e], ls[e]);
+      p[8 * kk + e] = (REV ? s >= t : s <= t) ? p[8 * kk + e] * d * scale : 0.f;
+      if constexpr (REV) w[kk][e] *= scale;
+    }
+  }
+  const float carry = REV ? dec.out[t] : dec.in[t] * scale;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) o[r] *= carry;
+  float dot = 0.f;
+  if constexpr (PAIR) {
+    f32x16 z = zero16();
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      const F y = TC::row_frag(sy, t, c0 / 16 + kk, lane);
+      Frag<Tin>::mma(z, TC::row_frag(sv, kr, c0 / 16 + kk, lane), y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dot += o[8 * kk + e] * (float)y[e];
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dot += held_row(r, lane) != t ? p[r] * z[r] : 0.f;
+    dot += __shfl_xor(dot, 32);
+  }
 #pragma unroll
   for (int i = 0; i < R / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[i][r] *= total;
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) {
-    float hs[8], ls[8], w[8], x[8];
-    weights8(dec.hi, kk, lane, hs);
-    weights8(dec.lo, kk, lane, ls);
-    weights8(REV ? dec.in : dec.out, kk, lane, w);
+    float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int s = 16 * kk + 8 * g + e;
-      const float d = REV ? decay2(hs[e], ls[e], hi, lo) : decay2(hi, lo, hs[e], ls[e]);
-      x[e] = (REV ? s >= t : s <= t) ? p[8 * kk + e] * d : 0.f;
-      if constexpr (REV) w[e] *= update_scale;
-    }
+    for (int e = 0; e < 8; ++e) x[e] = p[8 * kk + e];
     const F v = TC::col_frag(sv, c0, kk, lane);
     Frag<Tin>::mma(o, v, Frag<Tin>::from_floats(x));
-    const Scaled<Tin> y(v, w);
+    const Scaled<Tin> y(v, w[kk]);
 #pragma unroll
     for (int i = 0; i < R / 32; ++i) y.mma_b(S[i], TR::col_frag(sk, 32 * i, kk, lane));
   }
+  return dot;
 }
 
 // Eight consecutive values of an output row, rounded once to the output's type.
