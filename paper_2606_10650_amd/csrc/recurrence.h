@@ -1,5 +1,5 @@
 // Launches of the single-state recurrence and its backward pass (recurrence.hip,
-// recurrence_adjoint.hip, recurrence_step.hip).
+// recurrence_grad.hip, recurrence_step.hip).
 #pragma once
 #include "dla_common.h"
 #include "dla_train.h"
@@ -41,7 +41,7 @@ struct RecArgs {
   float* seg_state;    // [heads][nseg][dk][dv], the state before each segment
   float* seg_adj;      // [heads][nseg][dk][dv], the adjoint behind each segment
   float* seg_decay;    // [heads][nseg]
-  float4* decays;      // [heads][chunks * kRecChunk], see recurrence_tile.h
+  float2* decays;      // [heads][2][chunks * kRecChunk], see recurrence_tile.h
 };
 
 constexpr int kRecChunk = 32;   // tokens a workgroup takes at a time

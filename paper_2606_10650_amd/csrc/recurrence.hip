@@ -10,22 +10,24 @@
 //
 // dq_t = sum_{s <= t} e^{a_t - a_s} (do_t . v_s) k_s + e^{a_t} S do_t is the same with do,
 // v and k in the places of q, k and v and the state transposed.  That pass also leaves
-// qdot_t, what the pairs (s < t, t) give to the gates between them (recurrence_adjoint.hip).
+// qdot_t, what the pairs (s < t, t) give to the gates between them (recurrence_grad.hip).
 #include "recurrence_tile.h"
 
 namespace dla {
 namespace {
 
-struct FwdArgs {
+// One pass over the tokens, in the kernel's roles: q, k of R values and v of C, a state
+// [R][C], out of C.
+struct ScanArgs {
   RecArgs a;
-  Rows q, k, v, out;       // in the kernel's roles
-  const float* s0;         // state before the first token, or null
-  int64_t s_rs, s_cs;      // strides of a state's rows and columns, in the kernel's roles
-  const float* seg_state;  // state before each segment, or null: one segment
-  float* s_out;            // state behind the last token, or null
-  const float* dstate;     // dq only, or null
-  Rows x;                  // dq only: q
-  float* qdot;
+  Rows q, k, v, out;
+  Rows y;                  // PAIR: rows of C whose products with the pass's output go to dot
+  const float* first;      // the state before the pass's first token, per head, or null
+  int64_t s_rs, s_cs;      // strides of a state's rows and columns
+  const float* seg_first;  // the state before each segment, or null: one segment
+  float* last;             // the state behind the pass's last token, or null
+  float* dot;              // PAIR: [heads][T]
+  const float* end_with;   // PAIR: per head, or null; end_dot = <end_with, last state>
   float* end_dot;
   int out_f32;
 };
@@ -54,25 +56,27 @@ __global__ __launch_bounds__(256) void decays_kernel(RecArgs a) {
   const double w = rint(x);
   const float hi = (float)w - 131072.f * (float)n, lo = (float)(x - w);
   const float eh = __shfl(hi, kChunk - 1, kChunk), el = __shfl(lo, kChunk - 1, kChunk);
-  if (c < chunks)
-    a.decays[head * padded + t] = make_float4(hi, lo, decay2(hi, lo, 0.f, 0.f), decay2(eh, el, hi, lo));
+  if (c < chunks) {
+    float2* d = a.decays + 2 * head * padded;
+    d[t] = make_float2(hi, lo);
+    d[padded + t] = make_float2(decay2(hi, lo, 0.f, 0.f), decay2(eh, el, hi, lo));
+  }
 }
 
-// A chunk's tiles; two of them, so that the next chunk is stored while one is read and a
-// chunk takes one barrier.
-template <typename Tin, int DK, int DV, bool DQ>
-struct FwdTiles {
-  Tin q[kChunk * DK], k[kChunk * DK], v[kChunk * DV], x[DQ ? kChunk * DV : 8];
+template <typename Tin, int R, int C, bool PAIR>
+struct ScanTiles {
+  Tin q[Tile<Tin, R>::SIZE], k[Tile<Tin, R>::SIZE], v[Tile<Tin, C>::SIZE], y[PAIR ? Tile<Tin, C>::SIZE : 8];
   Decays dec;
-  float dots[DQ ? DV / 32 : 1][kChunk];
+  float dots[PAIR ? C / 32 : 1][kChunk];
 };
 
-template <typename Tin, int DK, int DV, bool DQ>
-__global__ __launch_bounds__(2 * DV, sizeof(Tin) == 2 ? 2 : 1) void forward_kernel(FwdArgs f) {
-  constexpr int NT = 2 * DV, NW = DV / 32, ST = DK / 32;
-  __shared__ __align__(16) FwdTiles<Tin, DK, DV, DQ> tiles[2];
+// REV: from the segment's last chunk to its first.
+template <typename Tin, int R, int C, bool REV, bool PAIR>
+__global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(ScanArgs f) {
+  constexpr int NT = 2 * C, NW = C / 32;
+  __shared__ __align__(16) ScanTiles<Tin, R, C, PAIR> now;
   const RecArgs& a = f.a;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
   const int b = head / a.H, h = head % a.H, c0 = 32 * wave;
   const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
@@ -80,88 +84,84 @@ __global__ __launch_bounds__(2 * DV, sizeof(Tin) == 2 ? 2 : 1) void forward_kern
   const Tin* q = row_base<const Tin>(f.q, b, h);
   const Tin* k = row_base<const Tin>(f.k, b, h);
   const Tin* v = row_base<const Tin>(f.v, b, h);
-  const Tin* x = DQ ? row_base<const Tin>(f.x, b, h) : nullptr;
-  const float4* decays = a.decays + head * rec_padded(a.T);
-  const int64_t D = (int64_t)DK * DV;
+  const Tin* y = PAIR ? row_base<const Tin>(f.y, b, h) : nullptr;
+  const int64_t D = (int64_t)R * C, padded = rec_padded(a.T);
+  const float2* decays = a.decays + 2 * head * padded;
 
-  Stage<Tin, DK, NT> gq, gk;
-  Stage<Tin, DV, NT> gv, gx;
-  float4 gd;
+  Stage<Tin, R, NT> gq, gk;
+  Stage<Tin, C, NT> gv, gy;
+  DecayStage<NT, REV> gd;
   auto request = [&](int t0) {
-    gq.load(q, f.q.st, t0, lim, tid);
-    gk.load(k, f.k.st, t0, lim, tid);
-    gv.load(v, f.v.st, t0, lim, tid);
-    if constexpr (DQ) gx.load(x, f.x.st, t0, lim, tid);
-    if (tid < kChunk) gd = decays[t0 + tid];
+    gq.load(q + t0 * f.q.st, f.q.st, lim - t0, tid);
+    gk.load(k + t0 * f.k.st, f.k.st, lim - t0, tid);
+    gv.load(v + t0 * f.v.st, f.v.st, lim - t0, tid);
+    if constexpr (PAIR) gy.load(y + t0 * f.y.st, f.y.st, lim - t0, tid);
+    gd.load(decays, padded, t0, tid);
   };
-  auto store = [&](FwdTiles<Tin, DK, DV, DQ>& to) {
-    gq.store(to.q, tid);
-    gk.store(to.k, tid);
-    gv.store(to.v, tid);
-    if constexpr (DQ) gx.store(to.x, tid);
-    if (tid < kChunk) to.dec.store(gd, tid);
-  };
-  request(begin);
-  f32x16 S[ST];
-  const float* first = f.seg_state ? f.seg_state + ((int64_t)head * a.nseg + seg) * D
-                                   : (f.s0 ? f.s0 + head * D : nullptr);
-  if (first) {
-    load_state(S, first, f.s_rs, f.s_cs, c0, lane);
-  } else {
-#pragma unroll
-    for (int i = 0; i < ST; ++i) S[i] = zero16();
-  }
-  store(tiles[0]);
-  __syncthreads();
-  int at = 0;
-  // the waves' parts of a chunk's dots, added up by the chunk's successor
-  auto sum_dots = [&](const FwdTiles<Tin, DK, DV, DQ>& from, int t0) {
+  // the waves' parts of a chunk's dots, added up when the next one's tokens are staged
+  auto sum_dots = [&](int t0) {
     if (tid < kChunk && t0 + tid < end) {
-      float y = 0.f;
+      float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) y += from.dots[w][tid];
-      f.qdot[(int64_t)head * a.T + t0 + tid] = t0 + tid < lim ? y : 0.f;
+      for (int w = 0; w < NW; ++w) x += now.dots[w][tid];
+      f.dot[(int64_t)head * a.T + t0 + tid] = t0 + tid < lim ? x : 0.f;
     }
   };
-  for (int t0 = begin; t0 < end; t0 += kChunk, at ^= 1) {
-    FwdTiles<Tin, DK, DV, DQ>& now = tiles[at];
-    if constexpr (DQ) {
-      if (t0 > begin) sum_dots(tiles[at ^ 1], t0 - kChunk);
+  const int n = (end - begin + kChunk - 1) / kChunk;
+  auto chunk_at = [&](int c) { return begin + (REV ? n - 1 - c : c) * kChunk; };
+  request(chunk_at(0));
+  State<R / 32> S;
+  const float* first = f.seg_first ? f.seg_first + ((int64_t)head * a.nseg + seg) * D
+                                   : (f.first ? f.first + head * D : nullptr);
+  if (first) load_state(S.s, first, f.s_rs, f.s_cs, c0, lane);
+  else S.clear();
+  for (int c = 0; c < n; ++c) {
+    const int t0 = chunk_at(c);
+    __syncthreads();   // the last chunk's tiles are read, its dots written
+    if constexpr (PAIR) {
+      if (c > 0) sum_dots(chunk_at(c - 1));
     }
-    if (t0 + kChunk < end) request(t0 + kChunk);
-    const int t = t0 + (lane & 31);
-    f32x16 o;
-    const float dot = chunk_step<Tin, DK, DV, false, DQ>(now.q, now.k, now.v, now.x, now.dec, a.scale, c0, lane, S, o);
-    if constexpr (DQ) {
-      if (g == 0) now.dots[wave][lane] = dot;
-    }
-    if (t >= lim) o = zero16();
-    if (t < end) {
-      if (DQ && f.out_f32) store_out(row_base<float>(f.out, b, h) + t * f.out.st, c0, o, lane);
-      else store_out(row_base<Tin>(f.out, b, h) + t * f.out.st, c0, o, lane);
-    }
-    if (t0 + kChunk < end) store(tiles[at ^ 1]);
+    gq.store(now.q, tid);
+    gk.store(now.k, tid);
+    gv.store(now.v, tid);
+    if constexpr (PAIR) gy.store(now.y, tid);
+    gd.store(now.dec, a.scale, tid);
     __syncthreads();
+    if (c + 1 < n) request(chunk_at(c + 1));
+    f32x16 o;
+    const float dot = chunk_step<Tin, R, C, REV, PAIR>(now.q, now.k, now.v, now.y, now.dec, a.scale, c0, lane, S, o);
+    if constexpr (PAIR) {
+      if (lane < 32) now.dots[wave][lane] = dot;
+    }
+    if (PAIR && f.out_f32)
+      store_out(row_base<float>(f.out, b, h) + t0 * f.out.st, f.out.st, c0, o, lim - t0, end - t0, lane);
+    else
+      store_out(row_base<Tin>(f.out, b, h) + t0 * f.out.st, f.out.st, c0, o, lim - t0, end - t0, lane);
   }
-  if constexpr (DQ) sum_dots(tiles[at ^ 1], begin + (end - begin - 1) / kChunk * kChunk);
-  if (seg == a.nseg - 1) {
-    if (f.s_out) store_state(S, f.s_out + head * D, f.s_rs, f.s_cs, c0, lane);
-    if constexpr (DQ) {
-      if (f.dstate) {
-        float y = 0.f;
+  if constexpr (PAIR) {
+    __syncthreads();
+    sum_dots(chunk_at(n - 1));
+  }
+  if (seg == (REV ? 0 : a.nseg - 1)) {
+    S.apply();
+    if (f.last) store_state(S.s, f.last + head * D, f.s_rs, f.s_cs, c0, lane);
+    if constexpr (PAIR) {
+      if (f.end_with) {
+        float x = 0.f;
 #pragma unroll
-        for (int i = 0; i < ST; ++i)
+        for (int i = 0; i < R / 32; ++i)
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            y += S[i][r] * f.dstate[head * D + (32 * i + held_row(r, lane)) * f.s_rs +
-                                    (c0 + perm_row(lane & 31)) * f.s_cs];
+            x += S.s[i][r] * f.end_with[head * D + (32 * i + held_row(r, lane)) * f.s_rs +
+                                        (c0 + perm_row(lane & 31)) * f.s_cs];
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) y += __shfl_xor(y, o);
-        if (lane == 0) tiles[at].dots[wave][0] = y;
+        for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+        __syncthreads();
+        if (lane == 0) now.dots[wave][0] = x;
         __syncthreads();
         if (tid == 0) {
           float z = 0.f;
-          for (int w = 0; w < NW; ++w) z += tiles[at].dots[w][0];
+          for (int w = 0; w < NW; ++w) z += now.dots[w][0];
           f.end_dot[head] = z;
         }
       }
@@ -174,12 +174,12 @@ __global__ __launch_bounds__(2 * DV, sizeof(Tin) == 2 ? 2 : 1) void forward_kern
 // the segment's start) q_s do_s^T.
 template <typename Tin, int DK, int DV>
 struct SegTiles {
-  Tin k[kChunk * DK], v[kChunk * DV];
-  Decays dec;
+  Tin k[Tile<Tin, DK>::SIZE], v[Tile<Tin, DV>::SIZE];
+  float in[kChunk], out[kChunk];
 };
 
 template <typename Tin, int DK, int DV, bool REV>
-__global__ __launch_bounds__(2 * DV, sizeof(Tin) == 2 ? 2 : 1) void segment_kernel(RecArgs a, Rows xr, Rows yr, float* dst) {
+__global__ __launch_bounds__(2 * DV, sizeof(Tin) == 4 ? 1 : (DV == 128 ? 3 : 2)) void segment_kernel(RecArgs a, Rows xr, Rows yr, float* dst) {
   constexpr int NT = 2 * DV, ST = DK / 32;
   __shared__ __align__(16) SegTiles<Tin, DK, DV> tiles[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -189,23 +189,26 @@ __global__ __launch_bounds__(2 * DV, sizeof(Tin) == 2 ? 2 : 1) void segment_kern
   const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
   const Tin* x = row_base<const Tin>(xr, b, h);
   const Tin* y = row_base<const Tin>(yr, b, h);
-  const float4* decays = a.decays + head * rec_padded(a.T);
-  f32x16 S[ST];
-#pragma unroll
-  for (int i = 0; i < ST; ++i) S[i] = zero16();
+  const int64_t padded = rec_padded(a.T);
+  const float2* decays = a.decays + 2 * head * padded + padded;
+  State<ST> S;
+  S.clear();
   float decay = 1.f;
   Stage<Tin, DK, NT> gx;
   Stage<Tin, DV, NT> gy;
-  float4 gd;
+  float2 gd;
   auto request = [&](int t0) {
-    gx.load(x, xr.st, t0, lim, tid);
-    gy.load(y, yr.st, t0, lim, tid);
+    gx.load(x + t0 * xr.st, xr.st, lim - t0, tid);
+    gy.load(y + t0 * yr.st, yr.st, lim - t0, tid);
     if (tid < kChunk) gd = decays[t0 + tid];
   };
   auto store = [&](SegTiles<Tin, DK, DV>& to) {
     gx.store(to.k, tid);
     gy.store(to.v, tid);
-    if (tid < kChunk) to.dec.store(gd, tid);
+    if (tid < kChunk) {
+      to.in[tid] = gd.x;
+      to.out[tid] = gd.y;
+    }
   };
   const int n = (end - begin + kChunk - 1) / kChunk;
   auto chunk_at = [&](int c) { return begin + (REV ? n - 1 - c : c) * kChunk; };
@@ -215,28 +218,25 @@ __global__ __launch_bounds__(2 * DV, sizeof(Tin) == 2 ? 2 : 1) void segment_kern
   for (int c = 0; c < n; ++c) {
     const SegTiles<Tin, DK, DV>& now = tiles[c & 1];
     if (c + 1 < n) request(chunk_at(c + 1));
-    const float total = now.dec.total();
+    const float total = now.in[kChunk - 1];
     decay *= total;
-#pragma unroll
-    for (int i = 0; i < ST; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) S[i][r] *= total;
+    if (S.decay(total)) S.apply();
+    const float inv = (REV ? a.scale : 1.f) * __builtin_amdgcn_rcpf(S.f);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
       float w[8];
-      weights8(REV ? now.dec.in : now.dec.out, kk, lane, w);
-      if constexpr (REV) {
+      weights8(REV ? now.in : now.out, kk, lane, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] *= a.scale;
-      }
+      for (int e = 0; e < 8; ++e) w[e] *= inv;
       const Scaled<Tin> z(Tile<Tin, DV>::col_frag(now.v, c0, kk, lane), w);
 #pragma unroll
-      for (int i = 0; i < ST; ++i) z.mma_b(S[i], Tile<Tin, DK>::col_frag(now.k, 32 * i, kk, lane));
+      for (int i = 0; i < ST; ++i) z.mma_b(S.s[i], Tile<Tin, DK>::col_frag(now.k, 32 * i, kk, lane));
     }
     if (c + 1 < n) store(tiles[(c + 1) & 1]);
     __syncthreads();
   }
-  store_state(S, dst + ((int64_t)head * a.nseg + seg) * DK * DV, DV, 1, c0, lane);
+  S.apply();
+  store_state(S.s, dst + ((int64_t)head * a.nseg + seg) * DK * DV, DV, 1, c0, lane);
   if (tid == 0) a.seg_decay[(int64_t)head * a.nseg + seg] = decay;
 }
 
@@ -258,21 +258,21 @@ __global__ __launch_bounds__(256) void prefix_kernel(RecArgs a, float* part, con
   }
 }
 
-template <typename Tin, int DK, int DV, bool DQ>
-hipError_t run_forward(const FwdArgs& f, hipStream_t st) {
-  const int grid = f.a.B * f.a.H * f.a.nseg;
-  hipLaunchKernelGGL((forward_kernel<Tin, DK, DV, DQ>), dim3(grid), dim3(2 * DV), 0, st, f);
-  return hipGetLastError();
-}
-
-template <bool DQ>
-hipError_t pick_forward(const FwdArgs& f, int dtype, int dk, int dv, hipStream_t st) {
+template <bool REV, bool PAIR>
+hipError_t launch_scan(const ScanArgs& f, int dtype, int R, int C, hipStream_t st) {
+  const dim3 grid(f.a.B * f.a.H * f.a.nseg), block(2 * C);
   if (dtype == DLA_BF16) {
-    if (dk == 128) return dv == 128 ? run_forward<bf16_t, 128, 128, DQ>(f, st) : run_forward<bf16_t, 128, 64, DQ>(f, st);
-    return dv == 128 ? run_forward<bf16_t, 64, 128, DQ>(f, st) : run_forward<bf16_t, 64, 64, DQ>(f, st);
+    if (R == 128 && C == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 128, 128, REV, PAIR>), grid, block, 0, st, f);
+    else if (R == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 128, 64, REV, PAIR>), grid, block, 0, st, f);
+    else if (C == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 64, 128, REV, PAIR>), grid, block, 0, st, f);
+    else hipLaunchKernelGGL((scan_kernel<bf16_t, 64, 64, REV, PAIR>), grid, block, 0, st, f);
+  } else {
+    if (R == 128 && C == 128) hipLaunchKernelGGL((scan_kernel<float, 128, 128, REV, PAIR>), grid, block, 0, st, f);
+    else if (R == 128) hipLaunchKernelGGL((scan_kernel<float, 128, 64, REV, PAIR>), grid, block, 0, st, f);
+    else if (C == 128) hipLaunchKernelGGL((scan_kernel<float, 64, 128, REV, PAIR>), grid, block, 0, st, f);
+    else hipLaunchKernelGGL((scan_kernel<float, 64, 64, REV, PAIR>), grid, block, 0, st, f);
   }
-  if (dk == 128) return dv == 128 ? run_forward<float, 128, 128, DQ>(f, st) : run_forward<float, 128, 64, DQ>(f, st);
-  return dv == 128 ? run_forward<float, 64, 128, DQ>(f, st) : run_forward<float, 64, 64, DQ>(f, st);
+  return hipGetLastError();
 }
 
 template <typename Tin, int DK, int DV>
@@ -311,44 +311,70 @@ hipError_t launch_recurrence_segments(const RecArgs& a, int dtype, bool reverse,
 hipError_t launch_recurrence_forward(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
                                      const Rows& v, const Rows& out, const float* s0, float* s_out,
                                      hipStream_t st) {
-  FwdArgs f;
+  ScanArgs f{};
   f.a = a;
   f.q = q;
   f.k = k;
   f.v = v;
   f.out = out;
-  f.s0 = s0;
+  f.first = s0;
   f.s_rs = a.dv;
   f.s_cs = 1;
-  f.seg_state = a.nseg > 1 ? a.seg_state : nullptr;
-  f.s_out = s_out;
-  f.dstate = nullptr;
-  f.qdot = f.end_dot = nullptr;
-  f.out_f32 = 0;
-  return pick_forward<false>(f, dtype, a.dk, a.dv, st);
+  f.seg_first = a.nseg > 1 ? a.seg_state : nullptr;
+  f.last = s_out;
+  return launch_scan<false, false>(f, dtype, a.dk, a.dv, st);
 }
 
 hipError_t launch_recurrence_dq(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
                                 const Rows& v, const Rows& dout, const Rows& dq, bool dq_f32,
                                 const float* s0, const float* dstate, float* qdot, float* end_dot,
                                 hipStream_t st) {
-  FwdArgs f;
+  ScanArgs f{};
   f.a = a;
   f.q = dout;
   f.k = v;
   f.v = k;
   f.out = dq;
-  f.s0 = s0;
+  f.y = q;
+  f.first = s0;
   f.s_rs = 1;
   f.s_cs = a.dv;
-  f.seg_state = a.nseg > 1 ? a.seg_state : nullptr;
-  f.s_out = nullptr;
-  f.dstate = dstate;
-  f.x = q;
-  f.qdot = qdot;
+  f.seg_first = a.nseg > 1 ? a.seg_state : nullptr;
+  f.dot = qdot;
+  f.end_with = dstate;
   f.end_dot = end_dot;
   f.out_f32 = dq_f32 ? 1 : 0;
-  return pick_forward<true>(f, dtype, a.dv, a.dk, st);
+  return launch_scan<false, true>(f, dtype, a.dv, a.dk, st);
+}
+
+hipError_t launch_recurrence_adjoint(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
+                                     const Rows& v, const Rows& dout, const Rows& dk, bool dk_f32,
+                                     const Rows& dv, const float* dstate, float* ds0, float* kdot,
+                                     hipStream_t st) {
+  ScanArgs f{};
+  f.a = a;
+  f.q = k;
+  f.k = q;
+  f.v = dout;
+  f.out = dv;
+  f.first = dstate;
+  f.s_rs = a.dv;
+  f.s_cs = 1;
+  f.seg_first = a.nseg > 1 ? a.seg_adj : nullptr;
+  f.last = ds0;
+  const hipError_t e = launch_scan<true, false>(f, dtype, a.dk, a.dv, st);
+  if (e != hipSuccess) return e;
+  f.q = v;
+  f.k = dout;
+  f.v = q;
+  f.out = dk;
+  f.y = k;
+  f.s_rs = 1;
+  f.s_cs = a.dv;
+  f.last = nullptr;
+  f.dot = kdot;
+  f.out_f32 = dk_f32 ? 1 : 0;
+  return launch_scan<true, true>(f, dtype, a.dv, a.dk, st);
 }
 
 }  // namespace dla

@@ -24,121 +24,6 @@
 namespace dla {
 namespace {
 
-struct AdjArgs {
-  RecArgs a;
-  Rows q, k, v, dout, dk, dv;
-  const float* dstate;
-  float* ds0;
-  float* kdot;   // [heads][T]: y_s
-  int dk_f32;
-};
-
-template <typename Tin, int DK, int DV>
-struct AdjTiles {
-  Tin q[kChunk * DK], k[kChunk * DK], v[kChunk * DV], o[kChunk * DV];
-  Decays dec;
-  float dots[DK / 32][kChunk];
-};
-
-// Waves 0 .. DV / 32 - 1 hold 32 columns each of R [DK][DV] and give dv; the others hold
-// those of its transpose and give dk.
-template <typename Tin, int DK, int DV>
-__global__ __launch_bounds__(2 * (DK + DV), 1) void adjoint_kernel(AdjArgs f) {
-  constexpr int NT = 2 * (DK + DV), KW = DK / 32, VW = DV / 32;
-  using Tiles = AdjTiles<Tin, DK, DV>;
-  __shared__ __align__(16) Tiles tiles[2];
-  const RecArgs& a = f.a;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5;
-  const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
-  const int b = head / a.H, h = head % a.H;
-  const bool of_v = wave < VW;
-  const int kw = wave - VW, c0 = 32 * (of_v ? wave : kw);
-  const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-  const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
-  const Tin* q = row_base<const Tin>(f.q, b, h);
-  const Tin* k = row_base<const Tin>(f.k, b, h);
-  const Tin* v = row_base<const Tin>(f.v, b, h);
-  const Tin* dout = row_base<const Tin>(f.dout, b, h);
-  const float4* decays = a.decays + head * rec_padded(a.T);
-  const int64_t D = (int64_t)DK * DV;
-
-  Stage<Tin, DK, NT> gq, gk;
-  Stage<Tin, DV, NT> gv, go;
-  float4 gd;
-  auto request = [&](int t0) {
-    gq.load(q, f.q.st, t0, lim, tid);
-    gk.load(k, f.k.st, t0, lim, tid);
-    gv.load(v, f.v.st, t0, lim, tid);
-    go.load(dout, f.dout.st, t0, lim, tid);
-    if (tid < kChunk) gd = decays[t0 + tid];
-  };
-  auto store = [&](Tiles& to) {
-    gq.store(to.q, tid);
-    gk.store(to.k, tid);
-    gv.store(to.v, tid);
-    go.store(to.o, tid);
-    if (tid < kChunk) to.dec.store(gd, tid);
-  };
-  const float* last = a.nseg > 1 ? a.seg_adj + ((int64_t)head * a.nseg + seg) * D
-                                 : (f.dstate ? f.dstate + head * D : nullptr);
-  const int t_last = begin + (end - begin - 1) / kChunk * kChunk;
-  request(t_last);
-  int at = 0;
-  if (of_v) {
-    f32x16 R[DK / 32];
-#pragma unroll
-    for (int i = 0; i < DK / 32; ++i) R[i] = zero16();
-    if (last) load_state(R, last, DV, 1, c0, lane);
-    store(tiles[0]);
-    __syncthreads();
-    for (int t0 = t_last; t0 >= begin; t0 -= kChunk, at ^= 1) {
-      const Tiles& now = tiles[at];
-      if (t0 > begin) request(t0 - kChunk);
-      const int s = t0 + (lane & 31);
-      f32x16 o;
-      chunk_step<Tin, DK, DV, true, false>(now.k, now.q, now.o, nullptr, now.dec, a.scale, c0, lane, R, o);
-      if (s >= lim) o = zero16();
-      if (s < end) store_out(row_base<Tin>(f.dv, b, h) + s * f.dv.st, c0, o, lane);
-      if (t0 > begin) store(tiles[at ^ 1]);
-      __syncthreads();
-    }
-    if (seg == 0 && f.ds0) store_state(R, f.ds0 + head * D, DV, 1, c0, lane);
-  } else {
-    f32x16 R[DV / 32];
-#pragma unroll
-    for (int i = 0; i < DV / 32; ++i) R[i] = zero16();
-    if (last) load_state(R, last, 1, DV, c0, lane);
-    // the waves' parts of a chunk's dots, added up by the chunk's successor
-    auto sum_dots = [&](const Tiles& from, int t0) {
-      if (kw == 0 && lane < kChunk && t0 + lane < end) {
-        float x = 0.f;
-#pragma unroll
-        for (int i = 0; i < KW; ++i) x += from.dots[i][lane];
-        f.kdot[(int64_t)head * a.T + t0 + lane] = t0 + lane < lim ? x : 0.f;
-      }
-    };
-    store(tiles[0]);
-    __syncthreads();
-    for (int t0 = t_last; t0 >= begin; t0 -= kChunk, at ^= 1) {
-      Tiles& now = tiles[at];
-      if (t0 < t_last) sum_dots(tiles[at ^ 1], t0 + kChunk);
-      if (t0 > begin) request(t0 - kChunk);
-      const int s = t0 + (lane & 31);
-      f32x16 o;
-      const float dot = chunk_step<Tin, DV, DK, true, true>(now.v, now.o, now.q, now.k, now.dec, a.scale, c0, lane, R, o);
-      if (g == 0) now.dots[kw][lane] = dot;
-      if (s >= lim) o = zero16();
-      if (s < end) {
-        if (f.dk_f32) store_out(row_base<float>(f.dk, b, h) + s * f.dk.st, c0, o, lane);
-        else store_out(row_base<Tin>(f.dk, b, h) + s * f.dk.st, c0, o, lane);
-      }
-      if (t0 > begin) store(tiles[at ^ 1]);
-      __syncthreads();
-    }
-    sum_dots(tiles[at ^ 1], begin);
-  }
-}
-
 // dg from the tokens' sums, from the last token back, in float64: what is added up spans
 // the sequence, what is left may be small.  A cut gate lets nothing through: dg is zero
 // there and the sum starts anew, exactly.  Two passes over blocks of tokens: each block's
@@ -274,38 +159,7 @@ __global__ __launch_bounds__(256) void head_sum_kernel(RecArgs a, const float* p
   }
 }
 
-template <typename Tin, int DK, int DV>
-hipError_t run_adjoint(const AdjArgs& f, hipStream_t st) {
-  hipLaunchKernelGGL((adjoint_kernel<Tin, DK, DV>), dim3(f.a.B * f.a.H * f.a.nseg),
-                     dim3(2 * (DK + DV)), 0, st, f);
-  return hipGetLastError();
-}
-
 }  // namespace
-
-hipError_t launch_recurrence_adjoint(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
-                                     const Rows& v, const Rows& dout, const Rows& dk, bool dk_f32,
-                                     const Rows& dv, const float* dstate, float* ds0, float* kdot,
-                                     hipStream_t st) {
-  AdjArgs f;
-  f.a = a;
-  f.q = q;
-  f.k = k;
-  f.v = v;
-  f.dout = dout;
-  f.dk = dk;
-  f.dv = dv;
-  f.dstate = dstate;
-  f.ds0 = ds0;
-  f.kdot = kdot;
-  f.dk_f32 = dk_f32 ? 1 : 0;
-  if (dtype == DLA_BF16) {
-    if (a.dk == 128) return a.dv == 128 ? run_adjoint<bf16_t, 128, 128>(f, st) : run_adjoint<bf16_t, 128, 64>(f, st);
-    return a.dv == 128 ? run_adjoint<bf16_t, 64, 128>(f, st) : run_adjoint<bf16_t, 64, 64>(f, st);
-  }
-  if (a.dk == 128) return a.dv == 128 ? run_adjoint<float, 128, 128>(f, st) : run_adjoint<float, 128, 64>(f, st);
-  return a.dv == 128 ? run_adjoint<float, 64, 128>(f, st) : run_adjoint<float, 64, 64>(f, st);
-}
 
 hipError_t launch_recurrence_dgate(const RecArgs& a, int dtype, const float* qdot, const float* kdot,
                                    const float* end_dot, double* block_sum, int* block_cut,

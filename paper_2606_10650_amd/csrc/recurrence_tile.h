@@ -21,30 +21,29 @@ namespace dla {
 
 constexpr int kChunk = 32;
 
-// 32 rows of D values in LDS, in 16-byte pieces whose place in a row depends on the row,
-// so that reads of one column by 16 rows, and of 64 (32: float32) bytes by the rows that
-// one transposing read takes, spread over the banks.
+// 32 rows of D values in LDS, read a row per lane (16 bytes a lane) and a column per lane
+// (bfloat16: 4 rows of 64 bytes per 16 lanes, transposed by the read; float32: 128 bytes of
+// two rows, 8 apart).  bfloat16 rows are padded by 64 bytes, which spreads four rows over
+// the banks, and pieces of 16 bytes change places within 64 bytes by bits 2 and 3 of the row,
+// which spreads sixteen; float32 rows are padded by 16 bytes.  Both kinds of read are then
+// free of conflicts, and but for those two bits every offset is a constant of the instruction.
 template <typename Tin, int D>
 struct Tile {
-  static constexpr int PE = 16 / (int)sizeof(Tin);   // elements per piece
-  static constexpr int NP = D / PE;                  // pieces per row
-  __device__ static __forceinline__ int swz(int row) {
-    if constexpr (sizeof(Tin) == 4) return row & 15;
-    if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
-    return ((row << 1) & 4) | ((row >> 2) & 3);
-  }
+  static constexpr int PE = 16 / (int)sizeof(Tin);             // elements per piece
+  static constexpr int NP = D / PE;                            // pieces per row
+  static constexpr int LD = D + (sizeof(Tin) == 2 ? 32 : 4);   // elements from row to row
+  static constexpr int SIZE = kChunk * LD;
+  __device__ static __forceinline__ int swz(int row) { return sizeof(Tin) == 2 ? (row >> 2) & 3 : 0; }
   __device__ static __forceinline__ int at(int row, int col) {
-    return row * D + (((col / PE) ^ swz(row)) * PE) + col % PE;
+    return row * LD + ((col / PE) ^ swz(row)) * PE + col % PE;
   }
   // operand with a token per lane: row `row`, columns 16 kk + 8 (lane / 32) + e
   __device__ static __forceinline__ typename Frag<Tin>::T row_frag(const Tin* p, int row, int kk,
                                                                    int lane) {
-    const int c = 16 * kk + 8 * (lane >> 5);
-    if constexpr (sizeof(Tin) == 2) return Frag<Tin>::load(p + at(row, c));
-    else return load_4x2<float>(p + at(row, c), p + at(row, c + 4));
+    return Frag<Tin>::load(p + at(row, 16 * (kk & 1) + 8 * (lane >> 5)) + 32 * (kk >> 1));
   }
-  // operand with a column per lane, c0 + perm_row(lane % 32), and tokens 16 kk + 8 (lane /
-  // 32) + e
+  // operand with a column per lane, c0 + perm_row(lane % 32) (c0 a multiple of 32), and
+  // tokens 16 kk + 8 (lane / 32) + e
   __device__ static __forceinline__ typename Frag<Tin>::T col_frag(const Tin* p, int c0, int kk,
                                                                    int lane);
 };
@@ -65,41 +64,50 @@ __device__ __forceinline__ typename Frag<Tin>::T Tile<Tin, D>::col_frag(const Ti
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4 lds4;
     const int i = lane & 15, c4 = i & 3;
-    const int col = c0 + (lane & 16) + 8 * (c4 & 1) + 4 * (c4 >> 1);
-    const int row = 16 * kk + 8 * g + (i >> 2);
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + at(row, col)));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + at(row + 4, col)));
+    const int row = 8 * g + (i >> 2), col = (lane & 16) + 8 * (c4 & 1) + 4 * (c4 >> 1);
+    const Tin* x = p + 16 * kk * LD + c0;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(x + at(row, col)));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(x + at(row + 4, col)));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   } else {
-    const int col = c0 + perm_row(lane & 31);
+    const Tin* x = p + at(8 * g, perm_row(lane & 31)) + 16 * kk * LD + c0;
     f32x8 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = p[at(16 * kk + 8 * g + e, col)];
+    for (int e = 0; e < 8; ++e) r[e] = x[e * LD];
     return r;
   }
 }
 
 // A chunk's tokens on their way from memory into a tile: loads are issued into registers
-// and stored later.  Rows from `lim` on are zero, whatever memory holds there.
+// and stored later.  `chunk` is the address of the chunk's first row, the same for all
+// threads; rows from n on are zero, whatever memory holds there.
 template <typename Tin, int D, int NT>
 struct Stage {
   using TL = Tile<Tin, D>;
-  static constexpr int ALL = kChunk * TL::NP, N = (ALL + NT - 1) / NT;
+  static constexpr int STEP = NT / TL::NP;                      // rows per pass
+  static constexpr int N = (kChunk + STEP - 1) / STEP;
+  static_assert(NT % TL::NP == 0, "whole rows per pass");
   u32x4 v[N];
-  __device__ __forceinline__ void load(const Tin* base, int64_t st, int t0, int lim, int tid) {
+  __device__ __forceinline__ void load(const Tin* chunk, int64_t st, int n, int tid) {
+    const uint32_t row = tid / TL::NP, off = row * (uint32_t)st + (tid % TL::NP) * TL::PE;
+    if (n >= kChunk && kChunk % STEP == 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int x = i * NT + tid, row = x / TL::NP, pc = x % TL::NP, t = t0 + row;
-      v[i] = u32x4{0u, 0u, 0u, 0u};
-      if ((ALL % NT == 0 || x < ALL) && t < lim)
-        v[i] = *reinterpret_cast<const u32x4*>(base + t * st + pc * TL::PE);
+      for (int i = 0; i < N; ++i) v[i] = *reinterpret_cast<const u32x4*>(chunk + i * STEP * st + off);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        v[i] = u32x4{0u, 0u, 0u, 0u};
+        if (i * STEP + (int)row < min(n, kChunk))
+          v[i] = *reinterpret_cast<const u32x4*>(chunk + i * STEP * st + off);
+      }
     }
   }
   __device__ __forceinline__ void store(Tin* p, int tid) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int x = i * NT + tid, row = x / TL::NP, pc = x % TL::NP;
-      if (ALL % NT == 0 || x < ALL) *reinterpret_cast<u32x4*>(p + TL::at(row, pc * TL::PE)) = v[i];
+      const int row = i * STEP + tid / TL::NP;
+      if (kChunk % STEP == 0 || row < kChunk)
+        *reinterpret_cast<u32x4*>(p + TL::at(row, tid % TL::NP * TL::PE)) = v[i];
     }
   }
 };
@@ -108,24 +116,55 @@ struct Stage {
 // that hi_t - hi_s is exact and the difference keeps float32's precision however large the
 // sums are.  A gate whose decay is below float32's smallest normal number (-inf among them)
 // cuts: it counts as a step of -2^17 in hi, which no sum of a chunk's other gates reaches.
-// The decays kernel forms them once for all kernels of a call, float4 per token:
-//   hi, lo, in = e^{a_t} (from before the chunk), out = e^{a_end - a_t} (to its end).
-struct Decays {
-  float hi[kChunk], lo[kChunk], in[kChunk], out[kChunk];
-  __device__ __forceinline__ void store(const float4& d, int t) {
-    hi[t] = d.x;
-    lo[t] = d.y;
-    in[t] = d.z;
-    out[t] = d.w;
-  }
-  __device__ __forceinline__ float total() const { return in[kChunk - 1]; }   // e^{a_end}
-};
-
+// The decays kernel forms them once for all kernels of a call, per head hi and lo of every
+// token, then
+//   in = e^{a_t} (from before the chunk) and out = e^{a_end - a_t} (to its end) of every token.
 __device__ __forceinline__ float decay2(float hi_t, float lo_t, float hi_s, float lo_s) {
   return __builtin_amdgcn_exp2f((hi_t - hi_s) + (lo_t - lo_s));
 }
 
 constexpr float kCutGate = -87.33655f;   // ln of 2^-126
+
+// A chunk's decays in LDS: in, out, and between all pairs of its tokens, zero where the
+// later of a pair should come first.  pair[t][s] is scale times the decay between the lane
+// token t of chunk_step and s, so from s to t, or with REV from t to s.
+struct Decays {
+  static constexpr int LD = kChunk + 4;
+  float in[kChunk], out[kChunk], pair[kChunk * LD];
+  __device__ __forceinline__ float total() const { return in[kChunk - 1]; }   // e^{a_end}
+};
+
+template <int NT, bool REV>
+struct DecayStage {
+  static constexpr int M = kChunk * kChunk / NT, G = kChunk / M;   // M consecutive s per thread
+  float2 io, t, s[M];
+  __device__ __forceinline__ void load(const float2* head, int64_t padded, int t0, int tid) {
+    if (tid < kChunk) io = head[padded + t0 + tid];
+    t = head[t0 + tid / G];
+#pragma unroll
+    for (int i = 0; i < M; i += 2) {
+      const float4 x = *reinterpret_cast<const float4*>(head + t0 + (tid % G) * M + i);
+      s[i] = make_float2(x.x, x.y);
+      s[i + 1] = make_float2(x.z, x.w);
+    }
+  }
+  __device__ __forceinline__ void store(Decays& d, float scale, int tid) const {
+    if (tid < kChunk) {
+      d.in[tid] = io.x;
+      d.out[tid] = io.y;
+    }
+    const int tt = tid / G, s0 = (tid % G) * M;
+    float x[M];
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const float y = REV ? decay2(s[i].x, s[i].y, t.x, t.y) : decay2(t.x, t.y, s[i].x, s[i].y);
+      x[i] = (REV ? s0 + i >= tt : s0 + i <= tt) ? y * scale : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < M; i += 4)
+      *reinterpret_cast<float4*>(d.pair + tt * Decays::LD + s0 + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+  }
+};
 
 // An operand scaled by float32 weights per k: for bfloat16 in two terms, whose sum keeps
 // 16 bits or more of it, so that the states they add up to are not held to the 8 bits of one.
@@ -135,11 +174,17 @@ template <>
 struct Scaled<bf16_t> {
   bf16x8 h, l;
   __device__ __forceinline__ Scaled(const bf16x8& x, const float (&w)[8]) {
+    float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float y = (float)x[e] * w[e];
-      h[e] = (__bf16)y;
-      l[e] = (__bf16)(y - (float)h[e]);
+      y[e] = (float)x[e] * w[e];
+      h[e] = (__bf16)y[e];
+    }
+    const u32x4 z = __builtin_bit_cast(u32x4, h);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      l[e] = (__bf16)(y[e] - __uint_as_float(z[e >> 1] << 16));
+      l[e + 1] = (__bf16)(y[e + 1] - __uint_as_float(z[e >> 1] & 0xFFFF0000u));
     }
   }
   __device__ __forceinline__ void mma_b(f32x16& acc, const bf16x8& a) const {
@@ -175,9 +220,13 @@ __device__ __forceinline__ typename Frag<Tin>::T state_frag(const f32x16& s, int
   return Frag<Tin>::from_floats(x);
 }
 __device__ __forceinline__ bf16x8 state_frag_low(const f32x16& s, int kk, const bf16x8& h) {
+  const u32x4 w = __builtin_bit_cast(u32x4, h);   // by words: element by element each is rounded again
   bf16x8 r;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (__bf16)(s[8 * kk + e] - (float)h[e]);
+  for (int e = 0; e < 8; e += 2) {
+    r[e] = (__bf16)(s[8 * kk + e] - __uint_as_float(w[e >> 1] << 16));
+    r[e + 1] = (__bf16)(s[8 * kk + e + 1] - __uint_as_float(w[e >> 1] & 0xFFFF0000u));
+  }
   return r;
 }
 
@@ -200,84 +249,115 @@ __device__ __forceinline__ void store_state(const f32x16 (&s)[N], float* p, int6
       p[(32 * i + held_row(r, lane)) * rs + (c0 + perm_row(lane & 31)) * cs] = s[i][r];
 }
 
+// A wave's columns of a state, as f times its tiles: a chunk's decay goes to the factor,
+// and to the tiles only when that has become small, which saves a pass over them per chunk.
+template <int N>
+struct State {
+  f32x16 s[N];
+  float f = 1.f;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = zero16();
+  }
+  // Takes a decay, the same in all lanes (and known to be so: the factor is kept, and
+  // branches on it are taken, once).  True if the factor has left 2^-16 .. 2^16, inside of
+  // which what is added to the tiles, divided by it, stays well inside float32.
+  __device__ __forceinline__ bool decay(float total) {
+    f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(f * total)));
+    return !(f >= 1.52587890625e-05f && f <= 65536.f);
+  }
+  __device__ __forceinline__ void apply() {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[i][r] *= f;
+    f = 1.f;
+  }
+};
+
 // One chunk, for a wave's 32 columns of a state of R rows.  Lane l % 32 is token t; the
-// elements of c and o are columns c0 + held_row(r).
+// elements of o are columns c0 + held_row(r).
 //   p[r] = q_t . k_s with s = held_row(r)
 //   c = carry_t S^T q_t
 //   o = c + scale sum over s of p masked and decayed, times v_s
 // and the state takes up the chunk.  REV: time runs back, so s >= t.  PAIR: c also
-// takes what the state's rounding to bfloat16 leaves, and the lane's part of
+// takes what the state's rounding to bfloat16 leaves, and
 //   dot_t = y_t . c + scale sum over s != t of p masked and decayed, times (y_t . v_s)
-// is returned, with the rows y_t (32 columns of them a wave) in sy: what the pairs (s, t)
-// give to the gates between them.
+// is returned, with the rows y_t (the wave's 32 columns of them) in sy: what the pairs
+// (s, t) give to the gates between them.  The state's products come before the arithmetic
+// on scores and outputs, which they do not need and hide.
 template <typename Tin, int R, int C, bool REV, bool PAIR>
 __device__ __forceinline__ float chunk_step(const Tin* sq, const Tin* sk, const Tin* sv, const Tin* sy,
                                             const Decays& dec, float scale, int c0, int lane,
-                                            f32x16 (&S)[R / 32], f32x16& o) {
+                                            State<R / 32>& S, f32x16& o) {
   using F = typename Frag<Tin>::T;
   using TR = Tile<Tin, R>;
   using TC = Tile<Tin, C>;
-  const int t = lane & 31, g = lane >> 5, kr = perm_row(t);
-  const float hi = dec.hi[t], lo = dec.lo[t], total = dec.total();
-  f32x16 p = zero16();
+  const int t = lane & 31, kr = perm_row(t);
+  f32x16 p = zero16(), z = zero16();
+  F y[2];
   o = zero16();
 #pragma unroll
   for (int kk = 0; kk < R / 16; ++kk) {
     const F q = TR::row_frag(sq, t, kk, lane);
     Frag<Tin>::mma(p, TR::row_frag(sk, kr, kk, lane), q);
-    const F s = state_frag<Tin>(S[kk >> 1], kk & 1);
-    if constexpr (PAIR && sizeof(Tin) == 2) Frag<Tin>::mma(o, state_frag_low(S[kk >> 1], kk & 1, s), q);
+    const F s = state_frag<Tin>(S.s[kk >> 1], kk & 1);
+    if constexpr (PAIR && sizeof(Tin) == 2) Frag<Tin>::mma(o, state_frag_low(S.s[kk >> 1], kk & 1, s), q);
     Frag<Tin>::mma(o, s, q);
   }
-  // the scores, masked and decayed
-  float w[2][8];
-#pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
-    float hs[8], ls[8];
-    weights8(dec.hi, kk, lane, hs);
-    weights8(dec.lo, kk, lane, ls);
-    weights8(REV ? dec.in : dec.out, kk, lane, w[kk]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int s = 16 * kk + 8 * g + e;
-      const float d = REV ? decay2(hs[e], ls[e], hi, lo) : decay2(hi, lo, hs[e], ls[e]);
-      p[8 * kk + e] = (REV ? s >= t : s <= t) ? p[8 * kk + e] * d * scale : 0.f;
-      if constexpr (REV) w[kk][e] *= scale;
-    }
-  }
-  const float carry = REV ? dec.out[t] : dec.in[t] * scale;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) o[r] *= carry;
-  float dot = 0.f;
   if constexpr (PAIR) {
-    f32x16 z = zero16();
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      const F y = TC::row_frag(sy, t, c0 / 16 + kk, lane);
-      Frag<Tin>::mma(z, TC::row_frag(sv, kr, c0 / 16 + kk, lane), y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) dot += o[8 * kk + e] * (float)y[e];
+      y[kk] = TC::row_frag(sy + c0, t, kk, lane);
+      Frag<Tin>::mma(z, TC::row_frag(sv + c0, kr, kk, lane), y[kk]);
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dot += held_row(r, lane) != t ? p[r] * z[r] : 0.f;
-    dot += __shfl_xor(dot, 32);
   }
+  const float carry = (REV ? dec.out[t] : dec.in[t] * scale) * S.f;
+  if (S.decay(dec.total())) S.apply();
+  const float inv = (REV ? scale : 1.f) * __builtin_amdgcn_rcpf(S.f);
+  F v[2];
 #pragma unroll
-  for (int i = 0; i < R / 32; ++i)
+  for (int kk = 0; kk < 2; ++kk) {
+    float w[8];
+    weights8(REV ? dec.in : dec.out, kk, lane, w);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) S[i][r] *= total;
+    for (int e = 0; e < 8; ++e) w[e] *= inv;
+    v[kk] = TC::col_frag(sv, c0, kk, lane);
+    const Scaled<Tin> x(v[kk], w);
+#pragma unroll
+    for (int i = 0; i < R / 32; ++i) x.mma_b(S.s[i], TR::col_frag(sk, 32 * i, kk, lane));
+  }
+  // the scores, masked and decayed, and the carried part
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    float d[8];
+    weights8(dec.pair + t * Decays::LD, kk, lane, d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[8 * kk + e] *= d[e];
+      o[8 * kk + e] *= carry;
+    }
+  }
+  float dot[4] = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (PAIR) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dot[r & 3] += o[r] * (float)y[r >> 3][r & 7];
+      dot[r & 3] += held_row(r, lane) != t ? p[r] * z[r] : 0.f;
+    }
+  }
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) {
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = p[8 * kk + e];
-    const F v = TC::col_frag(sv, c0, kk, lane);
-    Frag<Tin>::mma(o, v, Frag<Tin>::from_floats(x));
-    const Scaled<Tin> y(v, w[kk]);
-#pragma unroll
-    for (int i = 0; i < R / 32; ++i) y.mma_b(S[i], TR::col_frag(sk, 32 * i, kk, lane));
+    Frag<Tin>::mma(o, v[kk], Frag<Tin>::from_floats(x));
   }
-  return dot;
+  if constexpr (PAIR) {
+    const float x = (dot[0] + dot[1]) + (dot[2] + dot[3]);
+    return x + __shfl_xor(x, 32);
+  }
+  return 0.f;
 }
 
 // Eight consecutive values of an output row, rounded once to the output's type.
@@ -291,11 +371,18 @@ __device__ __forceinline__ void store8(float* p, const f32x16& x, int k) {
   *reinterpret_cast<float4*>(p) = make_float4(x[8 * k], x[8 * k + 1], x[8 * k + 2], x[8 * k + 3]);
   *reinterpret_cast<float4*>(p + 4) = make_float4(x[8 * k + 4], x[8 * k + 5], x[8 * k + 6], x[8 * k + 7]);
 }
-// A lane's columns of its token's output row
+// A chunk's outputs, lane l % 32 being a token: `chunk` is the address of its first row, the
+// same for all threads; rows from `end` on do not exist, those from n on are zero.
 template <typename Tout>
-__device__ __forceinline__ void store_out(Tout* row, int c0, const f32x16& o, int lane) {
+__device__ __forceinline__ void store_out(Tout* chunk, int64_t st, int c0, f32x16& o, int n, int end, int lane) {
+  const int t = lane & 31;
+  const uint32_t off = t * (uint32_t)st + c0 + 8 * (lane >> 5);
+  if (n < kChunk) {
+    if (t >= n) o = zero16();
+    if (t >= end) return;
+  }
 #pragma unroll
-  for (int k = 0; k < 2; ++k) store8(row + c0 + 16 * k + 8 * (lane >> 5), o, k);
+  for (int k = 0; k < 2; ++k) store8(chunk + off + 16 * k, o, k);
 }
 
 }  // namespace dla

@@ -122,7 +122,7 @@ RecArgs args_of(const dla_recurrence_desc& d, const Plan& p, const dla_rows* gat
   a.seg_state = (float*)(ws + s.seg_state);
   a.seg_adj = (float*)(ws + s.seg_adj);
   a.seg_decay = (float*)(ws + s.seg_decay);
-  a.decays = (float4*)(ws + s.decays);
+  a.decays = (float2*)(ws + s.decays);
   return a;
 }
 
