@@ -171,7 +171,10 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
 
 // A segment's own part of the state behind it, sum over its tokens of (decay to the
 // segment's end) k_s v_s^T; reverse: of the adjoint before it, sum of scale (decay from
-// the segment's start) q_s do_s^T.
+// the segment's start) q_s do_s^T.  Both go from the segment's last chunk to its first: the
+// pass that follows begins there, with what is still in the caches.  Going back the state
+// itself does not decay, each chunk's part does, and where nothing is left of it (a cut
+// gate behind it) the rest of the segment adds nothing and is not read.
 template <typename Tin, int DK, int DV>
 struct SegTiles {
   Tin k[Tile<Tin, DK>::SIZE], v[Tile<Tin, DV>::SIZE];
@@ -211,7 +214,7 @@ __global__ __launch_bounds__(2 * DV, sizeof(Tin) == 4 ? 1 : (DV == 128 ? 3 : 2))
     }
   };
   const int n = (end - begin + kChunk - 1) / kChunk;
-  auto chunk_at = [&](int c) { return begin + (REV ? n - 1 - c : c) * kChunk; };
+  auto chunk_at = [&](int c) { return begin + (n - 1 - c) * kChunk; };
   request(chunk_at(0));
   store(tiles[0]);
   __syncthreads();
@@ -219,19 +222,20 @@ __global__ __launch_bounds__(2 * DV, sizeof(Tin) == 4 ? 1 : (DV == 128 ? 3 : 2))
     const SegTiles<Tin, DK, DV>& now = tiles[c & 1];
     if (c + 1 < n) request(chunk_at(c + 1));
     const float total = now.in[kChunk - 1];
-    decay *= total;
-    if (S.decay(total)) S.apply();
-    const float inv = (REV ? a.scale : 1.f) * __builtin_amdgcn_rcpf(S.f);
+    if (REV && S.decay(total)) S.apply();
+    const float weight = REV ? a.scale * __builtin_amdgcn_rcpf(S.f) : decay;
+    decay = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(decay * total)));
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
       float w[8];
       weights8(REV ? now.in : now.out, kk, lane, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] *= inv;
+      for (int e = 0; e < 8; ++e) w[e] *= weight;
       const Scaled<Tin> z(Tile<Tin, DV>::col_frag(now.v, c0, kk, lane), w);
 #pragma unroll
       for (int i = 0; i < ST; ++i) z.mma_b(S.s[i], Tile<Tin, DK>::col_frag(now.k, 32 * i, kk, lane));
     }
+    if (!REV && decay == 0.f) break;
     if (c + 1 < n) store(tiles[(c + 1) & 1]);
     __syncthreads();
   }
