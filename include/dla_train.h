@@ -26,7 +26,9 @@ extern "C" {
  * elements.  [B][H][T][d] arrays, [B][T][H][d] ones and slices of a wider
  * projection's output are all rows.  Token rows start at multiples of 16 bytes:
  * data and every stride whose dimension is larger than 1.  Gates are rows of
- * d = 1 and need no alignment beyond their type's.
+ * d = 1 and need no alignment beyond their type's.  0 <= stride_t < 2^26.  Inputs may
+ * repeat rows (strides of zero); output rows are at least d apart in every
+ * dimension larger than 1, and overlap no input.
  */
 typedef struct {
   void* data;
@@ -60,7 +62,7 @@ typedef struct {
  * float32's precision to about 2^-17.  dg adds up what scores and rounded states
  * give and is of the inputs' type.
  * An infinity or NaN in a token reaches every later output of its head, and may
- * reach those of up to 63 tokens before it.
+ * reach those of up to 31 tokens before it.
  */
 typedef struct {
   int32_t B, H, Hk, T, d_k, d_v;
@@ -88,7 +90,7 @@ dla_status dla_recurrence_forward(const dla_recurrence_desc* desc, const dla_row
  * gradients of its outputs: dout, rows of d_v, and dstate_out [B][H][d_k][d_v], or
  * NULL for zero.  Writes dq, dk (Hk heads, summed over the heads that share them), dv,
  * dg (rows of one value in the inputs' type) and, where dstate is not NULL, the
- * gradient of S_0. */
+ * gradient of S_0 (which may be dstate_out's array). */
 dla_status dla_recurrence_backward(const dla_recurrence_desc* desc, const dla_rows* q,
                                    const dla_rows* k, const dla_rows* v, const dla_rows* log_gate,
                                    const float* state, const dla_rows* dout,

@@ -44,6 +44,7 @@ struct RecArgs {
   float2* decays;      // [heads][2][chunks * kRecChunk], see recurrence_tile.h
 };
 
+constexpr float kCutGate = -87.33655f;   // ln of 2^-126: a gate below it is a decay of zero
 constexpr int kRecChunk = 32;   // tokens a workgroup takes at a time
 __host__ __device__ inline int64_t rec_padded(int T) { return ((int64_t)T + kRecChunk - 1) / kRecChunk * kRecChunk; }
 
@@ -74,11 +75,10 @@ hipError_t launch_recurrence_segments(const RecArgs& a, int dtype, bool reverse,
 hipError_t launch_recurrence_step(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
                                   const Rows& v, const Rows& out, const float* s0, float* s_out,
                                   hipStream_t st);
-// dg from the per-token sums: dg_t = end_dot + sum over s >= t of (qdot_s - kdot_s).
+// dg from the per-token sums: dg_t = end_dot + sum over s >= t of (qdot_s - kdot_s); anchor:
+// [heads][nseg] of workspace.
 hipError_t launch_recurrence_dgate(const RecArgs& a, int dtype, const float* qdot, const float* kdot,
-                                   const float* end_dot, double* block_sum, int* block_cut,
-                                   const Rows& dg, hipStream_t st);
-constexpr int kDgateBlock = 1024;   // tokens per workgroup of the gate's gradient
+                                   double* anchor, const float* end_dot, const Rows& dg, hipStream_t st);
 // Sums the heads that share a key head: [B][H][T][d] float32 -> rows of B * Hk heads.
 hipError_t launch_head_sum(const RecArgs& a, int dtype, const float* part, const Rows& out,
                            hipStream_t st);

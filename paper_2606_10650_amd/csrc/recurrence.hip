@@ -29,7 +29,7 @@ struct ScanArgs {
   float* dot;              // PAIR: [heads][T]
   const float* end_with;   // PAIR: per head, or null; end_dot = <end_with, last state>
   float* end_dot;
-  int out_f32;
+  int out_f32;             // PAIR: out is float32
 };
 
 // Decays of a chunk's tokens, a half-wave per chunk.
@@ -355,30 +355,33 @@ hipError_t launch_recurrence_adjoint(const RecArgs& a, int dtype, const Rows& q,
                                      const Rows& v, const Rows& dout, const Rows& dk, bool dk_f32,
                                      const Rows& dv, const float* dstate, float* ds0, float* kdot,
                                      hipStream_t st) {
+  // dk before dv, so that ds0, which the latter writes, may be dstate's array
   ScanArgs f{};
   f.a = a;
-  f.q = k;
-  f.k = q;
-  f.v = dout;
-  f.out = dv;
-  f.first = dstate;
-  f.s_rs = a.dv;
-  f.s_cs = 1;
-  f.seg_first = a.nseg > 1 ? a.seg_adj : nullptr;
-  f.last = ds0;
-  const hipError_t e = launch_scan<true, false>(f, dtype, a.dk, a.dv, st);
-  if (e != hipSuccess) return e;
   f.q = v;
   f.k = dout;
   f.v = q;
   f.out = dk;
   f.y = k;
+  f.first = dstate;
   f.s_rs = 1;
   f.s_cs = a.dv;
-  f.last = nullptr;
+  f.seg_first = a.nseg > 1 ? a.seg_adj : nullptr;
   f.dot = kdot;
   f.out_f32 = dk_f32 ? 1 : 0;
-  return launch_scan<true, true>(f, dtype, a.dv, a.dk, st);
+  const hipError_t e = launch_scan<true, true>(f, dtype, a.dv, a.dk, st);
+  if (e != hipSuccess) return e;
+  f.q = k;
+  f.k = q;
+  f.v = dout;
+  f.out = dv;
+  f.y = Rows();
+  f.s_rs = a.dv;
+  f.s_cs = 1;
+  f.last = ds0;
+  f.dot = nullptr;
+  f.out_f32 = 0;
+  return launch_scan<true, false>(f, dtype, a.dk, a.dv, st);
 }
 
 }  // namespace dla

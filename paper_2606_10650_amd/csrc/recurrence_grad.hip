@@ -25,84 +25,95 @@ namespace dla {
 namespace {
 
 // dg from the tokens' sums, from the last token back, in float64: what is added up spans
-// the sequence, what is left may be small.  A cut gate lets nothing through: dg is zero
-// there and the sum starts anew, exactly.  Two passes over blocks of tokens: each block's
-// sum back to its first cut, then the tokens.
+// many tokens, what is left may be small.  Each segment starts from its own end, where the
+// sum is <adjoint behind the segment, state there>, so that what the tokens' sums were
+// rounded by adds up over a segment at most.  A cut gate lets nothing through: dg is zero
+// there and the sum starts anew, exactly.
+__global__ __launch_bounds__(256) void anchor_kernel(RecArgs a, double* anchor) {
+  __shared__ double sums[4];
+  const int64_t D = (int64_t)a.dk * a.dv;
+  const int seg = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
+  const float* s = a.seg_state + ((int64_t)head * a.nseg + seg + 1) * D;
+  const float* r = a.seg_adj + ((int64_t)head * a.nseg + seg) * D;
+  double x = 0.0;
+  for (int64_t i = tid * 4; i < D; i += 1024) {
+    const float4 p = *reinterpret_cast<const float4*>(s + i), q = *reinterpret_cast<const float4*>(r + i);
+    x += (double)p.x * q.x + (double)p.y * q.y + ((double)p.z * q.z + (double)p.w * q.w);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+  if ((tid & 63) == 0) sums[tid >> 6] = x;
+  __syncthreads();
+  if (tid == 0) anchor[(int64_t)head * a.nseg + seg] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+
 struct DgArgs {
   RecArgs a;
   const float* qdot;
   const float* kdot;
-  const float* end_dot;
-  double* block_sum;
-  int* block_cut;
+  const double* anchor;   // [heads][nseg], the last segment's apart:
+  const float* end_dot;   // [heads], or null for zero
   Rows dg;
   int dtype;
 };
 
-constexpr int kPer = kDgateBlock / 256;
+constexpr int kPer = 4, kDgateBlock = 256 * kPer;
 
+// x, cut: the sum of a run of tokens back to its first cut, and whether it has one; takes
+// the run behind it
 __device__ __forceinline__ void later(double& x, int& cut, double y, int ycut) {
-  // x, cut: the part before; y, ycut: the part behind it
   if (!cut) x += y;
   cut |= ycut;
 }
 
-template <bool LAST>
 __global__ __launch_bounds__(256) void dgate_kernel(DgArgs f) {
   const RecArgs& a = f.a;
-  const int nb = gridDim.x, block = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
-  const int lane = tid & 63, wave = tid >> 6;
+  const int seg = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = head / a.H, h = head % a.H;
   const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
   const float* gate = row_base<const float>(a.gate, b, h);
+  const float* qd = f.qdot + (int64_t)head * a.T;
+  const float* kd = f.kdot + (int64_t)head * a.T;
   __shared__ double sums[4];
   __shared__ int cuts[4];
-  const int64_t t0 = (int64_t)block * kDgateBlock + tid * kPer;
-  double x[kPer];
-  int cut[kPer];
-  double sum = 0.0;   // of the thread's tokens, from the last back to the first cut
-  int any = 0;
+  double carry = 0.0;   // of what is behind the block
+  if (seg < a.nseg - 1) carry = f.anchor[(int64_t)head * a.nseg + seg];
+  else if (f.end_dot) carry = (double)f.end_dot[head];
+  for (int base = begin + (end - begin - 1) / kDgateBlock * kDgateBlock; base >= begin; base -= kDgateBlock) {
+    const int t0 = base + tid * kPer;
+    double x[kPer];
+    int cut[kPer];
+    double sum = 0.0;   // of the thread's tokens, from the last back to the first cut
+    int any = 0;
 #pragma unroll
-  for (int i = kPer - 1; i >= 0; --i) {
-    const int64_t t = t0 + i;
-    x[i] = 0.0;
-    cut[i] = 0;
-    if (t < lim) {
-      x[i] = (double)f.qdot[(int64_t)head * a.T + t] - (double)f.kdot[(int64_t)head * a.T + t];
-      cut[i] = gate[t * a.gate.st] < kCutGate;
+    for (int i = kPer - 1; i >= 0; --i) {
+      const int t = t0 + i;
+      x[i] = 0.0;
+      cut[i] = 0;
+      if (t < end && t < lim) {
+        x[i] = (double)qd[t] - (double)kd[t];
+        cut[i] = gate[t * a.gate.st] < kCutGate;
+      }
+      // a cut at t: it and what is behind it count for no earlier token
+      sum = cut[i] ? 0.0 : sum + x[i];
+      any |= cut[i];
     }
-    // a cut at t: what is at t and behind it counts for no earlier token
-    double s = x[i];
-    int c = cut[i];
-    if (c) s = 0.0;
-    later(s, c, sum, any);
-    sum = s;
-    any = c;
-  }
-  // this thread's sum and those of the threads behind it in the wave
-  double ws = sum;
-  int wc = any;
+    double ws = sum;   // with the threads behind it in the wave
+    int wc = any;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_down(ws, o);
-    const int c = __shfl_down(wc, o);
-    if (lane + o < 64) later(ws, wc, y, c);
-  }
-  if (lane == 0) {
-    sums[wave] = ws;
-    cuts[wave] = wc;
-  }
-  __syncthreads();
-  if constexpr (!LAST) {
-    if (tid == 0) {
-      double s = sums[0];
-      int c = cuts[0];
-      for (int w = 1; w < 4; ++w) later(s, c, sums[w], cuts[w]);
-      f.block_sum[(int64_t)head * nb + block] = s;
-      f.block_cut[(int64_t)head * nb + block] = c;
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_down(ws, o);
+      const int c = __shfl_down(wc, o);
+      if (lane + o < 64) later(ws, wc, y, c);
     }
-  } else {
-    // what is behind this thread: the rest of its wave, the waves and blocks behind
+    __syncthreads();   // the last block's sums are read
+    if (lane == 0) {
+      sums[wave] = ws;
+      cuts[wave] = wc;
+    }
+    __syncthreads();
+    // what is behind this thread: the rest of its wave, the waves behind, the blocks behind
     double s = __shfl_down(ws, 1);
     int c = __shfl_down(wc, 1);
     if (lane == 63) {
@@ -110,14 +121,17 @@ __global__ __launch_bounds__(256) void dgate_kernel(DgArgs f) {
       c = 0;
     }
     for (int w = wave + 1; w < 4; ++w) later(s, c, sums[w], cuts[w]);
-    for (int i = block + 1; i < nb && !c; ++i)
-      later(s, c, f.block_sum[(int64_t)head * nb + i], f.block_cut[(int64_t)head * nb + i]);
-    if (!c && f.end_dot) s += (double)f.end_dot[head];
+    later(s, c, carry, 0);
+    double all = sums[0];
+    c = cuts[0];
+    for (int w = 1; w < 4; ++w) later(all, c, sums[w], cuts[w]);
+    later(all, c, carry, 0);
+    carry = all;
 #pragma unroll
     for (int i = kPer - 1; i >= 0; --i) {
-      const int64_t t = t0 + i;
+      const int t = t0 + i;
       s = cut[i] ? 0.0 : s + x[i];
-      if (t < a.T) {
+      if (t < end) {
         const float y = t < lim ? (float)s : 0.f;
         const int64_t at = b * f.dg.sb + h * f.dg.sh + t * f.dg.st;
         if (f.dtype == DLA_BF16) static_cast<__bf16*>(f.dg.p)[at] = (__bf16)y;
@@ -162,12 +176,10 @@ __global__ __launch_bounds__(256) void head_sum_kernel(RecArgs a, const float* p
 }  // namespace
 
 hipError_t launch_recurrence_dgate(const RecArgs& a, int dtype, const float* qdot, const float* kdot,
-                                   const float* end_dot, double* block_sum, int* block_cut,
-                                   const Rows& dg, hipStream_t st) {
-  DgArgs f{a, qdot, kdot, end_dot, block_sum, block_cut, dg, dtype};
-  const dim3 grid((a.T + kDgateBlock - 1) / kDgateBlock, a.B * a.H);
-  if (grid.x > 1) hipLaunchKernelGGL((dgate_kernel<false>), grid, dim3(256), 0, st, f);
-  hipLaunchKernelGGL((dgate_kernel<true>), grid, dim3(256), 0, st, f);
+                                   double* anchor, const float* end_dot, const Rows& dg, hipStream_t st) {
+  if (a.nseg > 1) hipLaunchKernelGGL(anchor_kernel, dim3(a.nseg - 1, a.B * a.H), dim3(256), 0, st, a, anchor);
+  const DgArgs f{a, qdot, kdot, anchor, end_dot, dg, dtype};
+  hipLaunchKernelGGL(dgate_kernel, dim3(a.nseg, a.B * a.H), dim3(256), 0, st, f);
   return hipGetLastError();
 }
 

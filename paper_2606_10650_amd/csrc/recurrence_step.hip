@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void step_kernel(RecArgs a, Rows q, Rows k, Ro
   for (int t = 0; t < a.T; ++t) {
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (t < lim) {
-      const float d = expf(gate[t * a.gate.st]);
+      const float x = gate[t * a.gate.st], d = x < kCutGate ? 0.f : expf(x);
       float y[4];
       load4f(vp + t * v.st, y);
 #pragma unroll

@@ -123,8 +123,6 @@ __device__ __forceinline__ float decay2(float hi_t, float lo_t, float hi_s, floa
   return __builtin_amdgcn_exp2f((hi_t - hi_s) + (lo_t - lo_s));
 }
 
-constexpr float kCutGate = -87.33655f;   // ln of 2^-126
-
 // A chunk's decays in LDS: in, out, and between all pairs of its tokens, zero where the
 // later of a pair should come first.  pair[t][s] is scale times the decay between the lane
 // token t of chunk_step and s, so from s to t, or with REV from t to s.

@@ -27,8 +27,8 @@ struct Plan {
 // so that all of them work, at the price of reading keys and values (queries and output
 // gradients) once more for the segments' states.
 Plan plan_of(const dla_recurrence_desc& d, bool backward) {
-  Plan p;
-  p.step = !backward && d.T <= kStepTokens;
+  Plan p{!backward && d.T <= kStepTokens, 1, kRecChunk};
+  if (d.B == 0 || d.T == 0) return p;   // nothing to plan
   const int chunk = kRecChunk, heads = d.B * d.H;
   const int chunks = (d.T + chunk - 1) / chunk;
   int n = 1;
@@ -38,15 +38,16 @@ Plan plan_of(const dla_recurrence_desc& d, bool backward) {
     if (n > 64) n = 64;
     if (n < 1) n = 1;
   }
+  // float32: at most 1024 tokens, so that dg's sums keep float32's precision
+  if (backward && d.dtype == DLA_F32 && n < (d.T + 1023) / 1024) n = (d.T + 1023) / 1024;
   const int per = (chunks + n - 1) / n;
   p.seg_len = per * chunk;
-  p.nseg = per > 0 ? (chunks + per - 1) / per : 1;
-  if (p.nseg < 1) p.nseg = 1;
+  p.nseg = (chunks + per - 1) / per;
   return p;
 }
 
 struct Space {
-  size_t decays, seg_state, seg_adj, seg_decay, qdot, kdot, end_dot, block_sum, block_cut, dq_part, dk_part, total;
+  size_t decays, seg_state, seg_adj, seg_decay, qdot, kdot, end_dot, anchor, dq_part, dk_part, total;
 };
 
 Space space_of(const dla_recurrence_desc& d, const Plan& p, bool backward) {
@@ -70,9 +71,7 @@ Space space_of(const dla_recurrence_desc& d, const Plan& p, bool backward) {
     s.qdot = take(tokens * 4);
     s.kdot = take(tokens * 4);
     s.end_dot = take(heads * 4);
-    const size_t blocks = ((size_t)d.T + kDgateBlock - 1) / kDgateBlock;
-    s.block_sum = take(heads * blocks * 8);
-    s.block_cut = take(heads * blocks * 4);
+    s.anchor = take(heads * p.nseg * 8);
     if (d.Hk != d.H) {
       s.dq_part = take(tokens * d.d_k * 4);
       s.dk_part = take(tokens * d.d_k * 4);
@@ -92,16 +91,20 @@ dla_status check(const dla_recurrence_desc* d) {
   return DLA_OK;
 }
 
-// Rows of a call's tensor: there, and aligned to `bytes` (0: to their type).
-bool rows_ok(const dla_rows* r, const dla_recurrence_desc& d, int heads, int bytes, int elem) {
+// Rows of `width` values of a call's tensor: there, aligned to 16 bytes (rows of one value:
+// to their type), with a token stride that 32 rows of it keep within 32 bits; of an output
+// also apart from each other.
+bool rows_ok(const dla_rows* r, const dla_recurrence_desc& d, int heads, int width, int elem, bool output) {
   if (!r || !r->data) return false;
-  const int align = bytes ? bytes : elem;
+  const int align = width > 1 ? 16 : elem;
   if ((uintptr_t)r->data % align) return false;
   const int64_t st[3] = {r->stride_b, r->stride_h, r->stride_t};
   const int n[3] = {d.B, heads, d.T};
-  for (int i = 0; i < 3; ++i)
-    if (n[i] > 1 && bytes && (st[i] * elem) % bytes) return false;
-  return true;
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] <= 1) continue;
+    if ((st[i] * elem) % align || (output && st[i] < width)) return false;
+  }
+  return d.T <= 1 || (r->stride_t >= 0 && r->stride_t < ((int64_t)1 << 26));
 }
 
 bool state_ok(const void* p) { return ((uintptr_t)p & 15u) == 0; }
@@ -229,8 +232,9 @@ dla_status dla_recurrence_forward(const dla_recurrence_desc* desc, const dla_row
   hipStream_t st = (hipStream_t)stream;
   if (d.B == 0) return remember(DLA_OK);
   if (d.T == 0) return remember(copy_state(d, state, state_out, st) == hipSuccess ? DLA_OK : DLA_ERR_HIP);
-  if (!rows_ok(q, d, d.Hk, 16, e) || !rows_ok(k, d, d.Hk, 16, e) || !rows_ok(v, d, d.H, 16, e) ||
-      !rows_ok(out, d, d.H, 16, e) || !rows_ok(log_gate, d, d.H, 0, 4))
+  if (!rows_ok(q, d, d.Hk, d.d_k, e, false) || !rows_ok(k, d, d.Hk, d.d_k, e, false) ||
+      !rows_ok(v, d, d.H, d.d_v, e, false) || !rows_ok(out, d, d.H, d.d_v, e, true) ||
+      !rows_ok(log_gate, d, d.H, 1, 4, false))
     return remember(DLA_ERR_INVALID_ARG);
   const Plan p = plan_of(d, false);
   const Space sp = space_of(d, p, false);
@@ -262,9 +266,11 @@ dla_status dla_recurrence_backward(const dla_recurrence_desc* desc, const dla_ro
   hipStream_t st = (hipStream_t)stream;
   if (d.B == 0) return remember(DLA_OK);
   if (d.T == 0) return remember(copy_state(d, dstate_out, dstate, st) == hipSuccess ? DLA_OK : DLA_ERR_HIP);
-  if (!rows_ok(q, d, d.Hk, 16, e) || !rows_ok(k, d, d.Hk, 16, e) || !rows_ok(v, d, d.H, 16, e) ||
-      !rows_ok(dout, d, d.H, 16, e) || !rows_ok(dq, d, d.Hk, 16, e) || !rows_ok(dk, d, d.Hk, 16, e) ||
-      !rows_ok(dv, d, d.H, 16, e) || !rows_ok(log_gate, d, d.H, 0, 4) || !rows_ok(dg, d, d.H, 0, e))
+  if (!rows_ok(q, d, d.Hk, d.d_k, e, false) || !rows_ok(k, d, d.Hk, d.d_k, e, false) ||
+      !rows_ok(v, d, d.H, d.d_v, e, false) || !rows_ok(dout, d, d.H, d.d_v, e, false) ||
+      !rows_ok(dq, d, d.Hk, d.d_k, e, true) || !rows_ok(dk, d, d.Hk, d.d_k, e, true) ||
+      !rows_ok(dv, d, d.H, d.d_v, e, true) || !rows_ok(log_gate, d, d.H, 1, 4, false) ||
+      !rows_ok(dg, d, d.H, 1, e, true))
     return remember(DLA_ERR_INVALID_ARG);
   const Plan p = plan_of(d, true);
   const Space sp = space_of(d, p, true);
@@ -299,8 +305,8 @@ dla_status dla_recurrence_backward(const dla_recurrence_desc* desc, const dla_ro
   if (r == hipSuccess)
     r = launch_recurrence_adjoint(a, d.dtype, qr, kr, vr, dor, dkp, shared, rows_of(dv, 1), dstate_out, dstate, kdot, st);
   if (r == hipSuccess)
-    r = launch_recurrence_dgate(a, d.dtype, qdot, kdot, dstate_out ? end_dot : nullptr,
-                                (double*)(ws + sp.block_sum), (int*)(ws + sp.block_cut), rows_of(dg, 1), st);
+    r = launch_recurrence_dgate(a, d.dtype, qdot, kdot, (double*)(ws + sp.anchor),
+                                dstate_out ? end_dot : nullptr, rows_of(dg, 1), st);
   if (shared && r == hipSuccess) {
     r = launch_head_sum(a, d.dtype, (const float*)dqp.p, dqr, st);
     if (r == hipSuccess) r = launch_head_sum(a, d.dtype, (const float*)dkp.p, dkr, st);
