@@ -10,37 +10,26 @@ for a model written in torch.
 from __future__ import annotations
 
 import ctypes
+import functools
+import struct
 from typing import Optional
 
 import torch
 
 from . import dla
-from .dla import DLA_BF16, DLA_F32, _check, _dtype_code, _ptr, _stream
+from .dla import DLA_BF16, DLA_F32, _check, _dtype_code
 
 DLA_STATE_FP8 = 2
 FP8 = torch.float8_e4m3fn
 FP8_BLOCK = 256          # elements per scale of 8-bit optimizer states
 
 
-class Rows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
-                ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64)]
-
-
-class RecurrenceDesc(ctypes.Structure):
-    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32),
-                ("T", ctypes.c_int32), ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32),
-                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
-                ("lengths", ctypes.c_void_p)]
-
-
-class NormDesc(ctypes.Structure):
-    _fields_ = [("rows", ctypes.c_int64), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
-                ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
-
-
-class NormRows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+# A decode step calls these with little to do on the GPU, so the descriptions of its
+# arguments are packed as bytes, which costs a tenth of filling ctypes structures.
+_ROWS = struct.Struct("Pqqq")            # dla_rows
+_RECURRENCE = struct.Struct("7ifP")      # dla_recurrence_desc
+_NORM = struct.Struct("q3if")            # dla_norm_desc
+_NORM_ROWS = struct.Struct("Pq")         # dla_norm_rows
 
 
 class AdamWTensor(ctypes.Structure):
@@ -58,85 +47,87 @@ class AdamWParams(ctypes.Structure):
                 ("grad_scale", ctypes.c_void_p)]
 
 
-_bound = False
-
-
+@functools.lru_cache(maxsize=None)
 def lib():
     """libdla.so with the training entry points declared."""
-    global _bound
     L = dla.lib()
-    if not _bound:
-        P, S, I = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
-        ref = ctypes.POINTER
-        R, N = ref(Rows), ref(NormRows)
-        L.dla_recurrence_workspace_size.argtypes = [ref(RecurrenceDesc), I, ref(S)]
-        L.dla_recurrence_forward.argtypes = [ref(RecurrenceDesc), R, R, R, R, P, R, P, P, S, P]
-        L.dla_recurrence_backward.argtypes = [ref(RecurrenceDesc), R, R, R, R, P, R, P, R, R, R, R,
-                                              P, P, S, P]
-        L.dla_rms_norm.argtypes = [ref(NormDesc), N, N, P, N, N, P, P]
-        L.dla_rms_norm_fp8.argtypes = [ref(NormDesc), N, N, P, N, N, P, P]
-        L.dla_rms_norm_workspace_size.argtypes = [ref(NormDesc), ref(S)]
-        L.dla_rms_norm_backward.argtypes = [ref(NormDesc), N, N, P, P, N, N, P, P, S, P]
-        L.dla_adamw_step.argtypes = [ref(AdamWTensor), I, ref(AdamWParams), P]
-        for name in dla.EXPORTED:
-            if name.startswith(("dla_recurrence", "dla_rms_norm", "dla_adamw")):
-                getattr(L, name).restype = ctypes.c_int
-        _bound = True
+    P, S, I = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
+    L.dla_recurrence_workspace_size.argtypes = [P, I, ctypes.POINTER(S)]
+    L.dla_recurrence_forward.argtypes = [P] * 9 + [S, P]
+    L.dla_recurrence_backward.argtypes = [P] * 14 + [S, P]
+    L.dla_rms_norm.argtypes = [P] * 8
+    L.dla_rms_norm_fp8.argtypes = [P] * 8
+    L.dla_rms_norm_workspace_size.argtypes = [P, ctypes.POINTER(S)]
+    L.dla_rms_norm_backward.argtypes = [P] * 9 + [S, P]
+    L.dla_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), I, ctypes.POINTER(AdamWParams), P]
+    for name in dla.EXPORTED:
+        if name.startswith(("dla_recurrence", "dla_rms_norm", "dla_adamw")):
+            getattr(L, name).restype = ctypes.c_int
     return L
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(device):
+    """The current stream's handle, without a Stream object around it where torch has a call for that."""
+    if _raw_stream is not None and device.index is not None:
+        return _raw_stream(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 # ---------------------------------------------------------------------------
 # recurrence
 # ---------------------------------------------------------------------------
-def _rows(t, name, d=None):
-    """dla_rows of a [B, heads, T, d] tensor, or of a [B, H, T] one (d None)."""
-    if t is None:
-        return None
-    if t.dim() != (3 if d is None else 4):
-        raise ValueError(f"{name}: {t.dim()} dimensions")
-    if d is not None and (t.shape[3] != d or (d > 1 and t.numel() and t.stride(3) != 1)):
-        raise ValueError(f"{name}: the last axis must be {d} contiguous values")
-    return ctypes.byref(Rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)))
+def _rows(t, name):
+    """dla_rows of a [B, heads, T, d] tensor, or of a [B, H, T] one."""
+    st = t.stride()
+    if len(st) == 4 and st[3] != 1 and t.numel():
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    return _ROWS.pack(t.data_ptr(), st[0], st[1], st[2])
 
 
-def _rec_desc(B, H, Hk, T, d_k, d_v, dtype, scale=1.0, lengths=None):
-    return RecurrenceDesc(B, H, Hk, T, d_k, d_v, _dtype_code(dtype), float(scale),
-                          None if lengths is None else lengths.data_ptr())
+def _desc(B, H, Hk, T, d_k, d_v, dtype, scale=1.0, lengths=None):
+    return _RECURRENCE.pack(B, H, Hk, T, d_k, d_v, _dtype_code(dtype), scale,
+                            0 if lengths is None else lengths.data_ptr())
 
 
+@functools.lru_cache(maxsize=4096)
 def recurrence_workspace_bytes(B: int, H: int, Hk: int, T: int, d_k: int, d_v: int, dtype, *,
                                backward: bool = False) -> int:
     """Workspace of a forward (or backward) pass; 0 where none is needed."""
     n = ctypes.c_size_t(0)
-    _check(lib().dla_recurrence_workspace_size(
-        ctypes.byref(_rec_desc(B, H, Hk, T, d_k, d_v, dtype)), int(backward), ctypes.byref(n)),
-        "dla_recurrence_workspace_size")
+    _check(lib().dla_recurrence_workspace_size(_desc(B, H, Hk, T, d_k, d_v, dtype), int(backward),
+                                               ctypes.byref(n)), "dla_recurrence_workspace_size")
     return int(n.value)
 
 
-def _checked(q, k, v, g, lengths, more):
-    """Shapes, types and devices of a call; (B, H, Hk, T, d_k, d_v)."""
+def _sizes(q, k, v, g, lengths):
+    """(B, H, Hk, T, d_k, d_v) of a call whose inputs fit each other."""
     B, Hk, T, d_k = q.shape
-    H, d_v = v.shape[1], v.shape[3]
-    if k.shape != q.shape or v.shape != (B, H, T, d_v) or g.shape != (B, H, T):
+    _, H, _, d_v = v.shape
+    if k.shape != q.shape or v.shape[0] != B or v.shape[2] != T or g.shape != (B, H, T):
         raise ValueError(f"shapes {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}, {tuple(g.shape)}")
-    if g.dtype != torch.float32:
-        raise ValueError("gates must be float32")
+    dtype, dev = q.dtype, q.device
+    if k.dtype != dtype or v.dtype != dtype or g.dtype != torch.float32:
+        raise ValueError(f"types {dtype}, {k.dtype}, {v.dtype}, {g.dtype}: one type and float32 gates are wanted")
+    if k.device != dev or v.device != dev or g.device != dev:
+        raise ValueError("q, k, v and g must be on one device")
     if lengths is not None and (lengths.shape != (B,) or lengths.dtype != torch.int32 or
-                                not lengths.is_contiguous()):
-        raise ValueError("lengths must be int32 [B], contiguous")
-    state = (B, H, d_k, d_v)
-    for t, shape, dtype in [(k, None, q.dtype), (v, None, q.dtype), (g, None, None), (lengths, None, None)] + more:
-        if t is None:
-            continue
-        if t.device != q.device or (dtype is not None and t.dtype != dtype):
-            raise ValueError(f"a tensor of type {t.dtype} on {t.device}, with q {q.dtype} on {q.device}")
-        if shape == "state":
-            if t.shape != state or t.dtype != torch.float32 or not t.is_contiguous():
-                raise ValueError(f"states must be float32 {state}, contiguous")
-        elif shape is not None and tuple(t.shape) != shape:
-            raise ValueError(f"shape {tuple(t.shape)}, not {shape}")
+                                not lengths.is_contiguous() or lengths.device != dev):
+        raise ValueError("lengths must be int32 [B], contiguous, on the inputs' device")
     return B, H, Hk, T, d_k, d_v
+
+
+def _like(t, shape, dtype, device, name, contiguous=False):
+    if t is not None and (t.shape != shape or t.dtype != dtype or t.device != device or
+                          (contiguous and not t.is_contiguous())):
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, not "
+                         f"{'contiguous ' if contiguous else ''}{dtype} {tuple(shape)} on {device}")
 
 
 def _space(workspace, need, device):
@@ -147,7 +138,7 @@ def _space(workspace, need, device):
 
 def _token_major(B, heads, T, d, dtype, device):
     """[B, heads, T, d], laid out [B][T][heads][d] as projections read it."""
-    return torch.empty((B, T, heads, d), dtype=dtype, device=device).transpose(1, 2)
+    return torch.empty_strided((B, heads, T, d), (T * heads * d, d, heads * d, 1), dtype=dtype, device=device)
 
 
 def recurrence(q, k, v, g, *, scale: float = 1.0, state=None, lengths=None, out=None,
@@ -157,20 +148,24 @@ def recurrence(q, k, v, g, *, scale: float = 1.0, state=None, lengths=None, out=
     last axis of q, k and v contiguous and its rows 16-byte aligned.  state: [B, H, d_k,
     d_v] float32 or None; state_out may be the same tensor.  Returns (out, state_out); out
     is laid out [B][T][H][d_v] unless given."""
-    B, H, Hk, T, d_k, d_v = _checked(q, k, v, g, lengths,
-                                     [(state, "state", None), (state_out, "state", None),
-                                      (out, tuple(v.shape), q.dtype)])
+    B, H, Hk, T, d_k, d_v = _sizes(q, k, v, g, lengths)
+    dtype, dev, f32 = q.dtype, q.device, torch.float32
+    _like(state, (B, H, d_k, d_v), f32, dev, "state", True)
     if out is None:
-        out = _token_major(B, H, T, d_v, v.dtype, v.device)
-    if state_out is None and want_state:
-        state_out = torch.empty((B, H, d_k, d_v), dtype=torch.float32, device=v.device)
-    need = recurrence_workspace_bytes(B, H, Hk, T, d_k, d_v, q.dtype)
-    workspace, size = _space(workspace, need, q.device) if need else (None, 0)
-    desc = _rec_desc(B, H, Hk, T, d_k, d_v, q.dtype, scale, lengths)
+        out = _token_major(B, H, T, d_v, dtype, dev)
+    else:
+        _like(out, v.shape, dtype, dev, "out")
+    if state_out is not None:
+        _like(state_out, (B, H, d_k, d_v), f32, dev, "state_out", True)
+    elif want_state:
+        state_out = torch.empty((B, H, d_k, d_v), dtype=f32, device=dev)
+    need, size = recurrence_workspace_bytes(B, H, Hk, T, d_k, d_v, dtype), 0
+    if need:
+        workspace, size = _space(workspace, need, dev)
     _check(lib().dla_recurrence_forward(
-        ctypes.byref(desc), _rows(q, "q", d_k), _rows(k, "k", d_k), _rows(v, "v", d_v),
-        _rows(g, "g"), _ptr(state), _rows(out, "out", d_v), _ptr(state_out), _ptr(workspace), size,
-        _stream(q.device)), "dla_recurrence_forward")
+        _desc(B, H, Hk, T, d_k, d_v, dtype, scale, lengths), _rows(q, "q"), _rows(k, "k"), _rows(v, "v"),
+        _rows(g, "g"), _ptr(state), _rows(out, "out"), _ptr(state_out), _ptr(workspace) if need else None,
+        size, _stream(dev)), "dla_recurrence_forward")
     return out, state_out
 
 
@@ -179,56 +174,57 @@ def recurrence_backward(q, k, v, g, dout, *, scale: float = 1.0, state=None, dst
     """Gradients of `recurrence` (dla_recurrence_backward) from those of its outputs, dout
     and dstate (None: zero).  Returns dq, dk, dv, dg, all of the inputs' type, and the
     gradient of `state` (float32; None without one, unless want_dstate)."""
-    B, H, Hk, T, d_k, d_v = _checked(q, k, v, g, lengths,
-                                     [(state, "state", None), (dstate, "state", None),
-                                      (dout, tuple(v.shape), q.dtype)])
-    dq = _token_major(B, Hk, T, d_k, q.dtype, q.device)
-    dk = _token_major(B, Hk, T, d_k, q.dtype, q.device)
-    dv = _token_major(B, H, T, d_v, q.dtype, q.device)
-    dg = torch.empty((B, T, H), dtype=q.dtype, device=q.device).transpose(1, 2)
+    B, H, Hk, T, d_k, d_v = _sizes(q, k, v, g, lengths)
+    dtype, dev, f32 = q.dtype, q.device, torch.float32
+    _like(state, (B, H, d_k, d_v), f32, dev, "state", True)
+    _like(dstate, (B, H, d_k, d_v), f32, dev, "dstate", True)
+    _like(dout, v.shape, dtype, dev, "dout")
+    dq = _token_major(B, Hk, T, d_k, dtype, dev)
+    dk = _token_major(B, Hk, T, d_k, dtype, dev)
+    dv = _token_major(B, H, T, d_v, dtype, dev)
+    dg = torch.empty_strided((B, H, T), (T * H, 1, H), dtype=dtype, device=dev)
     ds0 = None
     if state is not None if want_dstate is None else want_dstate:
-        ds0 = torch.empty((B, H, d_k, d_v), dtype=torch.float32, device=q.device)
-    need = recurrence_workspace_bytes(B, H, Hk, T, d_k, d_v, q.dtype, backward=True)
-    workspace, size = _space(workspace, need, q.device) if need else (None, 0)
-    desc = _rec_desc(B, H, Hk, T, d_k, d_v, q.dtype, scale, lengths)
+        ds0 = torch.empty((B, H, d_k, d_v), dtype=f32, device=dev)
+    need, size = recurrence_workspace_bytes(B, H, Hk, T, d_k, d_v, dtype, backward=True), 0
+    if need:
+        workspace, size = _space(workspace, need, dev)
     _check(lib().dla_recurrence_backward(
-        ctypes.byref(desc), _rows(q, "q", d_k), _rows(k, "k", d_k), _rows(v, "v", d_v),
-        _rows(g, "g"), _ptr(state), _rows(dout, "dout", d_v), _ptr(dstate), _rows(dq, "dq", d_k),
-        _rows(dk, "dk", d_k), _rows(dv, "dv", d_v), _rows(dg, "dg"), _ptr(ds0), _ptr(workspace),
-        size, _stream(q.device)), "dla_recurrence_backward")
+        _desc(B, H, Hk, T, d_k, d_v, dtype, scale, lengths), _rows(q, "q"), _rows(k, "k"), _rows(v, "v"),
+        _rows(g, "g"), _ptr(state), _rows(dout, "dout"), _ptr(dstate), _rows(dq, "dq"), _rows(dk, "dk"),
+        _rows(dv, "dv"), _rows(dg, "dg"), _ptr(ds0), _ptr(workspace) if need else None, size,
+        _stream(dev)), "dla_recurrence_backward")
     return dq, dk, dv, dg, ds0
 
 
 # ---------------------------------------------------------------------------
 # norm
 # ---------------------------------------------------------------------------
-def _norm_rows(t, shape, dtype, device, name):
+def _norm_rows(t, like, name):
     if t is None:
         return None
-    if tuple(t.shape) != shape or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, not {dtype} {shape} on {device}")
-    if shape[1] > 1 and t.numel() and t.stride(1) != 1:
+    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, not {like.dtype} "
+                         f"{tuple(like.shape)} on {like.device}")
+    st = t.stride()
+    if st[1] != 1 and t.shape[1] > 1 and t.numel():
         raise ValueError(f"{name}: rows must be contiguous")
-    return ctypes.byref(NormRows(t.data_ptr(), t.stride(0)))
+    return _NORM_ROWS.pack(t.data_ptr(), st[0])
 
 
 def _norm_desc(x, weight, eps):
-    if x.dim() != 2 or weight.shape != (x.shape[1],) or not weight.is_contiguous() or \
-            weight.device != x.device:
+    if x.dim() != 2 or weight.shape != x.shape[1:] or not weight.is_contiguous() or weight.device != x.device:
         raise ValueError(f"shapes {tuple(x.shape)}, {tuple(weight.shape)}: rows [N, D] and a weight [D] are wanted")
-    return NormDesc(x.shape[0], x.shape[1], _dtype_code(x.dtype), _dtype_code(weight.dtype), float(eps))
+    return _NORM.pack(*x.shape, _dtype_code(x.dtype), _dtype_code(weight.dtype), eps)
 
 
 def _norm_forward(call, x, weight, residual, eps, y, last):
-    shape, dev = tuple(x.shape), x.device
-    h = torch.empty(shape, dtype=x.dtype, device=dev) if residual is not None else None
-    desc = _norm_desc(x, weight, eps)
+    desc, D = _norm_desc(x, weight, eps), x.shape[1]
+    rows = _norm_rows(x, x, "x"), _norm_rows(residual, x, "residual")
+    h = None if residual is None else torch.empty_like(residual, memory_format=torch.contiguous_format)
     _check(getattr(lib(), call)(
-        ctypes.byref(desc), _norm_rows(x, shape, x.dtype, dev, "x"),
-        _norm_rows(residual, shape, x.dtype, dev, "residual"), _ptr(weight),
-        _norm_rows(h, shape, x.dtype, dev, "h"), _norm_rows(y, shape, y.dtype, dev, "y"),
-        _ptr(last), _stream(dev)), call)
+        desc, *rows, weight.data_ptr(), None if h is None else _NORM_ROWS.pack(h.data_ptr(), D),
+        _NORM_ROWS.pack(y.data_ptr(), D), last.data_ptr(), _stream(x.device)), call)
     return x if h is None else h
 
 
@@ -248,30 +244,29 @@ def rms_norm_fp8(x, weight, residual=None, *, eps: float = 1e-6):
     return y, _norm_forward("dla_rms_norm_fp8", x, weight, residual, eps, y, scale), scale
 
 
+@functools.lru_cache(maxsize=4096)
 def rms_norm_workspace_bytes(rows: int, D: int, dtype=torch.bfloat16) -> int:
     """Workspace of rms_norm_backward for rows of D values."""
     n = ctypes.c_size_t(0)
     code = _dtype_code(dtype)
-    _check(lib().dla_rms_norm_workspace_size(ctypes.byref(NormDesc(rows, D, code, code, 0.0)),
-                                             ctypes.byref(n)), "dla_rms_norm_workspace_size")
+    _check(lib().dla_rms_norm_workspace_size(_NORM.pack(rows, D, code, code, 0.0), ctypes.byref(n)),
+           "dla_rms_norm_workspace_size")
     return int(n.value)
 
 
 def rms_norm_backward(dy, h, weight, rstd, dres=None, *, workspace=None):
     """Gradients of rms_norm from dy and dres, those of its outputs y and h (None: zero):
     (dx, which is also the residual's, and dweight in float32)."""
-    shape, dev, dt = tuple(h.shape), h.device, h.dtype
+    dev = h.device
     desc = _norm_desc(h, weight, 0.0)
-    if rstd.shape != shape[:1] or rstd.dtype != torch.float32 or not rstd.is_contiguous() or rstd.device != dev:
-        raise ValueError("rstd must be float32 [N], contiguous")
-    dx = torch.empty(shape, dtype=dt, device=dev)
-    dw = torch.empty(shape[1:], dtype=torch.float32, device=dev)
-    workspace, size = _space(workspace, rms_norm_workspace_bytes(*shape, dt), dev)
+    _like(rstd, h.shape[:1], torch.float32, dev, "rstd", True)
+    dx = torch.empty(h.shape, dtype=h.dtype, device=dev)
+    dw = torch.empty(h.shape[1:], dtype=torch.float32, device=dev)
+    workspace, size = _space(workspace, rms_norm_workspace_bytes(*h.shape, h.dtype), dev)
     _check(lib().dla_rms_norm_backward(
-        ctypes.byref(desc), _norm_rows(dy, shape, dt, dev, "dy"), _norm_rows(h, shape, dt, dev, "h"),
-        _ptr(weight), _ptr(rstd), _norm_rows(dres, shape, dt, dev, "dres"),
-        _norm_rows(dx, shape, dt, dev, "dx"), _ptr(dw), _ptr(workspace), size, _stream(dev)),
-        "dla_rms_norm_backward")
+        desc, _norm_rows(dy, h, "dy"), _norm_rows(h, h, "h"), weight.data_ptr(), rstd.data_ptr(),
+        _norm_rows(dres, h, "dres"), _norm_rows(dx, h, "dx"), dw.data_ptr(), workspace.data_ptr(), size,
+        _stream(dev)), "dla_rms_norm_backward")
     return dx, dw
 
 

@@ -9,8 +9,6 @@ are each rounded once, by 2^-8 at most and less than half of that in the mean ov
 elements, so 2^-8 holds for the three together; states add up products whose factors keep
 16 bits, 2^-16.
 """
-import ctypes
-
 import pytest
 import torch
 
@@ -346,10 +344,9 @@ def test_refusals():
         tr.recurrence(q, k, v.transpose(2, 3).contiguous().transpose(2, 3), g)          # last axis strided
     # a short or unaligned workspace
     L = tr.lib()
-    desc = tr._rec_desc(1, 2, 2, 40, 64, 64, torch.bfloat16)
     out = torch.empty_like(v)
-    args = [ctypes.byref(desc), tr._rows(q, "q", 64), tr._rows(k, "k", 64), tr._rows(v, "v", 64), tr._rows(g, "g"),
-            None, tr._rows(out, "out", 64), None]
+    args = [tr._desc(1, 2, 2, 40, 64, 64, torch.bfloat16), tr._rows(q, "q"), tr._rows(k, "k"), tr._rows(v, "v"),
+            tr._rows(g, "g"), None, tr._rows(out, "out"), None]
     need = tr.recurrence_workspace_bytes(1, 2, 2, 40, 64, 64, torch.bfloat16)
     ws = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
     for p, n in ((None, need), (ws.data_ptr(), need - 1), (ws.data_ptr() + 64, need)):
