@@ -24,24 +24,28 @@ struct Plan {
 };
 
 // Segments of a pass: with fewer heads than the chip holds workgroups, sequences are cut
-// so that all of them work, at the price of reading keys and values (queries and output
-// gradients) once more for the segments' states.
+// so that all of them work, at the price of a pass over keys and values (backward also over
+// queries and output gradients) for the segments' states.  As many as the chip then holds
+// at once; not where that makes but two or three, which costs what it gives.  2048 bfloat16
+// tokens, forward and backward, 128 x 128: 96 heads in 1, 4, 5, 6 segments 561, 391, 361, 441
+// us, 150 in 1, 3, 4 584, 544, 634, 192 in 1, 2 594, 717; 64 x 64 (half the threads per
+// workgroup): 96 in 5, 8, 11 217, 184, 205, 192 in 1, 5, 8 484, 304, 360, 300 in 1, 3 621,
+// 492.  A segment has at least 4 chunks, 2 of float32, whose chunks take longer (15 heads x
+// 1531 tokens: 161 us, 175 with 4, 274 with 8).
 Plan plan_of(const dla_recurrence_desc& d, bool backward) {
   Plan p{!backward && d.T <= kStepTokens, 1, kRecChunk};
   if (d.B == 0 || d.T == 0) return p;   // nothing to plan
-  const int chunk = kRecChunk, heads = d.B * d.H;
-  const int chunks = (d.T + chunk - 1) / chunk;
-  int n = 1;
-  if (heads < 256) {
-    n = (512 + heads - 1) / heads;
-    if (n > chunks / 8) n = chunks / 8;
-    if (n > 64) n = 64;
-    if (n < 1) n = 1;
-  }
+  const int heads = d.B * d.H, chunks = (d.T + kRecChunk - 1) / kRecChunk;
+  const int narrow = (d.d_k == 64) + (d.d_v == 64);
+  const int most = chunks / (d.dtype == DLA_BF16 ? 4 : 2);
+  int n = (512 + 256 * narrow) / heads;
+  if (n < (narrow == 2 ? 3 : 4)) n = 1;
+  if (n > 64) n = 64;
+  if (n > most) n = most > 0 ? most : 1;
   // float32: at most 1024 tokens, so that dg's sums keep float32's precision
   if (backward && d.dtype == DLA_F32 && n < (d.T + 1023) / 1024) n = (d.T + 1023) / 1024;
   const int per = (chunks + n - 1) / n;
-  p.seg_len = per * chunk;
+  p.seg_len = per * kRecChunk;
   p.nseg = (chunks + per - 1) / per;
   return p;
 }
