@@ -67,7 +67,7 @@ template <typename Tin, int R, int C, bool PAIR>
 struct ScanTiles {
   Tin q[Tile<Tin, R>::SIZE], k[Tile<Tin, R>::SIZE], v[Tile<Tin, C>::SIZE], y[PAIR ? Tile<Tin, C>::SIZE : 8];
   Decays dec;
-  float dots[PAIR ? C / 32 : 1][kChunk];
+  float dots[2][PAIR ? C / 32 : 1][kChunk];   // of the chunk at hand and the one before
 };
 
 // REV: from the segment's last chunk to its first.
@@ -81,66 +81,80 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
   const int b = head / a.H, h = head % a.H, c0 = 32 * wave;
   const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
   const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
-  const Tin* q = row_base<const Tin>(f.q, b, h);
-  const Tin* k = row_base<const Tin>(f.k, b, h);
-  const Tin* v = row_base<const Tin>(f.v, b, h);
-  const Tin* y = PAIR ? row_base<const Tin>(f.y, b, h) : nullptr;
+  const int n = (end - begin + kChunk - 1) / kChunk;
+  const int t_first = REV ? begin + (n - 1) * kChunk : begin;
+  constexpr int STEP = REV ? -kChunk : kChunk;
   const int64_t D = (int64_t)R * C, padded = rec_padded(a.T);
-  const float2* decays = a.decays + 2 * head * padded;
+  // the addresses of the next chunk to load, and of the next one's outputs
+  const Tin* q = row_base<const Tin>(f.q, b, h) + t_first * f.q.st;
+  const Tin* k = row_base<const Tin>(f.k, b, h) + t_first * f.k.st;
+  const Tin* v = row_base<const Tin>(f.v, b, h) + t_first * f.v.st;
+  const Tin* y = PAIR ? row_base<const Tin>(f.y, b, h) + t_first * f.y.st : nullptr;
+  const float2* decays = a.decays + 2 * head * padded + t_first;
+  char* out = static_cast<char*>(f.out.p) +
+              (b * f.out.sb + (h / f.out.hdiv) * f.out.sh + t_first * f.out.st) * (PAIR && f.out_f32 ? 4 : sizeof(Tin));
+  float* dot_out = PAIR ? f.dot + (int64_t)head * a.T : nullptr;
 
   Stage<Tin, R, NT> gq, gk;
   Stage<Tin, C, NT> gv, gy;
   DecayStage<NT, REV> gd;
   auto request = [&](int t0) {
-    gq.load(q + t0 * f.q.st, f.q.st, lim - t0, tid);
-    gk.load(k + t0 * f.k.st, f.k.st, lim - t0, tid);
-    gv.load(v + t0 * f.v.st, f.v.st, lim - t0, tid);
-    if constexpr (PAIR) gy.load(y + t0 * f.y.st, f.y.st, lim - t0, tid);
-    gd.load(decays, padded, t0, tid);
+    gq.load(q, f.q.st, lim - t0, tid);
+    gk.load(k, f.k.st, lim - t0, tid);
+    gv.load(v, f.v.st, lim - t0, tid);
+    if constexpr (PAIR) gy.load(y, f.y.st, lim - t0, tid);
+    gd.load(decays, padded, tid);
+    q += STEP * f.q.st;
+    k += STEP * f.k.st;
+    v += STEP * f.v.st;
+    if constexpr (PAIR) y += STEP * f.y.st;
+    decays += STEP;
   };
-  // the waves' parts of a chunk's dots, added up when the next one's tokens are staged
-  auto sum_dots = [&](int t0) {
+  // a chunk's dots, the sum of the waves' parts
+  auto sum_dots = [&](int which, int t0) {
     if (tid < kChunk && t0 + tid < end) {
       float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) x += now.dots[w][tid];
-      f.dot[(int64_t)head * a.T + t0 + tid] = t0 + tid < lim ? x : 0.f;
+      for (int w = 0; w < NW; ++w) x += now.dots[which][w][tid];
+      dot_out[t0 + tid] = t0 + tid < lim ? x : 0.f;
     }
   };
-  const int n = (end - begin + kChunk - 1) / kChunk;
-  auto chunk_at = [&](int c) { return begin + (REV ? n - 1 - c : c) * kChunk; };
-  request(chunk_at(0));
+  request(t_first);
   State<R / 32> S;
   const float* first = f.seg_first ? f.seg_first + ((int64_t)head * a.nseg + seg) * D
                                    : (f.first ? f.first + head * D : nullptr);
   if (first) load_state(S.s, first, f.s_rs, f.s_cs, c0, lane);
   else S.clear();
-  for (int c = 0; c < n; ++c) {
-    const int t0 = chunk_at(c);
+  int t0 = t_first;
+  for (int c = 0; c < n; ++c, t0 += STEP) {
+    gd.form(a.scale, tid);
     __syncthreads();   // the last chunk's tiles are read, its dots written
-    if constexpr (PAIR) {
-      if (c > 0) sum_dots(chunk_at(c - 1));
-    }
     gq.store(now.q, tid);
     gk.store(now.k, tid);
     gv.store(now.v, tid);
     if constexpr (PAIR) gy.store(now.y, tid);
-    gd.store(now.dec, a.scale, tid);
+    gd.store(now.dec, tid);
     __syncthreads();
-    if (c + 1 < n) request(chunk_at(c + 1));
+    if (c + 1 < n) request(t0 + STEP);
+    if constexpr (PAIR) {
+      if (c > 0) sum_dots((c - 1) & 1, t0 - STEP);
+    }
     f32x16 o;
     const float dot = chunk_step<Tin, R, C, REV, PAIR>(now.q, now.k, now.v, now.y, now.dec, a.scale, c0, lane, S, o);
     if constexpr (PAIR) {
-      if (lane < 32) now.dots[wave][lane] = dot;
+      if (lane < 32) now.dots[c & 1][wave][lane] = dot;
     }
-    if (PAIR && f.out_f32)
-      store_out(row_base<float>(f.out, b, h) + t0 * f.out.st, f.out.st, c0, o, lim - t0, end - t0, lane);
-    else
-      store_out(row_base<Tin>(f.out, b, h) + t0 * f.out.st, f.out.st, c0, o, lim - t0, end - t0, lane);
+    if (PAIR && f.out_f32) {
+      store_out(reinterpret_cast<float*>(out), f.out.st, c0, o, lim - t0, end - t0, lane);
+      out += STEP * f.out.st * 4;
+    } else {
+      store_out(reinterpret_cast<Tin*>(out), f.out.st, c0, o, lim - t0, end - t0, lane);
+      out += STEP * f.out.st * (int)sizeof(Tin);
+    }
   }
   if constexpr (PAIR) {
     __syncthreads();
-    sum_dots(chunk_at(n - 1));
+    sum_dots((n - 1) & 1, t0 - STEP);
   }
   if (seg == (REV ? 0 : a.nseg - 1)) {
     S.apply();
@@ -157,15 +171,141 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
         __syncthreads();
-        if (lane == 0) now.dots[wave][0] = x;
+        if (lane == 0) now.dots[0][wave][0] = x;
         __syncthreads();
         if (tid == 0) {
           float z = 0.f;
-          for (int w = 0; w < NW; ++w) z += now.dots[w][0];
+          for (int w = 0; w < NW; ++w) z += now.dots[0][w][0];
           f.end_dot[head] = z;
         }
       }
     }
+  }
+}
+
+// dk and dv at once: half of the waves hold the adjoint's columns and give dv, the others
+// those of its transpose and give dk, from the same tiles.  A chunk's tokens are read once
+// for both, and its next one is stored into the other set of tiles meanwhile.
+template <typename Tin, int DK, int DV>
+struct AdjointTiles {
+  Tin q[Tile<Tin, DK>::SIZE], k[Tile<Tin, DK>::SIZE], v[Tile<Tin, DV>::SIZE], o[Tile<Tin, DV>::SIZE];
+  Decays dec;
+  float dots[DK / 32][kChunk];
+};
+
+struct AdjointArgs {
+  RecArgs a;
+  Rows q, k, v, dout, dk, dv;
+  const float* dstate;
+  float* ds0;
+  float* kdot;
+  int dk_f32;
+};
+
+template <typename Tin, int DK, int DV>
+__global__ __launch_bounds__(2 * (DK + DV), 2) void adjoint_kernel(AdjointArgs f) {
+  constexpr int NT = 2 * (DK + DV), KW = DK / 32, VW = DV / 32;
+  __shared__ __align__(16) AdjointTiles<Tin, DK, DV> tiles[2];
+  const RecArgs& a = f.a;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = blockIdx.x % (a.B * a.H), seg = blockIdx.x / (a.B * a.H);
+  const int b = head / a.H, h = head % a.H;
+  const int lim = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int begin = seg * a.seg_len, end = min(a.T, begin + a.seg_len);
+  const int t_last = begin + (end - begin - 1) / kChunk * kChunk;
+  const int64_t D = (int64_t)DK * DV, padded = rec_padded(a.T);
+  const Tin* q = row_base<const Tin>(f.q, b, h) + t_last * f.q.st;
+  const Tin* k = row_base<const Tin>(f.k, b, h) + t_last * f.k.st;
+  const Tin* v = row_base<const Tin>(f.v, b, h) + t_last * f.v.st;
+  const Tin* o = row_base<const Tin>(f.dout, b, h) + t_last * f.dout.st;
+  const float2* decays = a.decays + 2 * head * padded + t_last;
+  Stage<Tin, DK, NT> gq, gk;
+  Stage<Tin, DV, NT> gv, go;
+  DecayStage<NT, true> gd;
+  auto request = [&](int t0) {
+    gq.load(q, f.q.st, lim - t0, tid);
+    gk.load(k, f.k.st, lim - t0, tid);
+    gv.load(v, f.v.st, lim - t0, tid);
+    go.load(o, f.dout.st, lim - t0, tid);
+    gd.load(decays, padded, tid);
+    q -= kChunk * f.q.st;
+    k -= kChunk * f.k.st;
+    v -= kChunk * f.v.st;
+    o -= kChunk * f.dout.st;
+    decays -= kChunk;
+  };
+  auto store = [&](AdjointTiles<Tin, DK, DV>& to) {
+    gq.store(to.q, tid);
+    gk.store(to.k, tid);
+    gv.store(to.v, tid);
+    go.store(to.o, tid);
+    gd.form(a.scale, tid);
+    gd.store(to.dec, tid);
+  };
+  const float* last = a.nseg > 1 ? a.seg_adj + ((int64_t)head * a.nseg + seg) * D
+                                 : (f.dstate ? f.dstate + head * D : nullptr);
+  request(t_last);
+  int at = 0;
+  if (wave < VW) {
+    const int c0 = 32 * wave;
+    State<DK / 32> R;
+    if (last) load_state(R.s, last, DV, 1, c0, lane);
+    else R.clear();
+    store(tiles[0]);
+    __syncthreads();
+    Tin* out = row_base<Tin>(f.dv, b, h) + t_last * f.dv.st;
+    for (int t0 = t_last; t0 >= begin; t0 -= kChunk, at ^= 1) {
+      const AdjointTiles<Tin, DK, DV>& now = tiles[at];
+      if (t0 > begin) request(t0 - kChunk);
+      f32x16 x;
+      chunk_step<Tin, DK, DV, true, false>(now.k, now.q, now.o, nullptr, now.dec, a.scale, c0, lane, R, x);
+      store_out(out, f.dv.st, c0, x, lim - t0, end - t0, lane);
+      out -= kChunk * f.dv.st;
+      if (t0 > begin) store(tiles[at ^ 1]);
+      __syncthreads();
+    }
+    // dk's waves have read dstate before the first barrier: ds0 may be its array
+    if (seg == 0 && f.ds0) {
+      R.apply();
+      store_state(R.s, f.ds0 + head * D, DV, 1, c0, lane);
+    }
+  } else {
+    const int c0 = 32 * (wave - VW);
+    State<DV / 32> R;
+    if (last) load_state(R.s, last, 1, DV, c0, lane);
+    else R.clear();
+    float* dot_out = f.kdot + (int64_t)head * a.T;
+    auto sum_dots = [&](const AdjointTiles<Tin, DK, DV>& from, int t0) {
+      if (c0 == 0 && lane < kChunk && t0 + lane < end) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < KW; ++i) x += from.dots[i][lane];
+        dot_out[t0 + lane] = t0 + lane < lim ? x : 0.f;
+      }
+    };
+    store(tiles[0]);
+    __syncthreads();
+    char* out = static_cast<char*>(f.dk.p) +
+                (b * f.dk.sb + (h / f.dk.hdiv) * f.dk.sh + t_last * f.dk.st) * (f.dk_f32 ? 4 : sizeof(Tin));
+    for (int t0 = t_last; t0 >= begin; t0 -= kChunk, at ^= 1) {
+      AdjointTiles<Tin, DK, DV>& now = tiles[at];
+      if (t0 > begin) request(t0 - kChunk);
+      if (t0 < t_last) sum_dots(tiles[at ^ 1], t0 + kChunk);
+      f32x16 x;
+      const float dot = chunk_step<Tin, DV, DK, true, true>(now.v, now.o, now.q, now.k, now.dec, a.scale, c0, lane, R, x);
+      if (lane < 32) now.dots[c0 / 32][lane] = dot;
+      if (f.dk_f32) {
+        store_out(reinterpret_cast<float*>(out), f.dk.st, c0, x, lim - t0, end - t0, lane);
+        out -= kChunk * f.dk.st * 4;
+      } else {
+        store_out(reinterpret_cast<Tin*>(out), f.dk.st, c0, x, lim - t0, end - t0, lane);
+        out -= kChunk * f.dk.st * (int)sizeof(Tin);
+      }
+      if (t0 > begin) store(tiles[at ^ 1]);
+      __syncthreads();
+    }
+    sum_dots(tiles[at ^ 1], begin);
   }
 }
 
@@ -355,6 +495,15 @@ hipError_t launch_recurrence_adjoint(const RecArgs& a, int dtype, const Rows& q,
                                      const Rows& v, const Rows& dout, const Rows& dk, bool dk_f32,
                                      const Rows& dv, const float* dstate, float* ds0, float* kdot,
                                      hipStream_t st) {
+  if (dtype == DLA_BF16) {
+    const AdjointArgs f{a, q, k, v, dout, dk, dv, dstate, ds0, kdot, dk_f32 ? 1 : 0};
+    const dim3 grid(a.B * a.H * a.nseg), block(2 * (a.dk + a.dv));
+    if (a.dk == 128 && a.dv == 128) hipLaunchKernelGGL((adjoint_kernel<bf16_t, 128, 128>), grid, block, 0, st, f);
+    else if (a.dk == 128) hipLaunchKernelGGL((adjoint_kernel<bf16_t, 128, 64>), grid, block, 0, st, f);
+    else if (a.dv == 128) hipLaunchKernelGGL((adjoint_kernel<bf16_t, 64, 128>), grid, block, 0, st, f);
+    else hipLaunchKernelGGL((adjoint_kernel<bf16_t, 64, 64>), grid, block, 0, st, f);
+    return hipGetLastError();
+  }
   // dk before dv, so that ds0, which the latter writes, may be dstate's array
   ScanArgs f{};
   f.a = a;

@@ -132,35 +132,45 @@ struct Decays {
   __device__ __forceinline__ float total() const { return in[kChunk - 1]; }   // e^{a_end}
 };
 
+// On its way from memory: load, then, before the barrier behind which tiles may be
+// overwritten, form, then store.
 template <int NT, bool REV>
 struct DecayStage {
-  static constexpr int M = kChunk * kChunk / NT, G = kChunk / M;   // M consecutive s per thread
+  static constexpr int M = NT >= 256 ? 4 : kChunk * kChunk / NT;   // consecutive s per thread
+  static constexpr int G = kChunk / M, ALL = kChunk * G;           // of the first ALL threads
   float2 io, t, s[M];
-  __device__ __forceinline__ void load(const float2* head, int64_t padded, int t0, int tid) {
-    if (tid < kChunk) io = head[padded + t0 + tid];
-    t = head[t0 + tid / G];
+  float x[M];
+  // chunk: the first token's hi and lo; its in and out are `padded` behind
+  __device__ __forceinline__ void load(const float2* chunk, int64_t padded, int tid) {
+    if (tid < kChunk) io = chunk[padded + tid];
+    if (NT > ALL && tid >= ALL) return;
+    t = chunk[tid / G];
 #pragma unroll
     for (int i = 0; i < M; i += 2) {
-      const float4 x = *reinterpret_cast<const float4*>(head + t0 + (tid % G) * M + i);
-      s[i] = make_float2(x.x, x.y);
-      s[i + 1] = make_float2(x.z, x.w);
+      const float4 y = *reinterpret_cast<const float4*>(chunk + (tid % G) * M + i);
+      s[i] = make_float2(y.x, y.y);
+      s[i + 1] = make_float2(y.z, y.w);
     }
   }
-  __device__ __forceinline__ void store(Decays& d, float scale, int tid) const {
-    if (tid < kChunk) {
-      d.in[tid] = io.x;
-      d.out[tid] = io.y;
-    }
+  __device__ __forceinline__ void form(float scale, int tid) {
+    if (NT > ALL && tid >= ALL) return;
     const int tt = tid / G, s0 = (tid % G) * M;
-    float x[M];
 #pragma unroll
     for (int i = 0; i < M; ++i) {
       const float y = REV ? decay2(s[i].x, s[i].y, t.x, t.y) : decay2(t.x, t.y, s[i].x, s[i].y);
       x[i] = (REV ? s0 + i >= tt : s0 + i <= tt) ? y * scale : 0.f;
     }
+  }
+  __device__ __forceinline__ void store(Decays& d, int tid) const {
+    if (tid < kChunk) {
+      d.in[tid] = io.x;
+      d.out[tid] = io.y;
+    }
+    if (NT > ALL && tid >= ALL) return;
 #pragma unroll
     for (int i = 0; i < M; i += 4)
-      *reinterpret_cast<float4*>(d.pair + tt * Decays::LD + s0 + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+      *reinterpret_cast<float4*>(d.pair + tid / G * Decays::LD + (tid % G) * M + i) =
+          make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
   }
 };
 
