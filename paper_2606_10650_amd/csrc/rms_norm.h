@@ -19,12 +19,12 @@ struct NormArgs {
   NormRows x, res, h, y;
   float* rstd;
   float* y_scale;
-  float* dw_part;   // [slots][D]
-  int slots;
+  float* dw_part;   // [groups][D]
+  int groups;
 };
 
 int norm_threads(int64_t rows, int pieces);
-int norm_slots(int64_t rows, int pieces);
+int norm_groups(int64_t rows, int pieces);
 // kind 0: forward; 1: forward with 8-bit output; 2: backward
 hipError_t launch_norm(const NormArgs& a, int dtype, int kind, hipStream_t st);
 hipError_t launch_norm_dw(const NormArgs& a, float* dw, hipStream_t st);

@@ -20,18 +20,29 @@ struct Piece {
   struct __attribute__((packed, aligned(sizeof(T)))) Raw {
     uint32_t w[4];
   };
-  __device__ static __forceinline__ void load(const T* p, int n, float (&x)[N]) {
-    if (n >= N) {
-      const Raw r = *reinterpret_cast<const Raw*>(p);
+  // a piece as it lies, zero from element n on
+  __device__ static __forceinline__ Raw raw(const T* p, int n) {
+    if (n >= N) return *reinterpret_cast<const Raw*>(p);
+    Raw r;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if constexpr (sizeof(T) == 2) x[i] = __uint_as_float(i & 1 ? r.w[i >> 1] & 0xFFFF0000u : r.w[i >> 1] << 16);
-        else x[i] = __uint_as_float(r.w[i]);
+    for (int i = 0; i < 4; ++i) r.w[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (i < n) {
+        if constexpr (sizeof(T) == 2) r.w[i >> 1] |= (uint32_t)p[i].x << (16 * (i & 1));
+        else r.w[i] = __float_as_uint(p[i]);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = i < n ? to_f32(p[i]) : 0.f;
     }
+    return r;
+  }
+  __device__ static __forceinline__ float value(const Raw& r, int i) {
+    if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? r.w[i >> 1] & 0xFFFF0000u : r.w[i >> 1] << 16);
+    else return __uint_as_float(r.w[i]);
+  }
+  __device__ static __forceinline__ void load(const T* p, int n, float (&x)[N]) {
+    const Raw r = raw(p, n);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = value(r, i);
   }
   __device__ static __forceinline__ void store(T* p, int n, const float (&x)[N]) {
     if constexpr (sizeof(T) == 2) {
@@ -180,83 +191,115 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void norm_kernel(NormArgs a) {
   }
 }
 
-// dx = (dn - n mean(dn n)) / rms + dres with n = h / rms and dn = dy w; dw = sum of dy n
-template <typename T, int NT, int NP>
+// dx = (dn - n mean(dn n)) / rms + dres with n = h / rms and dn = dy w; dw = sum of dy n.
+// A row's pieces stay as they were loaded (half the registers of their values, and twice the
+// waves that have loads under way); dy w and h / rms are formed where they are used.
+template <typename T, int NT, int NP, bool WF32>
 __global__ __launch_bounds__(NT > 256 ? NT : 256) void norm_backward_kernel(NormArgs a) {
   constexpr int N = Piece<T>::N, PER = NT > 256 ? 1 : 256 / NT;
+  using Raw = typename Piece<T>::Raw;
   __shared__ float lds[NT / 64];
-  const int tid = threadIdx.x % NT, slot = blockIdx.x * PER + threadIdx.x / NT;
-  const int slots = gridDim.x * PER;
-  float w[NP][N], dw[NP][N];
+  __shared__ float sums[PER > 1 ? PER - 1 : 1][PER > 1 ? NT * N : 1];
+  const int tid = threadIdx.x % NT, sub = threadIdx.x / NT;
+  const int64_t step = (int64_t)gridDim.x * PER;
+  Raw w[WF32 ? 1 : NP];
+  float wf[WF32 ? NP : 1][N], dw[NP][N];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     const int c = (i * NT + tid) * N, n = a.D - c;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      dw[i][j] = 0.f;
-      w[i][j] = 0.f;
+    for (int j = 0; j < N; ++j) dw[i][j] = 0.f;
+    if constexpr (WF32) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) wf[i][j] = 0.f;
+      if (n > 0) load_weight<T>(a, c, n, wf[i]);
+    } else {
+      w[i] = Piece<T>::raw(static_cast<const T*>(a.w) + c, n > 0 ? n : 0);
     }
-    if (n > 0) load_weight<T>(a, c, n, w[i]);
   }
-  // slots is a whole number of workgroups' rows, so a workgroup's waves end together
-  for (int64_t row = slot; row < a.rows; row += slots) {
+  auto weight = [&](int i, int j) {
+    if constexpr (WF32) return wf[i][j];
+    else return Piece<T>::value(w[i], j);
+  };
+  // a workgroup's waves that share a row end together
+  for (int64_t row = (int64_t)blockIdx.x * PER + sub; row < a.rows; row += step) {
     const float rstd = a.rstd[row];
-    float dy[NP][N], n_[NP][N], sum = 0.f;
+    Raw dy[NP], h[NP], r[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int c = (i * NT + tid) * N, n = a.D - c;
+      const int c = (i * NT + tid) * N, n = a.D - c > 0 ? a.D - c : 0;
+      dy[i] = Piece<T>::raw(static_cast<const T*>(a.y.p) + row * a.y.st + c, n);
+      h[i] = Piece<T>::raw(static_cast<const T*>(a.h.p) + row * a.h.st + c, n);
+      r[i] = Piece<T>::raw(static_cast<const T*>(a.res.p) + row * a.res.st + c, a.res.p ? n : 0);
+    }
+    float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < N; ++j) dy[i][j] = n_[i][j] = 0.f;
-      if (n > 0) {
-        Piece<T>::load(static_cast<const T*>(a.y.p) + row * a.y.st + c, n, dy[i]);
-        Piece<T>::load(static_cast<const T*>(a.h.p) + row * a.h.st + c, n, n_[i]);
-      }
+    for (int i = 0; i < NP; ++i)
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        n_[i][j] *= rstd;
-        dw[i][j] += dy[i][j] * n_[i][j];
-        dy[i][j] *= w[i][j];
-        sum += dy[i][j] * n_[i][j];
+        const float x = Piece<T>::value(dy[i], j) * (Piece<T>::value(h[i], j) * rstd);
+        dw[i][j] += x;
+        sum += x * weight(i, j);
       }
-    }
     const float mean = over_row<NT, false>(sum, lds) / (float)a.D;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int c = (i * NT + tid) * N, n = a.D - c;
-      if (n > 0) {
-        float r[N];
+      float x[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) r[j] = 0.f;
-        if (a.res.p) Piece<T>::load(static_cast<const T*>(a.res.p) + row * a.res.st + c, n, r);
-#pragma unroll
-        for (int j = 0; j < N; ++j) r[j] += (dy[i][j] - n_[i][j] * mean) * rstd;
-        Piece<T>::store(static_cast<T*>(a.x.p) + row * a.x.st + c, n, r);
-      }
+      for (int j = 0; j < N; ++j)
+        x[j] = Piece<T>::value(r[i], j) +
+               (Piece<T>::value(dy[i], j) * weight(i, j) - Piece<T>::value(h[i], j) * rstd * mean) * rstd;
+      if (n > 0) Piece<T>::store(static_cast<T*>(a.x.p) + row * a.x.st + c, n, x);
     }
   }
   if (!a.dw_part) return;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
+    // the workgroup's rows one after the other into one sum
+    if constexpr (PER > 1) {
+      __syncthreads();
+      if (sub > 0) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) sums[sub - 1][j * NT + tid] = dw[i][j];
+      }
+      __syncthreads();
+      if (sub == 0) {
+#pragma unroll
+        for (int k = 0; k < PER - 1; ++k)
+#pragma unroll
+          for (int j = 0; j < N; ++j) dw[i][j] += sums[k][j * NT + tid];
+      }
+    }
     const int c = (i * NT + tid) * N;
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (c + j < a.D) a.dw_part[(int64_t)slot * a.D + c + j] = dw[i][j];
+      if (sub == 0 && c + j < a.D) a.dw_part[(int64_t)blockIdx.x * a.D + c + j] = dw[i][j];
   }
 }
 
-// dw[c] = sum over the slots' parts, 16 rows of 64 columns a workgroup
-__global__ __launch_bounds__(1024) void dw_kernel(const float* part, int slots, int D, float* dw) {
-  __shared__ float sums[16][64];
-  const int col = threadIdx.x & 63, r = threadIdx.x >> 6, c = blockIdx.x * 64 + col;
+// dw[c] = sum over the workgroups' parts: 32 columns a workgroup, 32 threads to a column,
+// eight loads under way in each
+__global__ __launch_bounds__(1024) void dw_kernel(const float* part, int parts, int D, float* dw) {
+  __shared__ float sums[32][33];
+  const int col = threadIdx.x & 31, r = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
   float s = 0.f;
-  if (c < D)
-    for (int i = r; i < slots; i += 16) s += part[(int64_t)i * D + c];
+  if (c < D) {
+    int i = r;
+    for (; i + 224 < parts; i += 256) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = part[(int64_t)(i + 32 * j) * D + c];
+      s += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    }
+    for (; i < parts; i += 32) s += part[(int64_t)i * D + c];
+  }
   sums[r][col] = s;
   __syncthreads();
   if (r == 0 && c < D) {
     float x = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x += sums[i][col];
+    for (int i = 0; i < 32; ++i) x += sums[i][col];
     dw[c] = x;
   }
 }
@@ -267,7 +310,8 @@ hipError_t go(const NormArgs& a, int kind, hipStream_t st) {
   const dim3 grid((unsigned)((a.rows + PER - 1) / PER)), block(BLOCK);
   if (kind == 0) hipLaunchKernelGGL((norm_kernel<T, NT, NP, false>), grid, block, 0, st, a);
   else if (kind == 1) hipLaunchKernelGGL((norm_kernel<T, NT, NP, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((norm_backward_kernel<T, NT, NP>), dim3(a.slots / PER), block, 0, st, a);
+  else if (sizeof(T) == 2 && !a.w_f32) hipLaunchKernelGGL((norm_backward_kernel<T, NT, NP, false>), dim3(a.groups), block, 0, st, a);
+  else hipLaunchKernelGGL((norm_backward_kernel<T, NT, NP, true>), dim3(a.groups), block, 0, st, a);
   return hipGetLastError();
 }
 
@@ -299,11 +343,12 @@ int norm_threads(int64_t rows, int pieces) {
   return pieces <= 2048 ? 256 : 1024;
 }
 
-// Rows that the backward pass works on at a time, each leaving one partial dw.
-int norm_slots(int64_t rows, int pieces) {
+// Workgroups of the backward pass, each leaving one part of dw: four a compute unit, where
+// there are rows for them.
+int norm_groups(int64_t rows, int pieces) {
   const int nt = norm_threads(rows, pieces), per = nt > 256 ? 1 : 256 / nt;
   const int64_t groups = (rows + per - 1) / per;
-  return (int)(groups < 512 ? groups : 512) * per;
+  return (int)(groups < 1024 ? groups : 1024);
 }
 
 hipError_t launch_norm(const NormArgs& a, int dtype, int kind, hipStream_t st) {
@@ -311,7 +356,7 @@ hipError_t launch_norm(const NormArgs& a, int dtype, int kind, hipStream_t st) {
 }
 
 hipError_t launch_norm_dw(const NormArgs& a, float* dw, hipStream_t st) {
-  hipLaunchKernelGGL(dw_kernel, dim3((a.D + 63) / 64), dim3(1024), 0, st, a.dw_part, a.slots, a.D, dw);
+  hipLaunchKernelGGL(dw_kernel, dim3((a.D + 31) / 32), dim3(1024), 0, st, a.dw_part, a.groups, a.D, dw);
   return hipGetLastError();
 }
 

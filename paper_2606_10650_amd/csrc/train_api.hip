@@ -181,7 +181,7 @@ NormArgs norm_args(const dla_norm_desc& d, const void* weight) {
   a.w = weight;
   a.w_f32 = d.weight_dtype == DLA_F32;
   a.rstd = a.y_scale = a.dw_part = nullptr;
-  a.slots = 0;
+  a.groups = 0;
   return a;
 }
 
@@ -335,7 +335,7 @@ dla_status dla_rms_norm_workspace_size(const dla_norm_desc* desc, size_t* bytes)
   const dla_status s = check(desc);
   if (s != DLA_OK) return remember(s);
   if (!bytes) return remember(DLA_ERR_INVALID_ARG);
-  *bytes = desc->rows ? (size_t)norm_slots(desc->rows, norm_pieces(*desc)) * desc->D * 4 : 0;
+  *bytes = desc->rows ? (size_t)norm_groups(desc->rows, norm_pieces(*desc)) * desc->D * 4 : 0;
   return remember(DLA_OK);
 }
 
@@ -355,14 +355,14 @@ dla_status dla_rms_norm_backward(const dla_norm_desc* desc, const dla_norm_rows*
     if (!rows_ok(dy, d, e) || !rows_ok(h, d, e) || !rows_ok(dx, d, e) || (dres && !rows_ok(dres, d, e)))
       return remember(DLA_ERR_INVALID_ARG);
     if (!rstd || ((uintptr_t)rstd & 3)) return remember(DLA_ERR_INVALID_ARG);
-    a.slots = norm_slots(d.rows, norm_pieces(d));
+    a.groups = norm_groups(d.rows, norm_pieces(d));
     a.y = norm_rows(dy);
     a.h = norm_rows(h);
     a.res = norm_rows(dres);
     a.x = norm_rows(dx);
     a.rstd = const_cast<float*>(rstd);
     if (dweight) {
-      if (!workspace_ok(workspace, workspace_bytes, (size_t)a.slots * d.D * 4)) return remember(DLA_ERR_WORKSPACE);
+      if (!workspace_ok(workspace, workspace_bytes, (size_t)a.groups * d.D * 4)) return remember(DLA_ERR_WORKSPACE);
       a.dw_part = (float*)workspace;
     }
   }
