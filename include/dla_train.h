@@ -27,8 +27,9 @@ extern "C" {
  * projection's output are all rows.  Token rows start at multiples of 16 bytes:
  * data and every stride whose dimension is larger than 1.  Gates are rows of
  * d = 1 and need no alignment beyond their type's.  0 <= stride_t < 2^26.  Inputs may
- * repeat rows (strides of zero); output rows are at least d apart in every
- * dimension larger than 1, and overlap no input.
+ * repeat rows (strides of zero); output rows do not overlap (each stride, of
+ * dimensions larger than 1, is at least what d and the smaller strides span), nor
+ * any input.
  */
 typedef struct {
   void* data;

@@ -96,17 +96,24 @@ dla_status check(const dla_recurrence_desc* d) {
 }
 
 // Rows of `width` values of a call's tensor: there, aligned to 16 bytes (rows of one value:
-// to their type), with a token stride that 32 rows of it keep within 32 bits; of an output
-// also apart from each other.
+// to their type), with a token stride that 32 rows of it keep within 32 bits; an output's
+// also apart from each other, each stride no smaller than what the smaller ones span.
 bool rows_ok(const dla_rows* r, const dla_recurrence_desc& d, int heads, int width, int elem, bool output) {
   if (!r || !r->data) return false;
   const int align = width > 1 ? 16 : elem;
   if ((uintptr_t)r->data % align) return false;
   const int64_t st[3] = {r->stride_b, r->stride_h, r->stride_t};
   const int n[3] = {d.B, heads, d.T};
-  for (int i = 0; i < 3; ++i) {
-    if (n[i] <= 1) continue;
-    if ((st[i] * elem) % align || (output && st[i] < width)) return false;
+  int64_t span = width;
+  bool seen[3] = {false, false, false};
+  for (int k = 0; k < 3; ++k) {
+    int i = -1;   // the smallest stride left
+    for (int j = 0; j < 3; ++j)
+      if (!seen[j] && n[j] > 1 && (i < 0 || st[j] < st[i])) i = j;
+    if (i < 0) break;
+    seen[i] = true;
+    if ((st[i] * elem) % align || (output && st[i] < span)) return false;
+    span += st[i] * (n[i] - 1);
   }
   return d.T <= 1 || (r->stride_t >= 0 && r->stride_t < ((int64_t)1 << 26));
 }

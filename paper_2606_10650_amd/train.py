@@ -339,3 +339,58 @@ class AdamW:
                                None if grad_scale is None else grad_scale.data_ptr())
             _check(lib().dla_adamw_step(arr, len(arr), ctypes.byref(args), _stream(dev)),
                    "dla_adamw_step")
+
+
+# ---------------------------------------------------------------------------
+# the same for torch's automatic differentiation
+# ---------------------------------------------------------------------------
+def _as_rows(t):
+    """A gradient as the library reads it: last axis contiguous, rows 16-byte aligned."""
+    e = t.element_size()
+    if t.stride(-1) != 1 or t.data_ptr() % 16 or any(s * e % 16 for s in t.stride()[:-1]):
+        return t.contiguous()
+    return t
+
+
+class Recurrence(torch.autograd.Function):
+    """out, last state = Recurrence.apply(q, k, v, g, state, scale, lengths); state and
+    lengths may be None."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, g, state=None, scale=1.0, lengths=None):
+        out, last = recurrence(q, k, v, g, scale=scale, state=state, lengths=lengths, want_state=True)
+        ctx.save_for_backward(q, k, v, g, state, lengths)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return out, last
+
+    @staticmethod
+    def backward(ctx, dout, dlast):
+        q, k, v, g, state, lengths = ctx.saved_tensors
+        dout = torch.zeros_like(v) if dout is None else _as_rows(dout.to(v.dtype))
+        dq, dk, dv, dg, ds = recurrence_backward(q, k, v, g, dout, scale=ctx.scale, state=state,
+                                                 dstate=None if dlast is None else dlast.contiguous(),
+                                                 lengths=lengths)
+        return dq, dk, dv, dg.to(g.dtype), ds, None, None
+
+
+class RMSNorm(torch.autograd.Function):
+    """y, h = RMSNorm.apply(x, residual, weight, eps): h = x + residual, y its norm."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps=1e-6):
+        D = x.shape[-1]
+        y, h, rstd = rms_norm(x.reshape(-1, D), weight, residual.reshape(-1, D), eps=eps)
+        ctx.save_for_backward(h, weight, rstd)
+        ctx.shape = x.shape
+        ctx.set_materialize_grads(False)
+        return y.view(x.shape), h.view(x.shape)
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        h, weight, rstd = ctx.saved_tensors
+        rows = lambda t: t.reshape(h.shape).to(h.dtype)  # noqa: E731
+        dy = torch.zeros_like(h) if dy is None else rows(dy)
+        dx, dw = rms_norm_backward(dy, h, weight, rstd, dres=None if dh is None else rows(dh))
+        dx = dx.view(ctx.shape)
+        return dx, dx, dw.to(weight.dtype), None
