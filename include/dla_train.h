@@ -58,10 +58,10 @@ typedef struct {
  * new sequence in the same row, and its own gradient is zero.  The state must be
  * finite there.
  * Sums and states are float32.  Of bfloat16 inputs, the products of two inputs are
- * exact; the scores and the state that a product reads are rounded once to
- * bfloat16, but what is added to the states keeps 16 bits, so that they hold
- * float32's precision to about 2^-17.  dg adds up what scores and rounded states
- * give and is of the inputs' type.
+ * exact; scores, and what is added to the states, keep 16 bits, so that the states
+ * hold float32's precision to about 2^-17; the state that out and dv read is rounded
+ * once to bfloat16.  dg adds up what the scores and both states give, in float64, and
+ * is of the inputs' type.
  * An infinity or NaN in a token reaches every later output of its head, and may
  * reach those of up to 31 tokens before it.
  */
@@ -161,7 +161,8 @@ dla_status dla_rms_norm_backward(const dla_norm_desc* desc, const dla_norm_rows*
  * [n] of m and of sqrt(v), in the floating point format of dla_rms_norm_fp8, times
  * m_scale, v_scale, float32 [ceil(n / 256)], one per 256 elements in order: the block's
  * largest magnitude / 448 (zero, with codes of zero, where that is below 1e-30).  A
- * sqrt(v) above zero has a code of at least 2^-9.  p is updated with the float32 m and
+ * sqrt(v) above zero has a code of at least 2^-9.  The operations that lead to codes are
+ * each rounded, in the order written above, so that codes follow from inputs bit by bit.  p is updated with the float32 m and
  * v of the step, before they are rounded.  seed 0 rounds codes to nearest even; another
  * seed rounds up or down with the probability that makes the mean right, from a hash of
  * seed, tensor number and element index: a v that moves by a thousandth a step would

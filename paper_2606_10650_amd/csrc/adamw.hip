@@ -186,6 +186,9 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
     float root[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
+      // every operation rounded, none contracted: a last bit can decide a code, and a code
+      // decides the next step, so states are to follow from these lines alone
+#pragma clang fp contract(off)
       g[j] *= scale;
       m[j] = s.beta1 * m[j] + s.rest1 * g[j];
       v[j] = s.beta2 * v[j] + s.rest2 * g[j] * g[j];
@@ -196,8 +199,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
     put4(param + i, n, wide, p);
     if constexpr (F8) {
       const float mt = block_top(m), vt = block_top(root);
-      const float mi = mt > kLeastTop ? 448.f / mt : (mt <= kLeastTop ? 0.f : mt);
-      const float vi = vt > kLeastTop ? 448.f / vt : (vt <= kLeastTop ? 0.f : vt);
+      const float mi = mt > kLeastTop ? 1.f / mt * 448.f : (mt <= kLeastTop ? 0.f : mt);
+      const float vi = vt > kLeastTop ? 1.f / vt * 448.f : (vt <= kLeastTop ? 0.f : vt);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float um = -1.f, uv = -1.f;
@@ -214,8 +217,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
       put_codes(static_cast<uint8_t*>(t.m) + i, n, wide, m);
       put_codes(static_cast<uint8_t*>(t.v) + i, n, wide, v);
       if (lane == 0) {
-        t.m_scale[blk] = mt > kLeastTop ? mt / 448.f : (mt <= kLeastTop ? 0.f : mt);
-        t.v_scale[blk] = vt > kLeastTop ? vt / 448.f : (vt <= kLeastTop ? 0.f : vt);
+        t.m_scale[blk] = mt > kLeastTop ? mt * (1.f / 448.f) : (mt <= kLeastTop ? 0.f : mt);
+        t.v_scale[blk] = vt > kLeastTop ? vt * (1.f / 448.f) : (vt <= kLeastTop ? 0.f : vt);
       }
     } else {
       put4(static_cast<float*>(t.m) + i, n, wide, m);

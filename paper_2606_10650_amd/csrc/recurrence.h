@@ -56,13 +56,14 @@ hipError_t launch_recurrence_forward(const RecArgs& a, int dtype, const Rows& q,
                                      const Rows& v, const Rows& out, const float* s0, float* s_out,
                                      hipStream_t st);
 // dq, by the forward kernel with do, v, k in the places of q, k, v and the state
-// transposed; qdot[head][t] = q_t . (the part of dq_t that came from before the chunk);
+// transposed; qdot[head][t]: what the pairs (s < t, t) give to the gates between them;
 // end_dot[head] = <dstate, last state> where dstate is given.
 hipError_t launch_recurrence_dq(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
                                 const Rows& v, const Rows& dout, const Rows& dq, bool dq_f32,
                                 const float* s0, const float* dstate, float* qdot, float* end_dot,
                                 hipStream_t st);
-// dk, dv, dstate0, and per token what its pairs inside the chunk and behind it add to dg.
+// dk, dv, dstate0 (ds0, which may be dstate's array), and kdot[head][t]: what the pairs (t,
+// u > t) give to the gates between them.
 hipError_t launch_recurrence_adjoint(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
                                      const Rows& v, const Rows& dout, const Rows& dk, bool dk_f32,
                                      const Rows& dv, const float* dstate, float* ds0, float* kdot,

@@ -1,4 +1,4 @@
-// The single-state recurrence over long sequences, and dq of its backward pass.
+// The single-state recurrence over long sequences, and dq, dk and dv of its backward pass.
 //
 // A workgroup takes one head's segment of tokens, a chunk at a time (recurrence_tile.h
 // has the chunk's formulas).  Wave w holds columns 32 w .. 32 w + 31 of the state, all
@@ -8,9 +8,22 @@
 // makes them, too, the operand of the product with the values; every wave forms them for
 // itself, which costs a quarter more products and saves a barrier and a pass through LDS.
 //
-// dq_t = sum_{s <= t} e^{a_t - a_s} (do_t . v_s) k_s + e^{a_t} S do_t is the same with do,
-// v and k in the places of q, k and v and the state transposed.  That pass also leaves
-// qdot_t, what the pairs (s < t, t) give to the gates between them (recurrence_grad.hip).
+// The backward pass is the same kernel with other roles (a_t, a_end as in recurrence_tile.h):
+//   dq_t = e^{a_t} S do_t + scale sum_{s <= t} e^{a_t - a_s} (do_t . v_s) k_s
+// with do, v and k in the places of q, k and v and the state transposed; and, back in time,
+// with R the adjoint of the state behind a chunk (what later tokens and the last state's
+// gradient ask of it),
+//   dv_s = e^{a_end - a_s} R^T k_s + scale sum_{u >= s} e^{a_u - a_s} (q_u . k_s) do_u
+//   dk_s = e^{a_end - a_s} R v_s   + scale sum_{u >= s} e^{a_u - a_s} (do_u . v_s) q_u
+//   R   <- e^{a_end} R + scale sum_u e^{a_u} q_u do_u^T.
+// The passes of dq and dk also leave what pairs of tokens give to the gates between them
+// (recurrence_grad.hip).
+//
+// What bounds it.  Forward, 4 x 16 heads x 16k tokens of 128 x 128 bfloat16: 232 us for 1.07
+// GB, 4.6 TB/s (a large copy 5.1), after 115 for the segments' states (0.54 GB).  dq: 349 us
+// for 1.34 GB; dk and dv: 584 us for 1.6 GB, the chunk's own chain of LDS reads, products and
+// arithmetic at two waves a SIMD (registers; three waves spill).  With every token in the
+// cache 256 heads x 2k tokens forward take 113 us of 132.
 #include "recurrence_tile.h"
 
 namespace dla {
@@ -70,7 +83,8 @@ struct ScanTiles {
   float dots[2][PAIR ? C / 32 : 1][kChunk];   // of the chunk at hand and the one before
 };
 
-// REV: from the segment's last chunk to its first.
+// REV: from the segment's last chunk to its first.  (REV is float32's; bfloat16's dk and dv
+// come from adjoint_kernel.)
 template <typename Tin, int R, int C, bool REV, bool PAIR>
 __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(ScanArgs f) {
   constexpr int NT = 2 * C, NW = C / 32;
@@ -185,7 +199,10 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
 
 // dk and dv at once: half of the waves hold the adjoint's columns and give dv, the others
 // those of its transpose and give dk, from the same tiles.  A chunk's tokens are read once
-// for both, and its next one is stored into the other set of tiles meanwhile.
+// for both, and its next one is stored into the other set of tiles meanwhile.  Against two
+// passes of scan_kernel: 200 heads x 2k tokens backward 430 us against 506, 512 heads (two
+// rounds of workgroups) 893 against 893, 16 heads x 2k forward and backward 134 against 146.
+// float32 does not fit: its operands are twice as wide, and the waves' registers spill.
 template <typename Tin, int DK, int DV>
 struct AdjointTiles {
   Tin q[Tile<Tin, DK>::SIZE], k[Tile<Tin, DK>::SIZE], v[Tile<Tin, DV>::SIZE], o[Tile<Tin, DV>::SIZE];
@@ -406,10 +423,12 @@ template <bool REV, bool PAIR>
 hipError_t launch_scan(const ScanArgs& f, int dtype, int R, int C, hipStream_t st) {
   const dim3 grid(f.a.B * f.a.H * f.a.nseg), block(2 * C);
   if (dtype == DLA_BF16) {
-    if (R == 128 && C == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 128, 128, REV, PAIR>), grid, block, 0, st, f);
-    else if (R == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 128, 64, REV, PAIR>), grid, block, 0, st, f);
-    else if (C == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 64, 128, REV, PAIR>), grid, block, 0, st, f);
-    else hipLaunchKernelGGL((scan_kernel<bf16_t, 64, 64, REV, PAIR>), grid, block, 0, st, f);
+    if constexpr (!REV) {
+      if (R == 128 && C == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 128, 128, false, PAIR>), grid, block, 0, st, f);
+      else if (R == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 128, 64, false, PAIR>), grid, block, 0, st, f);
+      else if (C == 128) hipLaunchKernelGGL((scan_kernel<bf16_t, 64, 128, false, PAIR>), grid, block, 0, st, f);
+      else hipLaunchKernelGGL((scan_kernel<bf16_t, 64, 64, false, PAIR>), grid, block, 0, st, f);
+    }
   } else {
     if (R == 128 && C == 128) hipLaunchKernelGGL((scan_kernel<float, 128, 128, REV, PAIR>), grid, block, 0, st, f);
     else if (R == 128) hipLaunchKernelGGL((scan_kernel<float, 128, 64, REV, PAIR>), grid, block, 0, st, f);

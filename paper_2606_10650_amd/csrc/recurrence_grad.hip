@@ -1,15 +1,5 @@
-// The part of the recurrence's backward pass that runs from the last token back: dk, dv,
-// the adjoint of the state, and the gate's gradient.
-//
-// With R the adjoint of the state behind a chunk (what later tokens and the last state's
-// gradient ask of it), a chunk gives
-//   dv_s = e^{a_end - a_s} R^T k_s + scale sum_{u >= s} e^{a_u - a_s} (q_u . k_s) do_u
-//   dk_s = e^{a_end - a_s} R v_s   + scale sum_{u >= s} e^{a_u - a_s} (do_u . v_s) q_u
-//   R   <- e^{a_end} R + scale sum_u e^{a_u} q_u do_u^T.
-// dv contracts R over its rows and dk over its columns.  Half of the workgroup's waves hold
-// 32 columns each of R, the others 32 columns each of R^T, in accumulators that are the
-// operands of those products as they are; keeping R twice costs the products that update it
-// and no pass through LDS.  Both halves run recurrence_tile.h's chunk step, back in time.
+// What the recurrence's backward pass adds up: the gate's gradient, and dq and dk over heads
+// that share keys.
 //
 // The gate's gradient: e^{g_t} scales what every token s < t leaves for every token u >= t,
 // so dg_t is the sum over those pairs of A_us = scale e^{a_u - a_s} (q_u . k_s)(do_u . v_s),
@@ -17,8 +7,8 @@
 // x_u the sum of A_us over s < u and y_s that over u > s, dg_t = <dstate, last state> + sum
 // over s >= t of (x_s - y_s).  No pair (t, t) enters either, so nothing large cancels where
 // the gates are steep.  The dq pass leaves x (a lane holds a token u and its pairs' scores
-// of do and v; each wave adds the products with its own 32 columns of q and k), this
-// kernel y, the other way round.
+// of do and v; each wave adds the products with its own 32 columns of q and k), the dk pass
+// y, the other way round.
 #include "recurrence_tile.h"
 
 namespace dla {

@@ -15,8 +15,11 @@ using namespace dla;
 
 namespace {
 
-// Tokens up to which a call goes token by token.
-constexpr int kStepTokens = 8;
+// Tokens up to which a call goes token by token, streaming the state once, in place of a
+// chunk.  2048 heads of 128 x 128, bfloat16: 6 tokens 53 us, 8 61, a chunk 53; 256 heads 12,
+// 14, 13.  float32, whose chunks take twice as long: 8 tokens 62 us, a chunk 111; 256 heads
+// 14, 19.
+int step_tokens(int dtype) { return dtype == DLA_BF16 ? 6 : 12; }
 
 struct Plan {
   bool step;
@@ -33,7 +36,7 @@ struct Plan {
 // 492.  A segment has at least 4 chunks, 2 of float32, whose chunks take longer (15 heads x
 // 1531 tokens: 161 us, 175 with 4, 274 with 8).
 Plan plan_of(const dla_recurrence_desc& d, bool backward) {
-  Plan p{!backward && d.T <= kStepTokens, 1, kRecChunk};
+  Plan p{!backward && d.T <= step_tokens(d.dtype), 1, kRecChunk};
   if (d.B == 0 || d.T == 0) return p;   // nothing to plan
   const int heads = d.B * d.H, chunks = (d.T + kRecChunk - 1) / kRecChunk;
   const int narrow = (d.d_k == 64) + (d.d_v == 64);
