@@ -69,19 +69,21 @@ hipError_t launch_recurrence_adjoint(const RecArgs& a, int dtype, const Rows& q,
                                      const Rows& dv, const float* dstate, float* ds0, float* kdot,
                                      hipStream_t st);
 // Each segment's own contribution to the state (or, reverse, to the adjoint), and from
-// them the state before (the adjoint behind) each segment.
+// them the state before (the adjoint behind) each segment.  reverse, after the other: also
+// anchor [heads][nseg][d_k d_v / 256], whose sums over the last axis are the products of the
+// adjoint behind each segment but the last with the state there.
 hipError_t launch_recurrence_segments(const RecArgs& a, int dtype, bool reverse, const Rows& x,
-                                      const Rows& y, const float* first, hipStream_t st);
+                                      const Rows& y, const float* first, double* anchor, hipStream_t st);
 // Token by token, for short sequences.
 hipError_t launch_recurrence_step(const RecArgs& a, int dtype, const Rows& q, const Rows& k,
                                   const Rows& v, const Rows& out, const float* s0, float* s_out,
                                   hipStream_t st);
-// dg from the per-token sums: dg_t = end_dot + sum over s >= t of (qdot_s - kdot_s); anchor:
-// [heads][nseg] of workspace.
+// dg from the per-token sums: dg_t = end_dot + sum over s >= t of (qdot_s - kdot_s), each
+// segment's sum from its anchor.
 hipError_t launch_recurrence_dgate(const RecArgs& a, int dtype, const float* qdot, const float* kdot,
-                                   double* anchor, const float* end_dot, const Rows& dg, hipStream_t st);
+                                   const double* anchor, const float* end_dot, const Rows& dg, hipStream_t st);
 // Sums the heads that share a key head: [B][H][T][d] float32 -> rows of B * Hk heads.
-hipError_t launch_head_sum(const RecArgs& a, int dtype, const float* part, const Rows& out,
-                           hipStream_t st);
+hipError_t launch_head_sums(const RecArgs& a, int dtype, const float* dq_part, const Rows& dq,
+                            const float* dk_part, const Rows& dk, hipStream_t st);
 
 }  // namespace dla

@@ -16,32 +16,14 @@ namespace {
 
 // dg from the tokens' sums, from the last token back, in float64: what is added up spans
 // many tokens, what is left may be small.  Each segment starts from its own end, where the
-// sum is <adjoint behind the segment, state there>, so that what the tokens' sums were
-// rounded by adds up over a segment at most.  A cut gate lets nothing through: dg is zero
-// there and the sum starts anew, exactly.
-__global__ __launch_bounds__(256) void anchor_kernel(RecArgs a, double* anchor) {
-  __shared__ double sums[4];
-  const int64_t D = (int64_t)a.dk * a.dv;
-  const int seg = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
-  const float* s = a.seg_state + ((int64_t)head * a.nseg + seg + 1) * D;
-  const float* r = a.seg_adj + ((int64_t)head * a.nseg + seg) * D;
-  double x = 0.0;
-  for (int64_t i = tid * 4; i < D; i += 1024) {
-    const float4 p = *reinterpret_cast<const float4*>(s + i), q = *reinterpret_cast<const float4*>(r + i);
-    x += (double)p.x * q.x + (double)p.y * q.y + ((double)p.z * q.z + (double)p.w * q.w);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-  if ((tid & 63) == 0) sums[tid >> 6] = x;
-  __syncthreads();
-  if (tid == 0) anchor[(int64_t)head * a.nseg + seg] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-}
-
+// sum is <adjoint behind the segment, state there> (parts of 256 elements, prefix_kernel), so
+// that what the tokens' sums were rounded by adds up over a segment at most.  A cut gate lets
+// nothing through: dg is zero there and the sum starts anew, exactly.
 struct DgArgs {
   RecArgs a;
   const float* qdot;
   const float* kdot;
-  const double* anchor;   // [heads][nseg], the last segment's apart:
+  const double* anchor;   // [heads][nseg][d_k d_v / 256], the last segment's apart:
   const float* end_dot;   // [heads], or null for zero
   Rows dg;
   int dtype;
@@ -68,8 +50,12 @@ __global__ __launch_bounds__(256) void dgate_kernel(DgArgs f) {
   __shared__ double sums[4];
   __shared__ int cuts[4];
   double carry = 0.0;   // of what is behind the block
-  if (seg < a.nseg - 1) carry = f.anchor[(int64_t)head * a.nseg + seg];
-  else if (f.end_dot) carry = (double)f.end_dot[head];
+  if (seg < a.nseg - 1) {
+    const int n = a.dk * a.dv / 256;   // up to 64: every wave adds them up
+    if (lane < n) carry = f.anchor[((int64_t)head * a.nseg + seg) * n + lane];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) carry += __shfl_xor(carry, o);
+  } else if (f.end_dot) carry = (double)f.end_dot[head];
   for (int base = begin + (end - begin - 1) / kDgateBlock * kDgateBlock; base >= begin; base -= kDgateBlock) {
     const int t0 = base + tid * kPer;
     double x[kPer];
@@ -132,18 +118,25 @@ __global__ __launch_bounds__(256) void dgate_kernel(DgArgs f) {
 }
 
 // [B][H][T][d] float32 -> the sum over the H / Hk heads of each key head, four columns a
-// thread, heads in order.
+// thread, heads in order, of dq and of dk in one launch.
+struct HeadSums {
+  const float* part[2];
+  Rows out[2];
+};
+
 template <typename Tin>
-__global__ __launch_bounds__(256) void head_sum_kernel(RecArgs a, const float* part, Rows out) {
+__global__ __launch_bounds__(256) void head_sum_kernel(RecArgs a, HeadSums f) {
   const int n4 = a.dk / 4, G = a.H / a.Hk;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)a.T * n4;
   if (i >= per) return;
-  const int64_t t = i / n4, c = 4 * (i % n4);
+  const int64_t t = i / n4, c = 4 * (i % n4), step = (int64_t)a.T * a.dk;
   const int b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk;
-  const float* p = part + (((int64_t)b * a.H + hk * G) * a.T + t) * a.dk + c;
+  const Rows& out = f.out[blockIdx.z];
+  const float* p = f.part[blockIdx.z] + (((int64_t)b * a.H + hk * G) * a.T + t) * a.dk + c;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
   for (int j = 0; j < G; ++j) {
-    const float4 x = *reinterpret_cast<const float4*>(p + (int64_t)j * a.T * a.dk);
+    const float4 x = *reinterpret_cast<const float4*>(p + j * step);
     s.x += x.x;
     s.y += x.y;
     s.z += x.z;
@@ -166,18 +159,18 @@ __global__ __launch_bounds__(256) void head_sum_kernel(RecArgs a, const float* p
 }  // namespace
 
 hipError_t launch_recurrence_dgate(const RecArgs& a, int dtype, const float* qdot, const float* kdot,
-                                   double* anchor, const float* end_dot, const Rows& dg, hipStream_t st) {
-  if (a.nseg > 1) hipLaunchKernelGGL(anchor_kernel, dim3(a.nseg - 1, a.B * a.H), dim3(256), 0, st, a, anchor);
+                                   const double* anchor, const float* end_dot, const Rows& dg, hipStream_t st) {
   const DgArgs f{a, qdot, kdot, anchor, end_dot, dg, dtype};
   hipLaunchKernelGGL(dgate_kernel, dim3(a.nseg, a.B * a.H), dim3(256), 0, st, f);
   return hipGetLastError();
 }
 
-hipError_t launch_head_sum(const RecArgs& a, int dtype, const float* part, const Rows& out,
-                           hipStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)a.T * a.dk / 4 + 255) / 256), a.B * a.Hk);
-  if (dtype == DLA_BF16) hipLaunchKernelGGL((head_sum_kernel<bf16_t>), grid, dim3(256), 0, st, a, part, out);
-  else hipLaunchKernelGGL((head_sum_kernel<float>), grid, dim3(256), 0, st, a, part, out);
+hipError_t launch_head_sums(const RecArgs& a, int dtype, const float* dq_part, const Rows& dq,
+                            const float* dk_part, const Rows& dk, hipStream_t st) {
+  const dim3 grid((unsigned)(((int64_t)a.T * a.dk / 4 + 255) / 256), a.B * a.Hk, 2);
+  const HeadSums f{{dq_part, dk_part}, {dq, dk}};
+  if (dtype == DLA_BF16) hipLaunchKernelGGL((head_sum_kernel<bf16_t>), grid, dim3(256), 0, st, a, f);
+  else hipLaunchKernelGGL((head_sum_kernel<float>), grid, dim3(256), 0, st, a, f);
   return hipGetLastError();
 }
 

@@ -78,7 +78,7 @@ Space space_of(const dla_recurrence_desc& d, const Plan& p, bool backward) {
     s.qdot = take(tokens * 4);
     s.kdot = take(tokens * 4);
     s.end_dot = take(heads * 4);
-    s.anchor = take(heads * p.nseg * 8);
+    if (p.nseg > 1) s.anchor = take(heads * p.nseg * (D / 256) * 8);
     if (d.Hk != d.H) {
       s.dq_part = take(tokens * d.d_k * 4);
       s.dk_part = take(tokens * d.d_k * 4);
@@ -260,7 +260,7 @@ dla_status dla_recurrence_forward(const dla_recurrence_desc* desc, const dla_row
     r = launch_recurrence_step(a, d.dtype, qr, kr, vr, outr, state, state_out, st);
   } else {
     r = launch_recurrence_decays(a, st);
-    if (r == hipSuccess && p.nseg > 1) r = launch_recurrence_segments(a, d.dtype, false, kr, vr, state, st);
+    if (r == hipSuccess && p.nseg > 1) r = launch_recurrence_segments(a, d.dtype, false, kr, vr, state, nullptr, st);
     if (r == hipSuccess) r = launch_recurrence_forward(a, d.dtype, qr, kr, vr, outr, state, state_out, st);
   }
   return remember(r == hipSuccess ? DLA_OK : DLA_ERR_HIP);
@@ -309,22 +309,21 @@ dla_status dla_recurrence_backward(const dla_recurrence_desc* desc, const dla_ro
   float* qdot = (float*)(ws + sp.qdot);
   float* kdot = (float*)(ws + sp.kdot);
   float* end_dot = (float*)(ws + sp.end_dot);
+  double* anchor = (double*)(ws + sp.anchor);
   hipError_t r = launch_recurrence_decays(a, st);
   if (r == hipSuccess && p.nseg > 1) {
-    r = launch_recurrence_segments(a, d.dtype, false, kr, vr, state, st);
-    if (r == hipSuccess) r = launch_recurrence_segments(a, d.dtype, true, qr, dor, dstate_out, st);
+    r = launch_recurrence_segments(a, d.dtype, false, kr, vr, state, nullptr, st);
+    if (r == hipSuccess) r = launch_recurrence_segments(a, d.dtype, true, qr, dor, dstate_out, anchor, st);
   }
   if (r == hipSuccess)
     r = launch_recurrence_dq(a, d.dtype, qr, kr, vr, dor, dqp, shared, state, dstate_out, qdot, end_dot, st);
   if (r == hipSuccess)
     r = launch_recurrence_adjoint(a, d.dtype, qr, kr, vr, dor, dkp, shared, rows_of(dv, 1), dstate_out, dstate, kdot, st);
   if (r == hipSuccess)
-    r = launch_recurrence_dgate(a, d.dtype, qdot, kdot, (double*)(ws + sp.anchor),
+    r = launch_recurrence_dgate(a, d.dtype, qdot, kdot, anchor,
                                 dstate_out ? end_dot : nullptr, rows_of(dg, 1), st);
-  if (shared && r == hipSuccess) {
-    r = launch_head_sum(a, d.dtype, (const float*)dqp.p, dqr, st);
-    if (r == hipSuccess) r = launch_head_sum(a, d.dtype, (const float*)dkp.p, dkr, st);
-  }
+  if (shared && r == hipSuccess)
+    r = launch_head_sums(a, d.dtype, (const float*)dqp.p, dqr, (const float*)dkp.p, dkr, st);
   return remember(r == hipSuccess ? DLA_OK : DLA_ERR_HIP);
 }
 
