@@ -80,7 +80,8 @@ template <typename Tin, int R, int C, bool PAIR>
 struct ScanTiles {
   Tin q[Tile<Tin, R>::SIZE], k[Tile<Tin, R>::SIZE], v[Tile<Tin, C>::SIZE], y[PAIR ? Tile<Tin, C>::SIZE : 8];
   Decays dec;
-  float dots[2][PAIR ? C / 32 : 1][kChunk];   // of the chunk at hand and the one before
+  Scores<Tin> p;
+  float dots[2][PAIR ? C / 32 + 2 : 1][kChunk];   // of the chunk at hand and the one before
 };
 
 // REV: from the segment's last chunk to its first.  (REV is float32's; bfloat16's dk and dv
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
 
   Stage<Tin, R, NT> gq, gk;
   Stage<Tin, C, NT> gv, gy;
-  DecayStage<NT, REV> gd;
+  DecayStage gd;
   auto request = [&](int t0) {
     gq.load(q, f.q.st, lim - t0, tid);
     gk.load(k, f.k.st, lim - t0, tid);
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
     if (tid < kChunk && t0 + tid < end) {
       float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) x += now.dots[which][w][tid];
+      for (int w = 0; w < NW + 2; ++w) x += now.dots[which][w][tid];
       dot_out[t0 + tid] = t0 + tid < lim ? x : 0.f;
     }
   };
@@ -141,7 +142,6 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
   else S.clear();
   int t0 = t_first;
   for (int c = 0; c < n; ++c, t0 += STEP) {
-    gd.form(a.scale, tid);
     __syncthreads();   // the last chunk's tiles are read, its dots written
     gq.store(now.q, tid);
     gk.store(now.k, tid);
@@ -153,8 +153,23 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
     if constexpr (PAIR) {
       if (c > 0) sum_dots((c - 1) & 1, t0 - STEP);
     }
+    // scores, a quarter (NW = 2: a half) a wave
+#pragma unroll
+    for (int i = wave; i < 4; i += NW) {
+      const int th = 16 * (i & 1), sh = 16 * (i >> 1);
+      f32x4 p = {0.f, 0.f, 0.f, 0.f};
+      float x = 0.f;
+      if (REV ? sh >= th : sh <= th) {
+        p = scores16<Tin, R>(now.k, now.q, sh, th, lane) * decays16<REV>(now.dec, a.scale, sh, th, lane);
+        if constexpr (PAIR) x = pairs16(p, scores16<Tin, C>(now.v, now.y, sh, th, lane), sh, th, lane);
+      }
+      now.p.put(th + (lane & 15), sh + 4 * (lane >> 4), p);
+      if constexpr (PAIR) {
+        if (lane < 16) now.dots[c & 1][NW + (i >> 1)][th + lane] = x;
+      }
+    }
     f32x16 o;
-    const float dot = chunk_step<Tin, R, C, REV, PAIR>(now.q, now.k, now.v, now.y, now.dec, a.scale, c0, lane, S, o);
+    const float dot = chunk_step<Tin, R, C, REV, PAIR>(now.q, now.k, now.v, now.y, now.dec, now.p, a.scale, c0, lane, S, o);
     if constexpr (PAIR) {
       if (lane < 32) now.dots[c & 1][wave][lane] = dot;
     }
@@ -207,7 +222,7 @@ template <typename Tin, int DK, int DV>
 struct AdjointTiles {
   Tin q[Tile<Tin, DK>::SIZE], k[Tile<Tin, DK>::SIZE], v[Tile<Tin, DV>::SIZE], o[Tile<Tin, DV>::SIZE];
   Decays dec;
-  float dots[DK / 32][kChunk];
+  float dots[DK / 32 + 2][kChunk];
 };
 
 struct AdjointArgs {
@@ -223,6 +238,7 @@ template <typename Tin, int DK, int DV>
 __global__ __launch_bounds__(2 * (DK + DV), 2) void adjoint_kernel(AdjointArgs f) {
   constexpr int NT = 2 * (DK + DV), KW = DK / 32, VW = DV / 32;
   __shared__ __align__(16) AdjointTiles<Tin, DK, DV> tiles[2];
+  __shared__ __align__(16) Scores<Tin> scores[2];   // of q and k, for dv; of dout and v, for dk
   const RecArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -239,7 +255,7 @@ __global__ __launch_bounds__(2 * (DK + DV), 2) void adjoint_kernel(AdjointArgs f
   const float2* decays = a.decays + 2 * head * padded + t_last;
   Stage<Tin, DK, NT> gq, gk;
   Stage<Tin, DV, NT> gv, go;
-  DecayStage<NT, true> gd;
+  DecayStage gd;
   auto request = [&](int t0) {
     gq.load(q, f.q.st, lim - t0, tid);
     gk.load(k, f.k.st, lim - t0, tid);
@@ -257,7 +273,6 @@ __global__ __launch_bounds__(2 * (DK + DV), 2) void adjoint_kernel(AdjointArgs f
     gk.store(to.k, tid);
     gv.store(to.v, tid);
     go.store(to.o, tid);
-    gd.form(a.scale, tid);
     gd.store(to.dec, tid);
   };
   const float* last = a.nseg > 1 ? a.seg_adj + ((int64_t)head * a.nseg + seg) * D
@@ -273,10 +288,27 @@ __global__ __launch_bounds__(2 * (DK + DV), 2) void adjoint_kernel(AdjointArgs f
     __syncthreads();
     Tin* out = row_base<Tin>(f.dv, b, h) + t_last * f.dv.st;
     for (int t0 = t_last; t0 >= begin; t0 -= kChunk, at ^= 1) {
-      const AdjointTiles<Tin, DK, DV>& now = tiles[at];
+      AdjointTiles<Tin, DK, DV>& now = tiles[at];
       if (t0 > begin) request(t0 - kChunk);
+      // dv's waves have less to do: both kinds of scores, and the pairs' sums
+#pragma unroll
+      for (int i = wave; i < 4; i += VW) {
+        const int th = 16 * (i & 1), sh = 16 * (i >> 1);
+        f32x4 p = {0.f, 0.f, 0.f, 0.f}, z = p;
+        float sum = 0.f;
+        if (sh >= th) {
+          const f32x4 d = decays16<true>(now.dec, a.scale, sh, th, lane);
+          p = scores16<Tin, DK>(now.q, now.k, sh, th, lane);
+          z = scores16<Tin, DV>(now.o, now.v, sh, th, lane) * d;
+          sum = pairs16(z, p, sh, th, lane);
+          p *= d;
+        }
+        scores[0].put(th + (lane & 15), sh + 4 * (lane >> 4), p);
+        scores[1].put(th + (lane & 15), sh + 4 * (lane >> 4), z);
+        if (lane < 16) now.dots[KW + (i >> 1)][th + lane] = sum;
+      }
       f32x16 x;
-      chunk_step<Tin, DK, DV, true, false>(now.k, now.q, now.o, nullptr, now.dec, a.scale, c0, lane, R, x);
+      chunk_step<Tin, DK, DV, true, false>(now.k, now.q, now.o, nullptr, now.dec, scores[0], a.scale, c0, lane, R, x);
       store_out(out, f.dv.st, c0, x, lim - t0, end - t0, lane);
       out -= kChunk * f.dv.st;
       if (t0 > begin) store(tiles[at ^ 1]);
@@ -297,7 +329,7 @@ __global__ __launch_bounds__(2 * (DK + DV), 2) void adjoint_kernel(AdjointArgs f
       if (c0 == 0 && lane < kChunk && t0 + lane < end) {
         float x = 0.f;
 #pragma unroll
-        for (int i = 0; i < KW; ++i) x += from.dots[i][lane];
+        for (int i = 0; i < KW + 2; ++i) x += from.dots[i][lane];
         dot_out[t0 + lane] = t0 + lane < lim ? x : 0.f;
       }
     };
@@ -310,7 +342,7 @@ __global__ __launch_bounds__(2 * (DK + DV), 2) void adjoint_kernel(AdjointArgs f
       if (t0 > begin) request(t0 - kChunk);
       if (t0 < t_last) sum_dots(tiles[at ^ 1], t0 + kChunk);
       f32x16 x;
-      const float dot = chunk_step<Tin, DV, DK, true, true>(now.v, now.o, now.q, now.k, now.dec, a.scale, c0, lane, R, x);
+      const float dot = chunk_step<Tin, DV, DK, true, true>(now.v, now.o, now.q, now.k, now.dec, scores[1], a.scale, c0, lane, R, x);
       if (lane < 32) now.dots[c0 / 32][lane] = dot;
       if (f.dk_f32) {
         store_out(reinterpret_cast<float*>(out), f.dk.st, c0, x, lim - t0, end - t0, lane);

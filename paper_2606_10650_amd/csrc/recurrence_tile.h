@@ -41,6 +41,10 @@ struct Tile {
                                                                    int lane) {
     return Frag<Tin>::load(p + at(row, 16 * (kk & 1) + 8 * (lane >> 5)) + 32 * (kk >> 1));
   }
+  // operand of a 16 x 16 product: row `row` per lane % 16, columns 32 k + 8 (lane / 16) + e
+  __device__ static __forceinline__ typename Frag<Tin>::T row_frag16(const Tin* p, int row, int k, int lane) {
+    return Frag<Tin>::load(p + at(row, 8 * (lane >> 4)) + 32 * k);
+  }
   // operand with a column per lane, c0 + perm_row(lane % 32) (c0 a multiple of 32), and
   // tokens 16 kk + 8 (lane / 32) + e
   __device__ static __forceinline__ typename Frag<Tin>::T col_frag(const Tin* p, int c0, int kk,
@@ -122,54 +126,29 @@ __device__ __forceinline__ float decay2(float hi_t, float lo_t, float hi_s, floa
   return __builtin_amdgcn_exp2f((hi_t - hi_s) + (lo_t - lo_s));
 }
 
-// A chunk's decays in LDS: in, out, and between all pairs of its tokens, zero where the
-// later of a pair should come first.  pair[t][s] is scale times the decay between the lane
-// token t of chunk_step and s, so from s to t, or with REV from t to s.
+// A chunk's decays in LDS: in and out, and a_t as hi and lo for those between its tokens.
 struct Decays {
-  static constexpr int LD = kChunk + 4;
-  float in[kChunk], out[kChunk], pair[kChunk * LD];
+  float in[kChunk], out[kChunk];
+  float2 at[kChunk];
   __device__ __forceinline__ float total() const { return in[kChunk - 1]; }   // e^{a_end}
 };
 
-// On its way from memory: load, then, before the barrier behind which tiles may be
-// overwritten, form, then store.
-template <int NT, bool REV>
+// On its way from memory, by the first threads.
 struct DecayStage {
-  static constexpr int M = NT >= 256 ? 4 : kChunk * kChunk / NT;   // consecutive s per thread
-  static constexpr int G = kChunk / M, ALL = kChunk * G;           // of the first ALL threads
-  float2 io, t, s[M];
-  float x[M];
+  float2 io, t;
   // chunk: the first token's hi and lo; its in and out are `padded` behind
   __device__ __forceinline__ void load(const float2* chunk, int64_t padded, int tid) {
-    if (tid < kChunk) io = chunk[padded + tid];
-    if (NT > ALL && tid >= ALL) return;
-    t = chunk[tid / G];
-#pragma unroll
-    for (int i = 0; i < M; i += 2) {
-      const float4 y = *reinterpret_cast<const float4*>(chunk + (tid % G) * M + i);
-      s[i] = make_float2(y.x, y.y);
-      s[i + 1] = make_float2(y.z, y.w);
-    }
-  }
-  __device__ __forceinline__ void form(float scale, int tid) {
-    if (NT > ALL && tid >= ALL) return;
-    const int tt = tid / G, s0 = (tid % G) * M;
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-      const float y = REV ? decay2(s[i].x, s[i].y, t.x, t.y) : decay2(t.x, t.y, s[i].x, s[i].y);
-      x[i] = (REV ? s0 + i >= tt : s0 + i <= tt) ? y * scale : 0.f;
+    if (tid < kChunk) {
+      t = chunk[tid];
+      io = chunk[padded + tid];
     }
   }
   __device__ __forceinline__ void store(Decays& d, int tid) const {
     if (tid < kChunk) {
       d.in[tid] = io.x;
       d.out[tid] = io.y;
+      d.at[tid] = t;
     }
-    if (NT > ALL && tid >= ALL) return;
-#pragma unroll
-    for (int i = 0; i < M; i += 4)
-      *reinterpret_cast<float4*>(d.pair + tid / G * Decays::LD + (tid % G) * M + i) =
-          make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
   }
 };
 
@@ -282,84 +261,152 @@ struct State {
   }
 };
 
-// One chunk, for a wave's 32 columns of a state of R rows.  Lane l % 32 is token t; the
-// elements of o are columns c0 + held_row(r).
-//   p[r] = q_t . k_s with s = held_row(r)
+// Masked and decayed scores of a chunk, [t][s], for the product with the values: bfloat16 in
+// two terms (two more of some thirty products, and outputs of short sequences lose 2^-9
+// instead of 2^-8.5).  Rows are padded by 16 bytes: reads of 16 bytes are free of conflicts.
+template <typename Tin>
+struct Scores;
+template <>
+struct Scores<bf16_t> {
+  static constexpr int LD = kChunk + 8, TERMS = 2;
+  bf16_t x[2][kChunk * LD];
+  __device__ __forceinline__ void put(int t, int s, const f32x4& p) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    bf16x4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      h[e] = (__bf16)p[e];
+      l[e] = (__bf16)(p[e] - (float)h[e]);
+    }
+    *reinterpret_cast<bf16x4*>(x[0] + t * LD + s) = h;
+    *reinterpret_cast<bf16x4*>(x[1] + t * LD + s) = l;
+  }
+  __device__ __forceinline__ bf16x8 frag(int term, int t, int s) const {
+    return Frag<bf16_t>::load(x[term] + t * LD + s);
+  }
+};
+template <>
+struct Scores<float> {
+  static constexpr int LD = kChunk + 4, TERMS = 1;
+  float x[kChunk * LD];
+  __device__ __forceinline__ void put(int t, int s, const f32x4& p) {
+    *reinterpret_cast<f32x4*>(x + t * LD + s) = p;
+  }
+  __device__ __forceinline__ f32x8 frag(int, int t, int s) const { return Frag<float>::load(x + t * LD + s); }
+};
+
+// 16 x 16 scores: lane l holds a . b of rows s0 + 4 (l / 16) + r of a and row t0 + l % 16 of b.
+template <typename Tin, int D>
+__device__ __forceinline__ f32x4 scores16(const Tin* a, const Tin* b, int s0, int t0, int lane) {
+  using TL = Tile<Tin, D>;
+  f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < D / 32; ++k)
+    mma16(p, TL::row_frag16(a, s0 + (lane & 15), k, lane), TL::row_frag16(b, t0 + (lane & 15), k, lane));
+  return p;
+}
+// scale times the decays between their tokens: from s to t, or with REV from t to s, zero
+// where the later of a pair should come first.
+template <bool REV>
+__device__ __forceinline__ f32x4 decays16(const Decays& dec, float scale, int s0, int t0, int lane) {
+  const int t = t0 + (lane & 15), s = s0 + 4 * (lane >> 4);
+  const float2 x = dec.at[t];
+  f32x4 d;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const float2 y = dec.at[s + r];
+    const float e = REV ? decay2(y.x, y.y, x.x, x.y) : decay2(x.x, x.y, y.x, y.y);
+    d[r] = (REV ? s + r >= t : s + r <= t) ? e * scale : 0.f;
+  }
+  return d;
+}
+// What the pairs (s, t), s != t, of a tile give to the gates between them, the sum over its
+// tokens s, in all lanes: decayed scores of the one product times the other's plain ones.
+__device__ __forceinline__ float pairs16(const f32x4& p, const f32x4& z, int s0, int t0, int lane) {
+  float x = 0.f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) x += s0 + 4 * (lane >> 4) + r != t0 + (lane & 15) ? p[r] * z[r] : 0.f;
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
+// One chunk, for a wave's 32 columns of a state of R rows, the scores being on their way into
+// P.  Lane l % 32 is token t; the elements of o are columns c0 + held_row(r).
 //   c = carry_t S^T q_t
-//   o = c + scale sum over s of p masked and decayed, times v_s
-// and the state takes up the chunk.  The decayed scores enter in two bfloat16 terms: two more
-// of some forty products, and outputs of short sequences lose 2^-9 instead of 2^-8.5.  REV: time runs back, so s >= t.  PAIR: c also
-// takes what the state's rounding to bfloat16 leaves, and
-//   dot_t = y_t . c + scale sum over s != t of p masked and decayed, times (y_t . v_s)
-// is returned, with the rows y_t (the wave's 32 columns of them) in sy: what the pairs
-// (s, t) give to the gates between them.  The state's products come before the arithmetic
-// on scores and outputs, which they do not need and hide.
+//   o = c + sum over s of P[t][s] v_s
+// and the state takes up the chunk.  REV: time runs back.  PAIR: c also takes what the
+// state's rounding to bfloat16 leaves, and y_t . c is returned, with the rows y_t (the wave's
+// 32 columns of them) in sy: what the tokens before the chunk give to the gates before t.
+// The barrier behind which all waves' scores are in P comes after the state's products.
+// Each step reads the next one's operands from LDS before it works on its own: the fences
+// keep the compiler from reading them only where they are used.
 template <typename Tin, int R, int C, bool REV, bool PAIR>
 __device__ __forceinline__ float chunk_step(const Tin* sq, const Tin* sk, const Tin* sv, const Tin* sy,
-                                            const Decays& dec, float scale, int c0, int lane,
-                                            State<R / 32>& S, f32x16& o) {
+                                            const Decays& dec, const Scores<Tin>& P, float scale, int c0,
+                                            int lane, State<R / 32>& S, f32x16& o) {
   using F = typename Frag<Tin>::T;
   using TR = Tile<Tin, R>;
   using TC = Tile<Tin, C>;
-  const int t = lane & 31, kr = perm_row(t);
-  f32x16 p = zero16(), z = zero16();
-  F y[2];
+  const int t = lane & 31;
+  constexpr int K = R / 16, I = R / 32;
+  F y[2], v[2];
   o = zero16();
+  F q = TR::row_frag(sq, t, 0, lane);
 #pragma unroll
-  for (int kk = 0; kk < R / 16; ++kk) {
-    const F q = TR::row_frag(sq, t, kk, lane);
-    Frag<Tin>::mma(p, TR::row_frag(sk, kr, kk, lane), q);
+  for (int kk = 0; kk < K; ++kk) {
+    F qn = q;
+    if (kk + 1 < K) qn = TR::row_frag(sq, t, kk + 1, lane);
+    else v[0] = TC::col_frag(sv, c0, 0, lane);
+    fence();
     const F s = state_frag<Tin>(S.s[kk >> 1], kk & 1);
     if constexpr (PAIR && sizeof(Tin) == 2) Frag<Tin>::mma(o, state_frag_low(S.s[kk >> 1], kk & 1, s), q);
     Frag<Tin>::mma(o, s, q);
-  }
-  if constexpr (PAIR) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      y[kk] = TC::row_frag(sy + c0, t, kk, lane);
-      Frag<Tin>::mma(z, TC::row_frag(sv + c0, kr, kk, lane), y[kk]);
-    }
+    fence();
+    q = qn;
   }
   const float carry = (REV ? dec.out[t] : dec.in[t] * scale) * S.f;
   if (S.decay(dec.total())) S.apply();
   const float inv = (REV ? scale : 1.f) * __builtin_amdgcn_rcpf(S.f);
-  F v[2];
+  F k = TR::col_frag(sk, 0, 0, lane);
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) {
     float w[8];
     weights8(REV ? dec.in : dec.out, kk, lane, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] *= inv;
-    v[kk] = TC::col_frag(sv, c0, kk, lane);
     const Scaled<Tin> x(v[kk], w);
 #pragma unroll
-    for (int i = 0; i < R / 32; ++i) x.mma_b(S.s[i], TR::col_frag(sk, 32 * i, kk, lane));
-  }
-  // the scores, masked and decayed, and the carried part
-#pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
-    float d[8];
-    weights8(dec.pair + t * Decays::LD, kk, lane, d);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[8 * kk + e] *= d[e];
-      o[8 * kk + e] *= carry;
+    for (int i = 0; i < I; ++i) {
+      F kn = k;
+      if (i + 1 < I) kn = TR::col_frag(sk, 32 * (i + 1), kk, lane);
+      else if (kk == 0) kn = TR::col_frag(sk, 0, 1, lane);
+      if (kk == 0 && i == 0) v[1] = TC::col_frag(sv, c0, 1, lane);
+      if constexpr (PAIR) {
+        if (kk == 1 && i + 1 == I) {
+          y[0] = TC::row_frag(sy + c0, t, 0, lane);
+          y[1] = TC::row_frag(sy + c0, t, 1, lane);
+        }
+      }
+      fence();
+      x.mma_b(S.s[i], k);
+      fence();
+      k = kn;
     }
   }
   float dot[4] = {0.f, 0.f, 0.f, 0.f};
-  if constexpr (PAIR) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      dot[r & 3] += o[r] * (float)y[r >> 3][r & 7];
-      dot[r & 3] += held_row(r, lane) != t ? p[r] * z[r] : 0.f;
-    }
+  for (int r = 0; r < 16; ++r) {
+    o[r] *= carry;
+    if constexpr (PAIR) dot[r & 3] += o[r] * (float)y[r >> 3][r & 7];
   }
+  __syncthreads();
 #pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
-    const F x = state_frag<Tin>(p, kk);
-    if constexpr (sizeof(Tin) == 2) Frag<Tin>::mma(o, v[kk], state_frag_low(p, kk, x));
-    Frag<Tin>::mma(o, v[kk], x);
-  }
+  for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+    for (int n = Scores<Tin>::TERMS - 1; n >= 0; --n)
+      Frag<Tin>::mma(o, v[kk], P.frag(n, t, 16 * kk + 8 * (lane >> 5)));
   if constexpr (PAIR) {
     const float x = (dot[0] + dot[1]) + (dot[2] + dot[3]);
     return x + __shfl_xor(x, 32);
