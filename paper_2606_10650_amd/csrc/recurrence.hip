@@ -4,9 +4,9 @@
 // has the chunk's formulas).  Wave w holds columns 32 w .. 32 w + 31 of the state, all
 // d_k rows of them, in the accumulators of the products that update it; their layout is
 // that of the first operand of the product that reads them, so the state never leaves
-// the registers.  The chunk's scores are formed with keys as the first operand, which
-// makes them, too, the operand of the product with the values; every wave forms them for
-// itself, which costs a quarter more products and saves a barrier and a pass through LDS.
+// the registers.  The chunk's scores are formed once, 16 x 16 of them a wave, and go through
+// LDS to all waves, which meet only after the state's products (4 x 16k tokens of 16 heads,
+// forward and backward: 1514 us when each wave formed them all for itself, 1415 so).
 //
 // The backward pass is the same kernel with other roles (a_t, a_end as in recurrence_tile.h):
 //   dq_t = e^{a_t} S do_t + scale sum_{s <= t} e^{a_t - a_s} (do_t . v_s) k_s
@@ -19,11 +19,13 @@
 // The passes of dq and dk also leave what pairs of tokens give to the gates between them
 // (recurrence_grad.hip).
 //
-// What bounds it.  Forward, 4 x 16 heads x 16k tokens of 128 x 128 bfloat16: 232 us for 1.07
-// GB, 4.6 TB/s (a large copy 5.1), after 115 for the segments' states (0.54 GB).  dq: 349 us
-// for 1.34 GB; dk and dv: 584 us for 1.6 GB, the chunk's own chain of LDS reads, products and
-// arithmetic at two waves a SIMD (registers; three waves spill).  With every token in the
-// cache 256 heads x 2k tokens forward take 113 us of 132.
+// What bounds it.  Forward, 4 x 16 heads x 16k tokens of 128 x 128 bfloat16: 234 us for 1.07
+// GB, 4.6 TB/s (a large copy 5.1), after 123 for the segments' states (0.54 GB).  dq: 326 us
+// for 1.34 GB, 4.1 TB/s; dk and dv: 528 us for 1.6 GB, the chunk's own chain of LDS reads,
+// products and arithmetic at two waves a SIMD.  A third wave in the forward pass takes 17
+// registers through scratch memory (300 heads x 2k tokens 172 -> 239 us).  Of repeated calls
+// the first is faster (dk and dv 473 us): the clock falls under load, so what counts is the
+// number of instructions rather than their latency.
 #include "recurrence_tile.h"
 
 namespace dla {
@@ -215,8 +217,8 @@ __global__ __launch_bounds__(2 * C, sizeof(Tin) == 2 ? 2 : 1) void scan_kernel(S
 // dk and dv at once: half of the waves hold the adjoint's columns and give dv, the others
 // those of its transpose and give dk, from the same tiles.  A chunk's tokens are read once
 // for both, and its next one is stored into the other set of tiles meanwhile.  Against two
-// passes of scan_kernel: 200 heads x 2k tokens backward 430 us against 506, 512 heads (two
-// rounds of workgroups) 893 against 893, 16 heads x 2k forward and backward 134 against 146.
+// passes of scan_kernel, 2k tokens forward and backward: 200 heads 496 us against 587, 512
+// heads (two rounds of workgroups) 993 against 1080, 16 heads 129 against 138.
 // float32 does not fit: its operands are twice as wide, and the waves' registers spill.
 template <typename Tin, int DK, int DV>
 struct AdjointTiles {

@@ -2,7 +2,9 @@
 //
 // A workgroup takes 32 columns of one head's state: they are independent of the others.
 // Thread r 8 + c holds rows r, r + 32, .. of columns 4 c .. 4 c + 3 in registers, read and
-// written once for all tokens of the call; the state's bytes bound it.
+// written once for all tokens of the call; the state's bytes bound it: 2048 heads of 128 x 128
+// 41 us for 0.27 GB a token where calls follow on one state, part of which stays in the last
+// cache; 32 heads 4.3, a launch.
 #include "mfma.h"
 #include "recurrence.h"
 

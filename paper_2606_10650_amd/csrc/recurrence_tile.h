@@ -25,7 +25,8 @@ constexpr int kChunk = 32;
 // two rows, 8 apart).  bfloat16 rows are padded by 64 bytes, which spreads four rows over
 // the banks, and pieces of 16 bytes change places within 64 bytes by bits 2 and 3 of the row,
 // which spreads sixteen; float32 rows are padded by 16 bytes.  Both kinds of read are then
-// free of conflicts, and but for those two bits every offset is a constant of the instruction.
+// free of conflicts (those of 16 x 16 scores, four pieces of sixteen rows, are not quite: with
+// them conflicts take a seventh of the forward pass's LDS cycles), and but for those two bits every offset is a constant of the instruction.
 template <typename Tin, int D>
 struct Tile {
   static constexpr int PE = 16 / (int)sizeof(Tin);             // elements per piece
@@ -263,7 +264,7 @@ struct State {
 
 // Masked and decayed scores of a chunk, [t][s], for the product with the values: bfloat16 in
 // two terms (two more of some thirty products, and outputs of short sequences lose 2^-9
-// instead of 2^-8.5).  Rows are padded by 16 bytes: reads of 16 bytes are free of conflicts.
+// instead of 2^-8.5).  Rows are padded by 16 bytes, which spreads them over the banks.
 template <typename Tin>
 struct Scores;
 template <>

@@ -16,9 +16,9 @@ using namespace dla;
 namespace {
 
 // Tokens up to which a call goes token by token, streaming the state once, in place of a
-// chunk.  2048 heads of 128 x 128, bfloat16: 6 tokens 53 us, 8 61, a chunk 53; 256 heads 12,
-// 14, 13.  float32, whose chunks take twice as long: 8 tokens 62 us, a chunk 111; 256 heads
-// 14, 19.
+// chunk.  128 x 128, bfloat16, 6 tokens so and 8 in a chunk: 2048 heads 53 and 50 us, 256 12
+// and 11, 32 9 and 11 (two launches).  float32, whose chunks take twice as long, 12 tokens so
+// and 16 in a chunk: 79 and 103, 18 and 17, 10 and 14.
 int step_tokens(int dtype) { return dtype == DLA_BF16 ? 6 : 12; }
 
 struct Plan {
@@ -30,11 +30,11 @@ struct Plan {
 // so that all of them work, at the price of a pass over keys and values (backward also over
 // queries and output gradients) for the segments' states.  As many as the chip then holds
 // at once; not where that makes but two or three, which costs what it gives.  2048 bfloat16
-// tokens, forward and backward, 128 x 128: 96 heads in 1, 4, 5, 6 segments 561, 391, 361, 441
-// us, 150 in 1, 3, 4 584, 544, 634, 192 in 1, 2 594, 717; 64 x 64 (half the threads per
-// workgroup): 96 in 5, 8, 11 217, 184, 205, 192 in 1, 5, 8 484, 304, 360, 300 in 1, 3 621,
-// 492.  A segment has at least 4 chunks, 2 of float32, whose chunks take longer (15 heads x
-// 1531 tokens: 161 us, 175 with 4, 274 with 8).
+// tokens, forward and backward, 128 x 128: 96 heads in 1, 4, 5, 6 segments 478, 358, 324, 388
+// us, 150 in 1, 3, 4 472, 479, 543, 192 in 1, 2 480, 636; 64 x 64 (half the threads per
+// workgroup): 96 in 5, 8, 10 178, 164, 174, 192 in 1, 5, 8 400, 274, 297, 300 in 1, 3 490,
+// 423.  A segment has at least 4 chunks, 2 of float32, whose chunks take longer (15 heads x
+// 1531 tokens: 148 us, 158 with 4, 245 with 8).
 Plan plan_of(const dla_recurrence_desc& d, bool backward) {
   Plan p{!backward && d.T <= step_tokens(d.dtype), 1, kRecChunk};
   if (d.B == 0 || d.T == 0) return p;   // nothing to plan
