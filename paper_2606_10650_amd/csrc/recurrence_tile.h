@@ -26,7 +26,8 @@ constexpr int kChunk = 32;
 // the banks, and pieces of 16 bytes change places within 64 bytes by bits 2 and 3 of the row,
 // which spreads sixteen; float32 rows are padded by 16 bytes.  Both kinds of read are then
 // free of conflicts (those of 16 x 16 scores, four pieces of sixteen rows, are not quite: with
-// them conflicts take a seventh of the forward pass's LDS cycles), and but for those two bits every offset is a constant of the instruction.
+// them conflicts take a seventh of the forward pass's LDS cycles), and but for those two bits
+// every offset is a constant of the instruction.
 template <typename Tin, int D>
 struct Tile {
   static constexpr int PE = 16 / (int)sizeof(Tin);             // elements per piece
