@@ -129,8 +129,9 @@ dla_status dla_rms_norm(const dla_norm_desc* desc, const dla_norm_rows* x,
 
 /* The same with y in 8-bit floating point (4 exponent and 3 mantissa bits, largest
  * value 448, no infinity) and a float32 scale per row: y_scale = max |y| / 448, the
- * codes are y / y_scale rounded to nearest even.  A row of zeros has scale and codes
- * zero; a row with an infinity or NaN has NaN codes. */
+ * codes are y / y_scale rounded to nearest even.  A row whose max |y| is below 448 times
+ * the smallest normal float32 (5.3e-36) has scale and codes zero; a row with an infinity
+ * or NaN has NaN codes. */
 dla_status dla_rms_norm_fp8(const dla_norm_desc* desc, const dla_norm_rows* x,
                             const dla_norm_rows* residual, const void* weight,
                             const dla_norm_rows* h, const dla_norm_rows* y, float* y_scale,

@@ -127,6 +127,10 @@ __device__ __forceinline__ float over_row(float x, float* lds) {
   return x;
 }
 
+// A row whose largest |y| is below this, 448 times the smallest normal float32, is all zero
+// in 8 bits: its scale would have fewer bits, and 448 / top no finite value.
+constexpr float kLeastTop = 448.f * 0x1p-126f;
+
 template <typename T, int NT, int NP, bool F8>
 __global__ __launch_bounds__(NT > 256 ? NT : 256) void norm_kernel(NormArgs a) {
   constexpr int N = Piece<T>::N, PER = NT > 256 ? 1 : 256 / NT;
@@ -175,8 +179,8 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void norm_kernel(NormArgs a) {
   }
   if constexpr (F8) {
     top = over_row<NT, true>(top, lds);
-    if (tid == 0) a.y_scale[row] = top / 448.f;
-    const float inv = top > 0.f ? 448.f / top : (top == 0.f ? 0.f : top);
+    if (tid == 0) a.y_scale[row] = top < kLeastTop ? 0.f : top / 448.f;
+    const float inv = top < kLeastTop ? 0.f : 448.f / top;   // (a NaN stays one)
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int c = (i * NT + tid) * N, n = a.D - c;
