@@ -106,7 +106,9 @@ dla_status dla_recurrence_backward(const dla_recurrence_desc* desc, const dla_ro
  * least D) and contiguous in themselves, at any alignment of their type.  dtype: type
  * of x, residual, h, y and their gradients; weight_dtype: that type or DLA_F32.
  * Everything is computed in float32 from the unrounded sum x + residual and rounded
- * once when it is stored.
+ * once when it is stored.  eps >= 0; r is right for any finite x + residual in float32,
+ * and zero for a row of which mean(h^2) + eps is below 2^-252 (eps = 0 and a row of zeros
+ * or of numbers below the normal ones): y is then zero, and h's only gradient is its own.
  */
 typedef struct {
   int64_t rows;

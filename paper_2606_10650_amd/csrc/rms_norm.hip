@@ -152,13 +152,27 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void norm_kernel(NormArgs a) {
 #pragma unroll
         for (int j = 0; j < N; ++j) h[i][j] += r[j];
       }
-      load_weight<T>(a, c, n, w[i]);
+      if constexpr (NT <= 256) load_weight<T>(a, c, n, w[i]);
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) sum += h[i][j] * h[i][j];
   }
   sum = over_row<NT, false>(sum, lds);
-  const float rstd = 1.f / sqrtf(sum / (float)a.D + a.eps);
+  float ms = sum / (float)a.D + a.eps, rstd = 1.f / sqrtf(ms);
+  if (!(ms >= 0x1p-100f && ms <= 0x1.fffffep127f)) {
+    // Squares that leave float32's range, in all threads of the row or in none: once more
+    // with the row scaled by a power of two.  (An infinity or NaN in the row stays one.)
+    const float f = ms < 1.f ? 0x1p100f : 0x1p-80f;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum += (h[i][j] * f) * (h[i][j] * f);
+    ms = over_row<NT, false>(sum, lds) / (float)a.D + a.eps * f * f;
+    // below 2^-126 in root mean square, which eps = 0 or a subnormal one allows, r has no
+    // finite value
+    rstd = ms < 0x1p-52f ? 0.f : f / sqrtf(ms);
+  }
   if (a.rstd && tid == 0) a.rstd[row] = rstd;
   float top = 0.f;
 #pragma unroll
@@ -166,6 +180,8 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void norm_kernel(NormArgs a) {
     const int c = (i * NT + tid) * N, n = a.D - c;
     if (n > 0) {
       if (a.h.p) Piece<T>::store(static_cast<T*>(a.h.p) + row * a.h.st + c, n, h[i]);
+      // (1024 threads need 64 registers or fewer for two workgroups a compute unit)
+      if constexpr (NT > 256) load_weight<T>(a, c, n, w[i]);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         h[i][j] = h[i][j] * rstd * w[i][j];
