@@ -15,6 +15,7 @@ import struct
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import dla
 from .dla import DLA_BF16, DLA_F32, _check, _dtype_code
@@ -342,7 +343,8 @@ class AdamW:
 
 
 # ---------------------------------------------------------------------------
-# the same for torch's automatic differentiation
+# the same for torch's automatic differentiation, once: the library has no second
+# derivatives, and asking for one raises an error
 # ---------------------------------------------------------------------------
 def _as_rows(t):
     """A gradient as the library reads it: last axis contiguous, rows 16-byte aligned."""
@@ -365,6 +367,7 @@ class Recurrence(torch.autograd.Function):
         return out, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dlast):
         q, k, v, g, state, lengths = ctx.saved_tensors
         dout = torch.zeros_like(v) if dout is None else _as_rows(dout.to(v.dtype))
@@ -387,6 +390,7 @@ class RMSNorm(torch.autograd.Function):
         return y.view(x.shape), h.view(x.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh):
         h, weight, rstd = ctx.saved_tensors
         rows = lambda t: t.reshape(h.shape).to(h.dtype)  # noqa: E731
