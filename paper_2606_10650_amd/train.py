@@ -377,6 +377,14 @@ class Recurrence(torch.autograd.Function):
         return dq, dk, dv, dg.to(g.dtype), ds, None, None
 
 
+def _as_norm_rows(t, D):
+    """The rows [N, D] of a tensor as the library reads them: contiguous, and apart."""
+    t = t.reshape(-1, D)
+    if (D > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < D):
+        t = t.contiguous()       # broadcast or transposed
+    return t
+
+
 class RMSNorm(torch.autograd.Function):
     """y, h = RMSNorm.apply(x, residual, weight, eps): h = x + residual, y its norm."""
 
@@ -393,7 +401,7 @@ class RMSNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy, dh):
         h, weight, rstd = ctx.saved_tensors
-        rows = lambda t: t.reshape(h.shape).to(h.dtype)  # noqa: E731
+        rows = lambda t: _as_norm_rows(t.to(h.dtype), h.shape[1])  # noqa: E731
         dy = torch.zeros_like(h) if dy is None else rows(dy)
         dx, dw = rms_norm_backward(dy, h, weight, rstd, dres=None if dh is None else rows(dh))
         dx = dx.view(ctx.shape)

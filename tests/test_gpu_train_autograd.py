@@ -39,3 +39,27 @@ def test_second_derivatives_are_refused():
     (g,) = torch.autograd.grad((out ** 3).sum() + (last ** 3).sum(), ins[0], create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         g.square().sum().backward()
+
+
+def _norm64(x, r, w):
+    h = x + r
+    return h / (h.square().mean(-1, keepdim=True) + 1e-6).sqrt() * w, h
+
+
+@pytest.mark.parametrize("loss", [
+    lambda y, h: y.sum(),                                       # one number for all
+    lambda y, h: y.mean() + h.mean(),
+    lambda y, h: (y.sum(0) * torch.arange(96, device="cuda")).sum() + h.sum(1)[0],   # one row for all tokens
+    lambda y, h: (y.sum(1) * torch.arange(6, device="cuda")).sum(),                  # one number a row
+    lambda y, h: (y.t() * torch.arange(6, device="cuda")).sin().sum(),               # transposed
+    lambda y, h: torch.cat([torch.zeros(3, device="cuda"), y.flatten(), h.flatten()]).cos().sum(),
+], ids=["sum", "mean", "tokens", "rows", "transposed", "cat"])
+def test_norm_takes_any_gradient(loss):
+    tr = _train()
+    ins = _norm_inputs()
+    loss(*tr.RMSNorm.apply(*ins)).backward()
+    exact = [x.detach().double().requires_grad_() for x in ins]
+    loss(*_norm64(*exact)).backward()
+    for x, e in zip(ins, exact):
+        # cos and sin turn 1e-5 of their argument into as much of themselves at most
+        assert (x.grad.double() - e.grad).norm() <= 4e-5 * e.grad.norm() + 1e-6
