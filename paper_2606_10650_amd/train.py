@@ -350,7 +350,8 @@ def _as_rows(t):
     """A gradient as the library reads it: last axis contiguous, rows 16-byte aligned."""
     e = t.element_size()
     if t.stride(-1) != 1 or t.data_ptr() % 16 or any(s * e % 16 for s in t.stride()[:-1]):
-        return t.contiguous()
+        # (contiguous() would hand back a contiguous view at any address)
+        return t.clone(memory_format=torch.contiguous_format)
     return t
 
 
@@ -372,7 +373,7 @@ class Recurrence(torch.autograd.Function):
         q, k, v, g, state, lengths = ctx.saved_tensors
         dout = torch.zeros_like(v) if dout is None else _as_rows(dout.to(v.dtype))
         dq, dk, dv, dg, ds = recurrence_backward(q, k, v, g, dout, scale=ctx.scale, state=state,
-                                                 dstate=None if dlast is None else dlast.contiguous(),
+                                                 dstate=None if dlast is None else _as_rows(dlast).contiguous(),
                                                  lengths=lengths)
         return dq, dk, dv, dg.to(g.dtype), ds, None, None
 

@@ -63,3 +63,37 @@ def test_norm_takes_any_gradient(loss):
     for x, e in zip(ins, exact):
         # cos and sin turn 1e-5 of their argument into as much of themselves at most
         assert (x.grad.double() - e.grad).norm() <= 4e-5 * e.grad.norm() + 1e-6
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shift", [1, 2, 5])
+def test_recurrence_takes_gradients_at_any_address(shift, dtype):
+    """The gradients of `out` and of the last state as views of a longer vector's, at odd
+    elements: the same bits as from tensors of their own."""
+    tr = _train()
+    ins = _recurrence_inputs(dtype=dtype)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda x: torch.randn(x.shape, generator=gen, device="cuda").to(x.dtype)  # noqa: E731
+    pad = torch.zeros(shift, device="cuda")
+    out, last = tr.Recurrence.apply(*ins, 0.5, None)
+    do, dS = rnd(out), rnd(last)
+    # each cat's backward pass hands out a narrow part of its gradient
+    loss = (torch.cat([pad.to(dtype), out.flatten()]) * torch.cat([pad.to(dtype), do.flatten()])).sum() + \
+        (torch.cat([pad, last.flatten()]) * torch.cat([pad, dS.flatten()])).sum()
+    loss.backward()
+    with torch.no_grad():
+        want = tr.recurrence_backward(*ins[:4], do, scale=0.5, state=ins[4], dstate=dS)
+    for x, y in zip(ins, want):
+        assert torch.equal(x.grad, y.to(x.dtype))
+
+
+def test_recurrence_takes_broadcast_gradients():
+    tr = _train()
+    ins = _recurrence_inputs()
+    out, last = tr.Recurrence.apply(*ins, 0.5, None)
+    (out.sum(2).sum() + 2 * last.sum()).backward()
+    with torch.no_grad():
+        want = tr.recurrence_backward(*ins[:4], torch.ones_like(out), scale=0.5, state=ins[4],
+                                      dstate=torch.full_like(last, 2.0))
+    for x, y in zip(ins, want):
+        assert torch.equal(x.grad, y)
