@@ -392,7 +392,7 @@ class RMSNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, weight, eps=1e-6):
         D = x.shape[-1]
-        y, h, rstd = rms_norm(x.reshape(-1, D), weight, residual.reshape(-1, D), eps=eps)
+        y, h, rstd = rms_norm(_as_norm_rows(x, D), weight, _as_norm_rows(residual, D), eps=eps)
         ctx.save_for_backward(h, weight, rstd)
         ctx.shape = x.shape
         ctx.set_materialize_grads(False)

@@ -97,3 +97,21 @@ def test_recurrence_takes_broadcast_gradients():
                                       dstate=torch.full_like(last, 2.0))
     for x, y in zip(ins, want):
         assert torch.equal(x.grad, y)
+
+
+def test_norm_takes_broadcast_inputs():
+    """One row for all tokens, as x, as the residual, and transposed ones: the gradient is
+    summed over what it was broadcast to."""
+    tr = _train()
+    x, r, w = _norm_inputs()
+    dy = torch.randn(x.shape, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")
+    row = x.detach()[0].clone().requires_grad_()
+    turned = x.detach().t().contiguous().requires_grad_()
+    for a, b, leaf in ((row.expand(6, 96), r, row), (r, row.expand(6, 96), row), (turned.t(), r, turned)):
+        leaf.grad = None
+        (tr.RMSNorm.apply(a, b, w)[0] * dy).sum().backward()
+        L = leaf.detach().double().requires_grad_()
+        wide = L.t() if leaf is turned else L.expand(6, 96)
+        (_norm64(*((wide, r.detach().double()) if a is not r else (r.detach().double(), wide)),
+                 w.detach().double())[0] * dy).sum().backward()
+        assert (leaf.grad.double() - L.grad).norm() <= 1e-5 * L.grad.norm()
