@@ -387,16 +387,18 @@ def _as_norm_rows(t, D):
 
 
 class RMSNorm(torch.autograd.Function):
-    """y, h = RMSNorm.apply(x, residual, weight, eps): h = x + residual, y its norm."""
+    """y, h = RMSNorm.apply(x, residual, weight, eps): h = x + residual, y its norm.
+    residual may be None: h is then x."""
 
     @staticmethod
     def forward(ctx, x, residual, weight, eps=1e-6):
         D = x.shape[-1]
-        y, h, rstd = rms_norm(_as_norm_rows(x, D), weight, _as_norm_rows(residual, D), eps=eps)
+        y, h, rstd = rms_norm(_as_norm_rows(x, D), weight,
+                              None if residual is None else _as_norm_rows(residual, D), eps=eps)
         ctx.save_for_backward(h, weight, rstd)
-        ctx.shape = x.shape
+        ctx.shape, ctx.residual = x.shape, residual is not None
         ctx.set_materialize_grads(False)
-        return y.view(x.shape), h.view(x.shape)
+        return y.view(x.shape), h.view(x.shape) if ctx.residual else x
 
     @staticmethod
     @once_differentiable
@@ -406,4 +408,4 @@ class RMSNorm(torch.autograd.Function):
         dy = torch.zeros_like(h) if dy is None else rows(dy)
         dx, dw = rms_norm_backward(dy, h, weight, rstd, dres=None if dh is None else rows(dh))
         dx = dx.view(ctx.shape)
-        return dx, dx, dw.to(weight.dtype), None
+        return dx, dx if ctx.residual else None, dw.to(weight.dtype), None

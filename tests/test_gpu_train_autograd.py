@@ -115,3 +115,26 @@ def test_norm_takes_broadcast_inputs():
         (_norm64(*((wide, r.detach().double()) if a is not r else (r.detach().double(), wide)),
                  w.detach().double())[0] * dy).sum().backward()
         assert (leaf.grad.double() - L.grad).norm() <= 1e-5 * L.grad.norm()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("use_h", [False, True])
+def test_norm_without_a_residual(use_h, dtype):
+    """h is x itself; the gradients are those of x as the residual of zeros, bit by bit."""
+    tr = _train()
+    x, _, w = (t.detach().to(dtype).requires_grad_() for t in _norm_inputs())
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    dy, dh = (torch.randn(x.shape, generator=gen, device="cuda").to(dtype) for _ in range(2))
+    got = []
+    for a, b in ((x, None), (torch.zeros_like(x), x)):
+        x.grad = w.grad = None
+        y, h = tr.RMSNorm.apply(a, b, w)
+        assert torch.equal(h, x)
+        ((y * dy).sum() + ((h * dh).sum() if use_h else 0)).backward()
+        got.append((y.detach(), x.grad, w.grad))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    # h stands for x in what follows it
+    with torch.no_grad():
+        y, h = tr.RMSNorm.apply(x.detach().view(2, 3, 96), None, w.detach())
+        assert y.shape == h.shape == (2, 3, 96) and h.data_ptr() == x.data_ptr()
