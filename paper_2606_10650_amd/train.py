@@ -276,16 +276,21 @@ def rms_norm_backward(dy, h, weight, rstd, dres=None, *, workspace=None):
 # ---------------------------------------------------------------------------
 class AdamW:
     """AdamW over many tensors at once (dla_adamw_step).  `add` names a tensor and its
-    buffers, which the caller keeps; `step` updates all of them in place on the current
-    stream.  Without m and v, `add` makes their states, zeroed, in the given format.
-    Tensors may differ in type; those of a kind go in the same launches."""
+    buffers, which are kept; `step` updates all of them in place on the current stream.
+    Without m and v, `add` makes their states, zeroed, in the given format.  Tensors may
+    differ in type; those of a kind go in the same launches.
+
+    Every step works on the memory that the tensors have then: one whose `.data` was
+    replaced is followed.  So is a gradient that is `param.grad` when it is added: each step
+    takes what `param.grad` then is, so that gradients may be set to None and made anew by
+    the next backward pass.  Any other gradient tensor is a buffer for the caller to fill."""
 
     def __init__(self, states: str = "f32"):
         if states not in ("f32", "fp8"):
             raise ValueError(f"states {states!r}: f32 or fp8")
         self.states = states
         self.kept = []       # the tensors of each entry
-        self._groups = {}    # (param, grad type, format) -> entries
+        self._groups = {}    # (param, grad type, format, device) -> entries
         self._arrays = None
 
     def add(self, param, grad, m=None, v=None, *, master=None, m_scale=None, v_scale=None,
@@ -302,27 +307,70 @@ class AdamW:
             raise ValueError(f"states of types {m.dtype}, {v.dtype}")
         if fp8 and (m_scale is None or v_scale is None):
             raise ValueError("8-bit states need their scales")
-        sizes = [(param, n, None), (grad, n, None), (m, n, None), (v, n, None),
-                 (master, n, torch.float32)]
-        if fp8:
-            sizes += [(t, -(-n // FP8_BLOCK), torch.float32) for t in (m_scale, v_scale)]
-        for t, size, dtype in sizes:
-            if t is not None and (t.numel() != size or not t.is_contiguous() or t.device != dev or
-                                  (dtype is not None and t.dtype != dtype)):
-                raise ValueError(f"a buffer of {t.numel()} {t.dtype} on {t.device} where {size} "
-                                 f"contiguous elements on {dev} are wanted")
+        blocks = -(-n // FP8_BLOCK)
+        # in the order of dla_adamw_tensor
+        buffers = [(param, n, param.dtype), (master, n, torch.float32), (grad, n, grad.dtype),
+                   (m, n, m.dtype), (v, n, m.dtype)]
+        buffers += [(t if fp8 else None, blocks, torch.float32) for t in (m_scale, v_scale)]
+        for t, size, dtype in buffers:
+            if t is not None:
+                self._fits(t, size, dtype, dev)
+        own = param.grad if param.is_leaf else None
+        follow = own is not None and own.data_ptr() == grad.data_ptr()
+        if follow:
+            buffers[2] = (None, n, grad.dtype)     # not kept: it may be freed between steps
         key = (_dtype_code(param.dtype), _dtype_code(grad.dtype), DLA_STATE_FP8 if fp8 else DLA_F32, dev)
-        self._groups.setdefault(key, []).append(
-            (param, master, grad, m, v, m_scale if fp8 else None, v_scale if fp8 else None, n,
-             float(weight_decay)))
+        self._groups.setdefault(key, []).append((buffers, n, float(weight_decay), follow))
         self.kept.append({"param": param, "master": master, "m": m, "v": v, "m_scale": m_scale,
                           "v_scale": v_scale})
         self._arrays = None
 
+    @staticmethod
+    def _fits(t, size, dtype, dev):
+        if t.numel() != size or not t.is_contiguous() or t.device != dev or t.dtype != dtype:
+            raise ValueError(f"a buffer of {t.numel()} {t.dtype} on {t.device} where {size} "
+                             f"contiguous {dtype} on {dev} are wanted")
+
     def _marshal(self):
-        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        self._arrays = [(key, (AdamWTensor * len(ts))(*[AdamWTensor(*map(ptr, t[:7]), *t[7:]) for t in ts]))
-                        for key, ts in self._groups.items()]
+        """The descriptions of all tensors.  `_tensors`: those kept that have an address in one;
+        `_followed`: the parameters whose gradients have, behind them; `_slots`: where each
+        address goes and what its tensor has to be; `_at`: the addresses there."""
+        self._tensors, self._followed, slots, gradients, arrays = [], [], [], [], []
+        for key, entries in self._groups.items():
+            array = (AdamWTensor * len(entries))()
+            for i, (buffers, n, decay, follow) in enumerate(entries):
+                array[i] = AdamWTensor(*[_ptr(t) for t, _, _ in buffers], n, decay)
+                for (field, _), (t, size, dtype) in zip(AdamWTensor._fields_, buffers):
+                    if t is not None:
+                        self._tensors.append(t)
+                        slots.append((array[i], field, size, dtype, key[3]))
+                if follow:
+                    self._followed.append(buffers[0][0])
+                    gradients.append((array[i], "grad", *buffers[2][1:], key[3]))
+            arrays.append((key, array))
+        self._slots = slots + gradients
+        self._at = list(map(_ptr, self._tensors)) + [None] * len(gradients)
+        self._arrays = arrays
+
+    def _refresh(self):
+        """Addresses as they are now."""
+        now = list(map(torch.Tensor.data_ptr, self._tensors))
+        for param, (_, _, size, dtype, dev) in zip(self._followed, self._slots[len(now):]):
+            grad = param.grad
+            if grad is None:
+                raise ValueError(f"a parameter of shape {tuple(param.shape)} has no gradient")
+            self._fits(grad, size, dtype, dev)
+            now.append(grad.data_ptr())
+        if now != self._at:
+            for i, (x, was) in enumerate(zip(now, self._at)):
+                if x != was:
+                    slot, field, size, dtype, dev = self._slots[i]
+                    if i < len(self._tensors):
+                        self._fits(self._tensors[i], size, dtype, dev)
+                    if size and not x:
+                        raise ValueError("a buffer without memory")
+                    setattr(slot, field, x)
+                    self._at[i] = x
 
     def step(self, step: int, *, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, seed: int = 0,
              grad_scale=None):
@@ -331,6 +379,7 @@ class AdamW:
         it is not finite."""
         if self._arrays is None:
             self._marshal()
+        self._refresh()
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32")
         for (p, g, fmt, dev), arr in self._arrays:

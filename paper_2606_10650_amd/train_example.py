@@ -33,7 +33,7 @@ class Model:
             p = master.to(torch.bfloat16).requires_grad_()
             p.grad = torch.zeros_like(p)
             self.params[name], self.masters[name] = p, master
-            self.opt.add(p.detach(), p.grad, master=master, weight_decay=decay)
+            self.opt.add(p, p.grad, master=master, weight_decay=decay)
 
         add("embed", vocab, width, std=0.5)
         for i in range(layers):
@@ -98,7 +98,7 @@ class Model:
         self.opt.step(t, lr=lr, betas=(0.9, 0.98), seed=t if self.opt.states == "fp8" else 0,
                       grad_scale=(1.0 / norm.clamp(min=1.0)).reshape(1))
         for p in self.params.values():
-            p.grad.zero_()
+            p.grad = None
 
 
 def recall(B, pairs, queries, keys, values, gen):
