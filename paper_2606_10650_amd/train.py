@@ -302,6 +302,8 @@ class AdamW:
                 m_scale, v_scale = (torch.zeros(-(-n // FP8_BLOCK), device=dev) for _ in range(2))
             else:
                 m, v = (torch.zeros(n, device=dev) for _ in range(2))
+        elif m is None or v is None:
+            raise ValueError("m and v come together")
         fp8 = m.dtype == FP8
         if v.dtype != m.dtype or m.dtype not in (torch.float32, FP8):
             raise ValueError(f"states of types {m.dtype}, {v.dtype}")
