@@ -102,7 +102,7 @@ dla_status dla_recurrence_backward(const dla_recurrence_desc* desc, const dla_ro
 /*
  * Root-mean-square norm of a residual stream.  Per row of D values:
  *   h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = r h weight
- * rows >= 0 rows, 1 <= D <= 16384, each array's rows `stride` elements apart (at
+ * 0 <= rows <= 2^31 - 4 rows, 1 <= D <= 16384, each array's rows `stride` elements apart (at
  * least D) and contiguous in themselves, at any alignment of their type.  dtype: type
  * of x, residual, h, y and their gradients; weight_dtype: that type or DLA_F32.
  * Everything is computed in float32 from the unrounded sum x + residual and rounded

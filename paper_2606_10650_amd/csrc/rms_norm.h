@@ -7,6 +7,12 @@ namespace dla {
 struct NormRows {
   void* p = nullptr;
   int64_t st = 0;   // elements from row to row
+  // the rows from one on, of elements of the given size
+  NormRows from(int64_t row, int elem) const {
+    NormRows r = *this;
+    if (p) r.p = static_cast<char*>(p) + row * st * elem;
+    return r;
+  }
 };
 
 struct NormArgs {

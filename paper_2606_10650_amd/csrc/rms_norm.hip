@@ -329,10 +329,24 @@ __global__ __launch_bounds__(1024) void dw_kernel(const float* part, int parts, 
 template <typename T, int NT, int NP>
 hipError_t go(const NormArgs& a, int kind, hipStream_t st) {
   constexpr int PER = NT > 256 ? 1 : 256 / NT, BLOCK = NT > 256 ? NT : 256;
-  const dim3 grid((unsigned)((a.rows + PER - 1) / PER)), block(BLOCK);
-  if (kind == 0) hipLaunchKernelGGL((norm_kernel<T, NT, NP, false>), grid, block, 0, st, a);
-  else if (kind == 1) hipLaunchKernelGGL((norm_kernel<T, NT, NP, true>), grid, block, 0, st, a);
-  else if (sizeof(T) == 2 && !a.w_f32) hipLaunchKernelGGL((norm_backward_kernel<T, NT, NP, false>), dim3(a.groups), block, 0, st, a);
+  const dim3 block(BLOCK);
+  if (kind < 2) {
+    // a launch has fewer than 2^32 threads
+    constexpr int64_t most = 0xFFFFFFFFll / BLOCK * PER;
+    NormArgs part = a;
+    for (int64_t row = 0; row < a.rows; row += most) {
+      part.rows = a.rows - row < most ? a.rows - row : most;
+      part.x = a.x.from(row, sizeof(T));
+      part.res = a.res.from(row, sizeof(T));
+      part.h = a.h.from(row, sizeof(T));
+      part.y = a.y.from(row, kind == 1 ? 1 : sizeof(T));
+      part.rstd = a.rstd ? a.rstd + row : nullptr;
+      part.y_scale = a.y_scale ? a.y_scale + row : nullptr;
+      const dim3 grid((unsigned)((part.rows + PER - 1) / PER));
+      if (kind == 0) hipLaunchKernelGGL((norm_kernel<T, NT, NP, false>), grid, block, 0, st, part);
+      else hipLaunchKernelGGL((norm_kernel<T, NT, NP, true>), grid, block, 0, st, part);
+    }
+  } else if (sizeof(T) == 2 && !a.w_f32) hipLaunchKernelGGL((norm_backward_kernel<T, NT, NP, false>), dim3(a.groups), block, 0, st, a);
   else hipLaunchKernelGGL((norm_backward_kernel<T, NT, NP, true>), dim3(a.groups), block, 0, st, a);
   return hipGetLastError();
 }

@@ -100,3 +100,32 @@ def test_rows_of_zeros_without_eps(D, dtype):
     assert rstd.tolist() == [1, 0, 1] and not y[1].any() and (y[::2] == 1).all()
     assert not codes[1].float().any() and scale[1] == 0 and (codes[::2].float() == 448).all()
     assert (dx[1] == 3).all() and (dw == 2).all()
+
+
+def test_more_rows_than_a_launch_takes():
+    """2^26 + 3 short rows, one wave each: more than 2^32 threads."""
+    tr = _train()
+    N, D = 2 ** 26 + 3, 2
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((N, D), generator=gen, device="cuda", dtype=torch.bfloat16)
+    r = torch.randn((N, D), generator=gen, device="cuda", dtype=torch.bfloat16)
+    w = torch.tensor([1.0, -2.0], device="cuda", dtype=torch.bfloat16)
+    H = x.float() + r.float()
+    R = 1 / (H.square().mean(-1) + 1e-6).sqrt()
+    y, h, rstd = tr.rms_norm(x, w, r)
+    assert torch.equal(h, H.bfloat16())
+    assert ((rstd - R).abs() <= 1e-5 * R).all()
+    want = H * R[:, None] * w.float()
+    assert ((y.float() - want).abs() <= (2.0 ** -8 + 1e-5) * want.abs()).all()
+    del rstd, y, h
+    codes, h, scale = tr.rms_norm_fp8(x, w, r)
+    assert torch.equal(h, H.bfloat16())
+    top = want.abs().amax(-1)
+    assert ((scale - top / 448).abs() <= 1e-5 * top / 448).all()
+    off = (codes.float() * scale[:, None] - want).abs()
+    assert (off <= want.abs() * (2.0 ** -4 + 1e-5) + scale[:, None] * 2.0 ** -10).all()
+    dx, dw = tr.rms_norm_backward(y := want.bfloat16(), h, w, R)
+    torch.cuda.synchronize()
+    n, dn = h.float() * R[:, None], y.float() * w.float()
+    want = (dn - n * (dn * n).mean(-1, keepdim=True)) * R[:, None]
+    assert ((dx.float() - want).abs() <= (2.0 ** -8 + 1e-5) * (dn.abs().amax(-1) * R)[:, None] * 2).all()
