@@ -158,7 +158,7 @@ dla_status dla_rms_norm_backward(const dla_norm_desc* desc, const dla_norm_rows*
  *   p = p (1 - lr weight_decay) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
  * in float32.  p is master where that is given (param is then its rounded copy and
  * only written), else param.  No alignment is needed beyond the types'; 16-byte aligned
- * tensors are faster.  A tensor may have no elements.  Tensors must not overlap.
+ * tensors are faster.  A tensor has 0 to 2^36 - 4096 elements.  Tensors must not overlap.
  *
  * state_format DLA_F32: m, v are float32 [n].  DLA_STATE_FP8: m and v are 8-bit codes
  * [n] of m and of sqrt(v), in the floating point format of dla_rms_norm_fp8, times

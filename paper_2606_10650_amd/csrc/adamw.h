@@ -5,6 +5,8 @@
 
 namespace dla {
 
+constexpr int64_t kAdamWMost = ((int64_t)1 << 36) - 4096;   // elements of a tensor
+
 struct AdamWScalars {
   float beta1, rest1, beta2, rest2;   // rest = 1 - beta
   float lr, step_size;                // lr / (1 - beta1^step)

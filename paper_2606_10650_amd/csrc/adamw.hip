@@ -22,6 +22,8 @@ namespace {
 constexpr int kTensors = 40;
 constexpr int kChunk = 4096;
 constexpr int kBlock = 256;
+constexpr uint64_t kGroups = 0xFFFFFFFFu / 256;   // a launch has fewer than 2^32 threads
+static_assert(kAdamWMost / kChunk <= kGroups, "a tensor fits one launch");
 
 struct Table {
   dla_adamw_tensor t[kTensors];
@@ -251,7 +253,7 @@ hipError_t launch_adamw(const dla_adamw_tensor* t, int n, const AdamWScalars& s,
       tab.first[k] = (uint32_t)grid;
       if (i + k < n) {
         const uint64_t groups = (uint64_t)((t[i + k].n + kChunk - 1) / kChunk);
-        if (grid + groups > 0x7FFFFFFFu) break;   // the rest goes by the next launch
+        if (grid + groups > kGroups) break;   // the rest goes by the next launch
         tab.t[k] = t[i + k];
         grid += groups;
       }

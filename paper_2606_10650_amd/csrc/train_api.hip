@@ -396,6 +396,7 @@ dla_status dla_adamw_step(const dla_adamw_tensor* tensors, int32_t n, const dla_
   for (int32_t i = 0; i < n; ++i) {
     const dla_adamw_tensor& t = tensors[i];
     if (t.n < 0 || t.n > ((int64_t)1 << 40) || !isfinite(t.weight_decay)) return remember(DLA_ERR_INVALID_ARG);
+    if (t.n > kAdamWMost) return remember(DLA_ERR_UNSUPPORTED);
     if (t.n == 0) continue;
     if (!t.param || !t.grad || !t.m || !t.v || (f8 && (!t.m_scale || !t.v_scale)))
       return remember(DLA_ERR_INVALID_ARG);
