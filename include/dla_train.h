@@ -44,8 +44,9 @@ typedef struct {
  * It is dla_prefill with C = 1 and lambda = scale, as an operator of its own that
  * can be differentiated: with no scores, decisions or cache around it.
  *
- * B, T >= 0 sequences and tokens; H heads, which share Hk <= H key heads (H a
- * multiple of Hk): head h has the queries and keys of head h / (H / Hk).  d_k,
+ * B, T >= 0 sequences and tokens, T <= 2^30; H heads, which share Hk <= H key heads (H
+ * a multiple of Hk): head h has the queries and keys of head h / (H / Hk).  B H is at
+ * most 65535, in a forward call of up to 6 tokens 2^21 - 1.  d_k,
  * d_v in {64, 128}.  dtype: type of q, k, v, out and of all gradients but the
  * states', which like the states, and like the gates, are float32.  States are
  * [B][H][d_k][d_v], contiguous, 16-byte aligned.

@@ -19,7 +19,8 @@ namespace {
 // chunk.  128 x 128, bfloat16, 6 tokens so and 8 in a chunk: 2048 heads 53 and 50 us, 256 12
 // and 11, 32 9 and 11 (two launches).  float32, whose chunks take twice as long, 12 tokens so
 // and 16 in a chunk: 79 and 103, 18 and 17, 10 and 14.
-int step_tokens(int dtype) { return dtype == DLA_BF16 ? 6 : 12; }
+constexpr int kStepTokens = 6, kStepTokensF32 = 12;
+int step_tokens(int dtype) { return dtype == DLA_BF16 ? kStepTokens : kStepTokensF32; }
 
 struct Plan {
   bool step;
@@ -88,13 +89,20 @@ Space space_of(const dla_recurrence_desc& d, const Plan& p, bool backward) {
   return s;
 }
 
-dla_status check(const dla_recurrence_desc* d) {
+// Heads of a call: chunk kernels have them in a grid dimension of 65535; the step kernel has
+// not, and what a launch takes of its up to 1024 threads a head.
+constexpr int kHeads = 65535, kStepHeads = (1 << 21) - 1;
+static_assert((int64_t)kStepHeads * 1024 < ((int64_t)1 << 32), "fewer than 2^32 threads");
+
+dla_status check(const dla_recurrence_desc* d, bool backward) {
   if (!d) return DLA_ERR_INVALID_ARG;
   if (d->B < 0 || d->T < 0 || d->H < 1 || d->Hk < 1 || d->H % d->Hk) return DLA_ERR_INVALID_ARG;
   if (d->dtype != DLA_F32 && d->dtype != DLA_BF16) return DLA_ERR_INVALID_ARG;
   if ((d->d_k != 64 && d->d_k != 128) || (d->d_v != 64 && d->d_v != 128)) return DLA_ERR_UNSUPPORTED;
-  // heads are a grid dimension, and a token's number with a chunk added stays an int32
-  if ((int64_t)d->B * d->H > 65535 || d->T > (1 << 30)) return DLA_ERR_UNSUPPORTED;
+  if ((int64_t)d->B * d->H > (!backward && d->T <= kStepTokens ? kStepHeads : kHeads))
+    return DLA_ERR_UNSUPPORTED;
+  // a token's number with a chunk added stays an int32
+  if (d->T > (1 << 30)) return DLA_ERR_UNSUPPORTED;
   return DLA_OK;
 }
 
@@ -144,14 +152,15 @@ RecArgs args_of(const dla_recurrence_desc& d, const Plan& p, const dla_rows* gat
 }
 
 __global__ void fill_kernel(float* p, int64_t n, const float* from) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) p[i] = from ? from[i] : 0.f;
+  const int64_t step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) p[i] = from ? from[i] : 0.f;
 }
 
 hipError_t copy_state(const dla_recurrence_desc& d, const float* from, float* to, hipStream_t st) {
   const int64_t n = (int64_t)d.B * d.H * d.d_k * d.d_v;
   if (!to || to == from || n == 0) return hipSuccess;
-  hipLaunchKernelGGL(fill_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, to, n, from);
+  const int64_t groups = (n + 255) / 256;
+  hipLaunchKernelGGL(fill_kernel, dim3(groups < 65536 ? (unsigned)groups : 65536u), dim3(256), 0, st, to, n, from);
   return hipGetLastError();
 }
 
@@ -227,7 +236,7 @@ extern "C" {
 
 dla_status dla_recurrence_workspace_size(const dla_recurrence_desc* desc, int32_t backward,
                                          size_t* bytes) {
-  const dla_status s = check(desc);
+  const dla_status s = check(desc, backward != 0);
   if (s != DLA_OK) return remember(s);
   if (!bytes) return remember(DLA_ERR_INVALID_ARG);
   *bytes = space_of(*desc, plan_of(*desc, backward != 0), backward != 0).total;
@@ -238,7 +247,7 @@ dla_status dla_recurrence_forward(const dla_recurrence_desc* desc, const dla_row
                                   const dla_rows* k, const dla_rows* v, const dla_rows* log_gate,
                                   const float* state, const dla_rows* out, float* state_out,
                                   void* workspace, size_t workspace_bytes, void* stream) {
-  const dla_status s = check(desc);
+  const dla_status s = check(desc, false);
   if (s != DLA_OK) return remember(s);
   const dla_recurrence_desc& d = *desc;
   const int e = d.dtype == DLA_BF16 ? 2 : 4, G = d.H / d.Hk;
@@ -272,7 +281,7 @@ dla_status dla_recurrence_backward(const dla_recurrence_desc* desc, const dla_ro
                                    const float* dstate_out, const dla_rows* dq, const dla_rows* dk,
                                    const dla_rows* dv, const dla_rows* dg, float* dstate,
                                    void* workspace, size_t workspace_bytes, void* stream) {
-  const dla_status s = check(desc);
+  const dla_status s = check(desc, true);
   if (s != DLA_OK) return remember(s);
   const dla_recurrence_desc& d = *desc;
   const int e = d.dtype == DLA_BF16 ? 2 : 4, G = d.H / d.Hk;

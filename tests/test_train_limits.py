@@ -3,6 +3,7 @@ is refused before anything is enqueued."""
 import ctypes
 
 import pytest
+import torch
 
 from paper_2606_10650_amd import dla, train
 
@@ -19,3 +20,21 @@ def test_adamw_elements(states):
     for n in ((1 << 36) - 4095, 1 << 36, 1 << 40):
         assert step(n) == dla.DLA_ERR_UNSUPPORTED
     assert step((1 << 40) + 1) == dla.DLA_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_heads(dtype):
+    """65535 of them, in a forward call of up to 6 tokens 2^21 - 1."""
+    n = ctypes.c_size_t(0)
+
+    def ask(heads, T, backward=False):
+        d = train._desc(1, heads, heads, T, 64, 64, dtype)
+        return train.lib().dla_recurrence_workspace_size(d, int(backward), ctypes.byref(n))
+
+    for T in (0, 1, 6):
+        assert ask((1 << 21) - 1, T) == dla.DLA_OK and n.value == 0
+        assert ask(1 << 21, T) == dla.DLA_ERR_UNSUPPORTED
+        assert ask(65535, T, True) == dla.DLA_OK
+        assert ask(65536, T, True) == dla.DLA_ERR_UNSUPPORTED
+    assert ask(65535, 7) == dla.DLA_OK and ask(65536, 7) == dla.DLA_ERR_UNSUPPORTED
+    assert ask(1, 1 << 30) == dla.DLA_OK and ask(1, (1 << 30) + 1) == dla.DLA_ERR_UNSUPPORTED
