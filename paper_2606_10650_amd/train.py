@@ -132,6 +132,9 @@ def _like(t, shape, dtype, device, name, contiguous=False):
 
 
 def _space(workspace, need, device):
+    """A workspace and its size: the caller's, where that is large enough, else a new one."""
+    if workspace is not None and (workspace.device != device or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be contiguous on {device}")
     if workspace is None or workspace.numel() * workspace.element_size() < need:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
     return workspace, workspace.numel() * workspace.element_size()
