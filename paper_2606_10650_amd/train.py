@@ -81,6 +81,21 @@ def _stream(device):
     return torch.cuda.current_stream(device).cuda_stream
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _run(call, device, *args):
+    """A library call on the device's current stream.  Kernels go to the calling thread's
+    current device, whichever a stream's is."""
+    f = getattr(lib(), call)
+    if device.index == _current_device():
+        status = f(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = f(*args, _stream(device))
+    _check(status, call)
+
+
 # ---------------------------------------------------------------------------
 # recurrence
 # ---------------------------------------------------------------------------
@@ -166,10 +181,9 @@ def recurrence(q, k, v, g, *, scale: float = 1.0, state=None, lengths=None, out=
     need, size = recurrence_workspace_bytes(B, H, Hk, T, d_k, d_v, dtype), 0
     if need:
         workspace, size = _space(workspace, need, dev)
-    _check(lib().dla_recurrence_forward(
-        _desc(B, H, Hk, T, d_k, d_v, dtype, scale, lengths), _rows(q, "q"), _rows(k, "k"), _rows(v, "v"),
-        _rows(g, "g"), _ptr(state), _rows(out, "out"), _ptr(state_out), _ptr(workspace) if need else None,
-        size, _stream(dev)), "dla_recurrence_forward")
+    _run("dla_recurrence_forward", dev,
+         _desc(B, H, Hk, T, d_k, d_v, dtype, scale, lengths), _rows(q, "q"), _rows(k, "k"), _rows(v, "v"),
+         _rows(g, "g"), _ptr(state), _rows(out, "out"), _ptr(state_out), _ptr(workspace) if need else None, size)
     return out, state_out
 
 
@@ -193,11 +207,10 @@ def recurrence_backward(q, k, v, g, dout, *, scale: float = 1.0, state=None, dst
     need, size = recurrence_workspace_bytes(B, H, Hk, T, d_k, d_v, dtype, backward=True), 0
     if need:
         workspace, size = _space(workspace, need, dev)
-    _check(lib().dla_recurrence_backward(
-        _desc(B, H, Hk, T, d_k, d_v, dtype, scale, lengths), _rows(q, "q"), _rows(k, "k"), _rows(v, "v"),
-        _rows(g, "g"), _ptr(state), _rows(dout, "dout"), _ptr(dstate), _rows(dq, "dq"), _rows(dk, "dk"),
-        _rows(dv, "dv"), _rows(dg, "dg"), _ptr(ds0), _ptr(workspace) if need else None, size,
-        _stream(dev)), "dla_recurrence_backward")
+    _run("dla_recurrence_backward", dev,
+         _desc(B, H, Hk, T, d_k, d_v, dtype, scale, lengths), _rows(q, "q"), _rows(k, "k"), _rows(v, "v"),
+         _rows(g, "g"), _ptr(state), _rows(dout, "dout"), _ptr(dstate), _rows(dq, "dq"), _rows(dk, "dk"),
+         _rows(dv, "dv"), _rows(dg, "dg"), _ptr(ds0), _ptr(workspace) if need else None, size)
     return dq, dk, dv, dg, ds0
 
 
@@ -226,9 +239,9 @@ def _norm_forward(call, x, weight, residual, eps, y, last):
     desc, D = _norm_desc(x, weight, eps), x.shape[1]
     rows = _norm_rows(x, x, "x"), _norm_rows(residual, x, "residual")
     h = None if residual is None else torch.empty_like(residual, memory_format=torch.contiguous_format)
-    _check(getattr(lib(), call)(
-        desc, *rows, weight.data_ptr(), None if h is None else _NORM_ROWS.pack(h.data_ptr(), D),
-        _NORM_ROWS.pack(y.data_ptr(), D), last.data_ptr(), _stream(x.device)), call)
+    _run(call, x.device, desc, *rows, weight.data_ptr(),
+         None if h is None else _NORM_ROWS.pack(h.data_ptr(), D), _NORM_ROWS.pack(y.data_ptr(), D),
+         last.data_ptr())
     return x if h is None else h
 
 
@@ -267,10 +280,9 @@ def rms_norm_backward(dy, h, weight, rstd, dres=None, *, workspace=None):
     dx = torch.empty(h.shape, dtype=h.dtype, device=dev)
     dw = torch.empty(h.shape[1:], dtype=torch.float32, device=dev)
     workspace, size = _space(workspace, rms_norm_workspace_bytes(*h.shape, h.dtype), dev)
-    _check(lib().dla_rms_norm_backward(
-        desc, _norm_rows(dy, h, "dy"), _norm_rows(h, h, "h"), weight.data_ptr(), rstd.data_ptr(),
-        _norm_rows(dres, h, "dres"), _norm_rows(dx, h, "dx"), dw.data_ptr(), workspace.data_ptr(), size,
-        _stream(dev)), "dla_rms_norm_backward")
+    _run("dla_rms_norm_backward", dev,
+         desc, _norm_rows(dy, h, "dy"), _norm_rows(h, h, "h"), weight.data_ptr(), rstd.data_ptr(),
+         _norm_rows(dres, h, "dres"), _norm_rows(dx, h, "dx"), dw.data_ptr(), workspace.data_ptr(), size)
     return dx, dw
 
 
@@ -392,8 +404,7 @@ class AdamW:
                 raise ValueError(f"grad_scale on {grad_scale.device}, tensors on {dev}")
             args = AdamWParams(lr, betas[0], betas[1], eps, step, p, g, fmt, seed & 0xFFFFFFFF,
                                None if grad_scale is None else grad_scale.data_ptr())
-            _check(lib().dla_adamw_step(arr, len(arr), ctypes.byref(args), _stream(dev)),
-                   "dla_adamw_step")
+            _run("dla_adamw_step", dev, arr, len(arr), ctypes.byref(args))
 
 
 # ---------------------------------------------------------------------------

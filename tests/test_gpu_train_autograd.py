@@ -138,3 +138,15 @@ def test_norm_without_a_residual(use_h, dtype):
     with torch.no_grad():
         y, h = tr.RMSNorm.apply(x.detach().view(2, 3, 96), None, w.detach())
         assert y.shape == h.shape == (2, 3, 96) and h.data_ptr() == x.data_ptr()
+
+
+def test_tensors_in_host_memory_are_refused():
+    tr = _train()
+    q, g, x, w = torch.zeros(1, 1, 4, 64), torch.zeros(1, 1, 4), torch.zeros(4, 64), torch.ones(64)
+    plan = tr.AdamW()
+    plan.add(w, torch.ones(64))
+    for bad in (lambda: tr.recurrence(q, q, q, g), lambda: tr.recurrence_backward(q, q, q, g, q),
+                lambda: tr.rms_norm(x, w), lambda: tr.rms_norm_fp8(x, w),
+                lambda: tr.rms_norm_backward(x, x, w, torch.ones(4)), lambda: plan.step(1, lr=1e-3)):
+        with pytest.raises(ValueError, match="cuda device"):
+            bad()
