@@ -163,14 +163,25 @@ dla_status dla_rms_norm_backward(const dla_norm_desc* desc, const dla_norm_rows*
  *
  * state_format DLA_F32: m, v are float32 [n].  DLA_STATE_FP8: m and v are 8-bit codes
  * [n] of m and of sqrt(v), in the floating point format of dla_rms_norm_fp8, times
- * m_scale, v_scale, float32 [ceil(n / 256)], one per 256 elements in order: the block's
- * largest magnitude / 448 (zero, with codes of zero, where that is below 1e-30).  A
- * sqrt(v) above zero has a code of at least 2^-9.  The operations that lead to codes are
- * each rounded, in the order written above, so that codes follow from inputs bit by bit.  p is updated with the float32 m and
- * v of the step, before they are rounded.  seed 0 rounds codes to nearest even; another
- * seed rounds up or down with the probability that makes the mean right, from a hash of
- * seed, tensor number and element index: a v that moves by a thousandth a step would
- * otherwise stay at its code.  Give each step a seed of its own.
+ * m_scale, v_scale, float32 [ceil(n / 256)], one per 256 elements in order.  p is updated
+ * with the float32 m and v of the step, before they are rounded.  Codes follow from the
+ * inputs bit by bit, by these float32 operations, each rounded, beta and 1 - beta (formed in
+ * double) rounded to float32:
+ *   g = grad_scale grad
+ *   m = beta1 (code m_scale) + (1 - beta1) g
+ *   v = beta2 (code v_scale)^2 + ((1 - beta2) g) g,  r = sqrt(v)
+ * and for x either of m and r, with top the largest |x| of its 256:
+ *   scale = top / 448,  y = x (448 / top)
+ * (top at most 1e-30: scale and codes are zero).  seed 0: the code is y, at most 448 in
+ * magnitude, rounded to nearest even.  Another seed rounds up or down with the probability
+ * that makes the mean right, as a v that moves by a thousandth a step would otherwise stay
+ * at its code: with d = max(2^(floor(log2 |y|) - 3), 2^-9) the codes' spacing at y,
+ *   |code| = min(floor(|y| / d + u) d, 448)
+ * where u is h >> 16 for m and h & 65535 for r, over 65536, and of the element's index in
+ * its tensor, the tensor's number in the call and the seed, modulo 2^32,
+ *   h = (index + 0x9E3779B9 (number + 1)) ^ seed
+ *   h = h 0x2545F491,  h = h ^ (h >> 16),  h = h 0x9E3779B1,  h = h ^ (h >> 15).
+ * An r above zero has a code of at least 2^-9.  Give each step a seed of its own.
  *
  * grad_scale: NULL for 1, or one float32 on the device (a clipping or loss-scale factor);
  * where it is infinite or NaN the step changes nothing.

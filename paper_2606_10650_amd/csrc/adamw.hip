@@ -137,6 +137,10 @@ __device__ __forceinline__ float block_top(const float (&x)[4]) {
   return top;
 }
 
+__device__ __forceinline__ float lane_value(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
+
 constexpr float kLeastTop = 1e-30f;   // a block whose largest value is below this is all zero
 
 template <typename Tp, typename Tg, bool F8>
@@ -191,7 +195,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       // every operation rounded, none contracted: a last bit can decide a code, and a code
-      // decides the next step, so states are to follow from these lines alone
+      // decides the next step, so states are to follow from dla_train.h's lines alone
 #pragma clang fp contract(off)
       g[j] *= scale;
       m[j] = s.beta1 * m[j] + s.rest1 * g[j];
@@ -203,8 +207,11 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
     put4(param + i, n, wide, p);
     if constexpr (F8) {
       const float mt = block_top(m), vt = block_top(root);
-      const float mi = mt > kLeastTop ? 1.f / mt * 448.f : (mt <= kLeastTop ? 0.f : mt);
-      const float vi = vt > kLeastTop ? 1.f / vt * 448.f : (vt <= kLeastTop ? 0.f : vt);
+      // 448 / mt, 448 / vt, mt / 448 and vt / 448 by one division, in the first four lanes
+      const float top = lane & 1 ? vt : mt;
+      float q = (lane & 2 ? top : 448.f) / (lane & 2 ? 448.f : top);
+      q = top > kLeastTop ? q : (top <= kLeastTop ? 0.f : top);
+      const float mi = lane_value(q, 0), vi = lane_value(q, 1);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float um = -1.f, uv = -1.f;
@@ -220,10 +227,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
       }
       put_codes(static_cast<uint8_t*>(t.m) + i, n, wide, m);
       put_codes(static_cast<uint8_t*>(t.v) + i, n, wide, v);
-      if (lane == 0) {
-        t.m_scale[blk] = mt > kLeastTop ? mt * (1.f / 448.f) : (mt <= kLeastTop ? 0.f : mt);
-        t.v_scale[blk] = vt > kLeastTop ? vt * (1.f / 448.f) : (vt <= kLeastTop ? 0.f : vt);
-      }
+      if (lane == 2) t.m_scale[blk] = q;
+      if (lane == 3) t.v_scale[blk] = q;
     } else {
       put4(static_cast<float*>(t.m) + i, n, wide, m);
       put4(static_cast<float*>(t.v) + i, n, wide, v);
