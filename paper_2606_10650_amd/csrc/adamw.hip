@@ -149,7 +149,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
   float scale = 1.f;
   if (s.grad_scale) {
     scale = *s.grad_scale;
-    if (!(fabsf(scale) <= 3.4e38f)) return;
+    if (!(fabsf(scale) <= 0x1.fffffep127f)) return;
   }
   int k = 0;
 #pragma unroll

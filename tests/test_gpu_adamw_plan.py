@@ -111,3 +111,16 @@ def test_what_a_step_refuses():
     torch.cuda.synchronize()
     assert torch.equal(p.detach(), was)
     plan.step(2, **HY)
+
+
+@pytest.mark.parametrize("factor", [3.402823466e38, -3.401e38])
+def test_the_largest_factors_count(factor):
+    """A finite grad_scale is one however large: only an infinite one, or NaN, stops the step."""
+    tr = _train()
+    p, g = torch.ones(64, device="cuda"), torch.full((64,), 2.0 ** -126, device="cuda")
+    plan = tr.AdamW()
+    plan.add(p, g)
+    plan.step(1, lr=0.125, eps=0.0, grad_scale=torch.tensor([factor], device="cuda"))
+    torch.cuda.synchronize()
+    # the first step is lr in the gradient's direction
+    assert ((p - (1 - 0.125 * (1 if factor > 0 else -1))).abs() <= 1e-6).all()
