@@ -171,7 +171,7 @@ dla_status dla_rms_norm_backward(const dla_norm_desc* desc, const dla_norm_rows*
  *   m = beta1 (code m_scale) + (1 - beta1) g
  *   v = beta2 (code v_scale)^2 + ((1 - beta2) g) g,  r = sqrt(v)
  * and for x either of m and r, with top the largest |x| of its 256:
- *   scale = top / 448,  y = x (448 / top)
+ *   scale = top (1 / 448),  y = x ((1 / top) 448)
  * (top at most 1e-30: scale and codes are zero).  seed 0: the code is y, at most 448 in
  * magnitude, rounded to nearest even.  Another seed rounds up or down with the probability
  * that makes the mean right, as a v that moves by a thousandth a step would otherwise stay

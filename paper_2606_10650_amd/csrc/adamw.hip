@@ -207,11 +207,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
     put4(param + i, n, wide, p);
     if constexpr (F8) {
       const float mt = block_top(m), vt = block_top(root);
-      // 448 / mt, 448 / vt, mt / 448 and vt / 448 by one division, in the first four lanes
+      // both kinds by one division: m's in lane 0, the root's in lane 1
       const float top = lane & 1 ? vt : mt;
-      float q = (lane & 2 ? top : 448.f) / (lane & 2 ? 448.f : top);
-      q = top > kLeastTop ? q : (top <= kLeastTop ? 0.f : top);
-      const float mi = lane_value(q, 0), vi = lane_value(q, 1);
+      const bool some = top > kLeastTop;
+      const float none = top <= kLeastTop ? 0.f : top;   // (a NaN stays one)
+      const float inv = some ? 1.f / top * 448.f : none;
+      const float mi = lane_value(inv, 0), vi = lane_value(inv, 1);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float um = -1.f, uv = -1.f;
@@ -221,14 +222,15 @@ __global__ __launch_bounds__(256) void adamw_kernel(Table tab) {
           uv = (float)(r & 0xFFFFu) * (1.f / 65536.f);
         }
         m[j] = to_code(m[j] * mi, um);
-        const bool some = root[j] > 0.f && vi > 0.f;
+        const bool least = root[j] > 0.f && vi > 0.f;
         v[j] = to_code(root[j] * vi, uv);
-        if (some && v[j] < 0.001953125f) v[j] = 0.001953125f;   // 2^-9, the least code
+        if (least && v[j] < 0.001953125f) v[j] = 0.001953125f;   // 2^-9, the least code
       }
       put_codes(static_cast<uint8_t*>(t.m) + i, n, wide, m);
       put_codes(static_cast<uint8_t*>(t.v) + i, n, wide, v);
-      if (lane == 2) t.m_scale[blk] = q;
-      if (lane == 3) t.v_scale[blk] = q;
+      const float unit = some ? top * (1.f / 448.f) : none;
+      if (lane == 0) t.m_scale[blk] = unit;
+      if (lane == 1) t.v_scale[blk] = unit;
     } else {
       put4(static_cast<float*>(t.m) + i, n, wide, m);
       put4(static_cast<float*>(t.v) + i, n, wide, v);

@@ -36,8 +36,8 @@ def _code(x, u, root):
     n = len(x)
     blocks = np.pad(np.abs(x), (0, -n % 256)).reshape(-1, 256).max(1)
     some = blocks > F(1e-30)
-    scale = np.where(some, blocks / F(448), F(0))
-    per = np.repeat(np.where(some, F(448) / np.where(some, blocks, F(1)), F(0)), 256)[:n]
+    scale = np.where(some, blocks * (F(1) / F(448)), F(0))
+    per = np.repeat(np.where(some, F(1) / np.where(some, blocks, F(1)) * F(448), F(0)), 256)[:n]
     y = x * per
     a = np.abs(y)
     if u is not None:
