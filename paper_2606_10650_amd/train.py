@@ -306,6 +306,7 @@ class AdamW:
         self.states = states
         self.kept = []       # the tensors of each entry
         self._groups = {}    # (param, grad type, format, device) -> entries
+        self._tensors, self._at = [], []     # what has an address in a description, and which
         self._arrays = None
 
     def add(self, param, grad, m=None, v=None, *, master=None, m_scale=None, v_scale=None,
@@ -324,78 +325,63 @@ class AdamW:
             raise ValueError(f"states of types {m.dtype}, {v.dtype}")
         if fp8 and (m_scale is None or v_scale is None):
             raise ValueError("8-bit states need their scales")
-        blocks = -(-n // FP8_BLOCK)
-        # in the order of dla_adamw_tensor
-        buffers = [(param, n, param.dtype), (master, n, torch.float32), (grad, n, grad.dtype),
-                   (m, n, m.dtype), (v, n, m.dtype)]
-        buffers += [(t if fp8 else None, blocks, torch.float32) for t in (m_scale, v_scale)]
-        for t, size, dtype in buffers:
-            if t is not None:
-                self._fits(t, size, dtype, dev)
+        key = (_dtype_code(param.dtype), _dtype_code(grad.dtype), DLA_STATE_FP8 if fp8 else DLA_F32, dev)
+        tensors = [param, master, grad, m, v] + ([m_scale, v_scale] if fp8 else [None, None])
+        self._fit(key, tensors, n)
         own = param.grad if param.is_leaf else None
         follow = own is not None and own.data_ptr() == grad.data_ptr()
         if follow:
-            buffers[2] = (None, n, grad.dtype)     # not kept: it may be freed between steps
-        key = (_dtype_code(param.dtype), _dtype_code(grad.dtype), DLA_STATE_FP8 if fp8 else DLA_F32, dev)
-        self._groups.setdefault(key, []).append((buffers, n, float(weight_decay), follow))
+            tensors[2] = None       # looked up, and not kept: it may be freed between steps
+        self._groups.setdefault(key, []).append((tensors, n, float(weight_decay), follow))
         self.kept.append({"param": param, "master": master, "m": m, "v": v, "m_scale": m_scale,
                           "v_scale": v_scale})
+        self._tensors += [t for t in tensors if t is not None]
+        self._at += [t.data_ptr() for t in tensors if t is not None]
         self._arrays = None
 
     @staticmethod
-    def _fits(t, size, dtype, dev):
-        if t.numel() != size or not t.is_contiguous() or t.device != dev or t.dtype != dtype:
-            raise ValueError(f"a buffer of {t.numel()} {t.dtype} on {t.device} where {size} "
-                             f"contiguous {dtype} on {dev} are wanted")
+    def _fit(key, tensors, n):
+        """Refuses an entry's tensors (in the order of dla_adamw_tensor) that are not its kind's."""
+        p, g, fmt, dev = key
+        dtypes = {DLA_F32: torch.float32, DLA_BF16: torch.bfloat16}
+        state = FP8 if fmt == DLA_STATE_FP8 else torch.float32
+        for i, (t, dtype) in enumerate(zip(tensors, (dtypes[p], torch.float32, dtypes[g], state, state,
+                                                     torch.float32, torch.float32))):
+            size = n if i < 5 else -(-n // FP8_BLOCK)
+            if t is not None and (t.numel() != size or t.dtype != dtype or t.device != dev or
+                                  not t.is_contiguous() or (size and not t.data_ptr())):
+                raise ValueError(f"a buffer of {t.numel()} {t.dtype} on {t.device} where {size} "
+                                 f"contiguous {dtype} on {dev} are wanted")
 
     def _marshal(self):
-        """The descriptions of all tensors.  `_tensors`: those kept that have an address in one;
-        `_followed`: the parameters whose gradients have, behind them; `_slots`: where each
-        address goes and what its tensor has to be; `_at`: the addresses there."""
-        self._tensors, self._followed, slots, gradients, arrays = [], [], [], [], []
-        for key, entries in self._groups.items():
-            array = (AdamWTensor * len(entries))()
-            for i, (buffers, n, decay, follow) in enumerate(entries):
-                array[i] = AdamWTensor(*[_ptr(t) for t, _, _ in buffers], n, decay)
-                for (field, _), (t, size, dtype) in zip(AdamWTensor._fields_, buffers):
-                    if t is not None:
-                        self._tensors.append(t)
-                        slots.append((array[i], field, size, dtype, key[3]))
-                if follow:
-                    self._followed.append(buffers[0][0])
-                    gradients.append((array[i], "grad", *buffers[2][1:], key[3]))
-            arrays.append((key, array))
-        self._slots = slots + gradients
-        self._at = list(map(_ptr, self._tensors)) + [None] * len(gradients)
-        self._arrays = arrays
+        """The descriptions of all tensors, and the gradients that every step looks up."""
+        self._arrays = [(key, (AdamWTensor * len(es))(*[AdamWTensor(*map(_ptr, e[0]), *e[1:3]) for e in es]))
+                        for key, es in self._groups.items()]
+        self._followed = [(e[0][0], array[i], key, e[1]) for key, array in self._arrays
+                          for i, e in enumerate(self._groups[key]) if e[3]]
 
     def _refresh(self):
         """Addresses as they are now."""
-        now = list(map(torch.Tensor.data_ptr, self._tensors))
-        for param, (_, _, size, dtype, dev) in zip(self._followed, self._slots[len(now):]):
+        at = list(map(torch.Tensor.data_ptr, self._tensors))
+        if at != self._at:
+            for key, entries in self._groups.items():
+                for tensors, n, *_ in entries:
+                    self._fit(key, tensors, n)
+            self._at, self._arrays = at, None
+        if self._arrays is None:
+            self._marshal()
+        for param, description, key, n in self._followed:
             grad = param.grad
             if grad is None:
                 raise ValueError(f"a parameter of shape {tuple(param.shape)} has no gradient")
-            self._fits(grad, size, dtype, dev)
-            now.append(grad.data_ptr())
-        if now != self._at:
-            for i, (x, was) in enumerate(zip(now, self._at)):
-                if x != was:
-                    slot, field, size, dtype, dev = self._slots[i]
-                    if i < len(self._tensors):
-                        self._fits(self._tensors[i], size, dtype, dev)
-                    if size and not x:
-                        raise ValueError("a buffer without memory")
-                    setattr(slot, field, x)
-                    self._at[i] = x
+            self._fit(key, (None, None, grad), n)
+            description.grad = grad.data_ptr()
 
     def step(self, step: int, *, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, seed: int = 0,
              grad_scale=None):
         """The step-th update (from 1).  seed: of 8-bit states' rounding, 0 for nearest.
         grad_scale: a float32 tensor of one element, or None; the step changes nothing where
         it is not finite."""
-        if self._arrays is None:
-            self._marshal()
         self._refresh()
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32")

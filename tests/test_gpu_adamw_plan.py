@@ -124,3 +124,22 @@ def test_the_largest_factors_count(factor):
     torch.cuda.synchronize()
     # the first step is lr in the gradient's direction
     assert ((p - (1 - 0.125 * (1 if factor > 0 else -1))).abs() <= 1e-6).all()
+
+
+def test_data_replaced_before_the_first_step():
+    tr = _train()
+    p, g = _rnd(1, 100), _rnd(2, 100)
+    plan, other = tr.AdamW(), tr.AdamW()
+    plan.add(p, g)
+    q = p.clone()
+    other.add(q, g)
+    p.data = p.data.clone()
+    plan.step(1, **HY)
+    other.step(1, **HY)
+    assert torch.equal(p, q)
+    plan = tr.AdamW()
+    plan.add(p, g)
+    p.data = torch.zeros(50, device="cuda")
+    for _ in range(2):
+        with pytest.raises(ValueError):
+            plan.step(1, **HY)
