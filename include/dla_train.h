@@ -54,7 +54,7 @@ typedef struct {
  * tokens.  Nothing is read behind its end (whatever memory holds there, NaN
  * included), outputs and gradients there are zero, and the last state is the one
  * at the end.
- * Gates are log decays, g <= 0.  A gate below -87.33 (a decay smaller than the
+ * Gates are log decays, g <= 0.  A gate below -87.33655 (a decay smaller than the
  * smallest normal float32), -inf among them, counts as a decay of zero: it starts a
  * new sequence in the same row, and its own gradient is zero.  The state must be
  * finite there.
@@ -62,9 +62,11 @@ typedef struct {
  * exact; scores, and what is added to the states, keep 16 bits, so that the states
  * hold float32's precision to about 2^-17; the state that out and dv read is rounded
  * once to bfloat16.  dg adds up what the scores and both states give, in float64, and
- * is of the inputs' type.
- * An infinity or NaN in a token reaches every later output of its head, and may
- * reach those of up to 31 tokens before it.
+ * is rounded to the inputs' type.  Of k, v, scale q and scale dout, magnitudes up to 2^110
+ * are taken; they are scaled by up to 2^16 on the way.
+ * An infinity or NaN in a token reaches every later output of its head, those behind a
+ * gate that cuts among them, and may reach those of up to 31 tokens before it (not in
+ * forward calls of up to 6 tokens, which go one by one).
  */
 typedef struct {
   int32_t B, H, Hk, T, d_k, d_v;
@@ -132,7 +134,7 @@ dla_status dla_rms_norm(const dla_norm_desc* desc, const dla_norm_rows* x,
 
 /* The same with y in 8-bit floating point (4 exponent and 3 mantissa bits, largest
  * value 448, no infinity) and a float32 scale per row: y_scale = max |y| / 448, the
- * codes are y / y_scale rounded to nearest even.  A row whose max |y| is below 448 times
+ * codes are y (448 / max |y|) rounded to nearest even.  A row whose max |y| is below 448 times
  * the smallest normal float32 (5.3e-36) has scale and codes zero; a row with an infinity
  * or NaN has NaN codes. */
 dla_status dla_rms_norm_fp8(const dla_norm_desc* desc, const dla_norm_rows* x,

@@ -3,8 +3,8 @@
 // recorded.  A workgroup takes kChunk elements of one tensor, a wave 256 at a time: four
 // consecutive ones a lane, and with 8-bit states one block, whose scales it forms with lane
 // moves.  Every byte is read and written once; they bound it: 134M bfloat16 parameters with
-// float32 masters 735 us for 3.8 GB, 5.1 TB/s, a large copy's rate; with 8-bit states 460 us
-// for 2.1 GB, 4.7 TB/s, where the roots, hashes and conversions show.
+// float32 masters 736 us for 3.8 GB, 5.1 TB/s, a large copy's rate; with 8-bit states 463 us
+// for 2.1 GB, 4.6 TB/s, where the roots, hashes and conversions show.
 //
 // 8-bit states are codes of m and of r = sqrt(v) (4 exponent and 3 mantissa bits) times a
 // float32 scale per 256 elements, the block's largest magnitude / 448.  The root halves the

@@ -6,7 +6,8 @@
 // with the state before all tokens and the gradient of the last one as further ends.  With
 // x_u the sum of A_us over s < u and y_s that over u > s, dg_t = <dstate, last state> + sum
 // over s >= t of (x_s - y_s).  No pair (t, t) enters either, so nothing large cancels where
-// the gates are steep.  The dq pass leaves x (a lane holds a token u and its pairs' scores
+// the gates are steep.  dg is rounded once, to the inputs' type: gates are a projection of the
+// same type, whose backward pass multiplies their gradient in that type.  The dq pass leaves x (a lane holds a token u and its pairs' scores
 // of do and v; each wave adds the products with its own 32 columns of q and k), the dk pass
 // y, the other way round.
 #include "recurrence_tile.h"

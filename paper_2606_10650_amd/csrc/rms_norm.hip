@@ -6,8 +6,10 @@
 // are read once and written once, so bytes bound the forward pass, and the backward pass
 // but for dw: a workgroup goes over many rows with dw's sums of its columns in registers,
 // leaves one partial sum per column, and a second kernel adds those up in a fixed order.
-// 65536 rows of 2048 bfloat16: forward 201 us for 1.07 GB, 5.3 TB/s (a large copy 5.1),
-// backward 207 us and 5 for dw.  64 rows of 4096 to 8 bits: 6.6 us, most of it a launch.
+// 65536 rows of 2048 bfloat16: forward 204 us for 1.07 GB, 5.3 TB/s (a large copy 5.1),
+// backward 208 us and 6 for dw; float32: 484 us, 4.4 TB/s, and 416, 5.2.  8192 rows of 16384
+// float32: 484 us, 4.4 TB/s, and backward 476, 4.5, with seven registers a lane in scratch
+// memory.  64 rows of 4096 to 8 bits: 6.8 us, most of it a launch.
 // Rows may start at any element: a piece is read as it lies, whatever its alignment.
 #include "dla_common.h"
 #include "dla_train.h"

@@ -30,11 +30,17 @@ struct Plan {
 // Segments of a pass: with fewer heads than the chip holds workgroups, sequences are cut
 // so that all of them work, at the price of a pass over keys and values (backward also over
 // queries and output gradients) for the segments' states.  As many as the chip then holds
-// at once; not where that makes but two or three, which costs what it gives.  2048 bfloat16
-// tokens, forward and backward, 128 x 128: 96 heads in 1, 4, 5, 6 segments 478, 358, 324, 388
-// us, 150 in 1, 3, 4 472, 479, 543, 192 in 1, 2 480, 636; 64 x 64 (half the threads per
-// workgroup): 96 in 5, 8, 10 178, 164, 174, 192 in 1, 5, 8 400, 274, 297, 300 in 1, 3 490,
-// 423.  A segment has at least 4 chunks, 2 of float32, whose chunks take longer (15 heads x
+// at once, about 512 workgroups, half as many again for each of d_k and d_v that is 64; not
+// where that makes but two or three, which costs what it gives.  2048 bfloat16 tokens,
+// forward and backward, us by segments, the rule's in brackets:
+//   128 x 128   96 heads 1: 481, 4: 358, [5: 336], 6: 406   192 heads [1: 487], 2: 645
+//   128 x 64    96 1: 433, 5: 256, [8: 250], 10: 283   192 1: 442, [4: 442], 5: 475
+//               300 [1: 666], 2: 725
+//   64 x 128    96 1: 471, 5: 254, [8: 262], 10: 296   192 1: 483, [4: 450], 5: 485
+//               300 [1: 723], 2: 726, 3: 698
+//   64 x 64     96 1: 401, 5: 179, 8: 163, [10: 174]   192 1: 401, 4: 281, [5: 281], 8: 315
+//               300 1: 483, [3: 417], 4: 450
+// A segment has at least 4 chunks, 2 of float32, whose chunks take longer (15 heads x
 // 1531 tokens: 148 us, 158 with 4, 245 with 8).
 Plan plan_of(const dla_recurrence_desc& d, bool backward) {
   Plan p{!backward && d.T <= step_tokens(d.dtype), 1, kRecChunk};
