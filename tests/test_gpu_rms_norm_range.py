@@ -129,3 +129,14 @@ def test_more_rows_than_a_launch_takes():
     n, dn = h.float() * R[:, None], y.float() * w.float()
     want = (dn - n * (dn * n).mean(-1, keepdim=True)) * R[:, None]
     assert ((dx.float() - want).abs() <= (2.0 ** -8 + 1e-5) * (dn.abs().amax(-1) * R)[:, None] * 2).all()
+
+
+def test_broadcast_rows_are_refused():
+    """One row for all is no rows apart: rms_norm takes none (the RMSNorm function copies)."""
+    tr = _train()
+    from paper_2606_10650_amd import dla
+    x, w = torch.ones((1, 64), device="cuda"), torch.ones(64, device="cuda")
+    for call in (tr.rms_norm, tr.rms_norm_fp8):
+        with pytest.raises(dla.DLAError) as e:
+            call(x.expand(4, 64), w)
+        assert e.value.status == dla.DLA_ERR_INVALID_ARG
