@@ -1,0 +1,203 @@
+// The gated feed-forward block for a few rows, and what its products need around them: float32 or
+// unaligned operands as planes of bfloat16, and the gradients of both projections' outputs.
+#include "gated_ff.h"
+#include "mfma.h"
+#include "piece.h"
+
+namespace dla {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+}
+
+// A few rows: the weights are read once, 16 rows of each a workgroup, its waves taking K in turn;
+// the rows of x are the products' columns.  Bytes of the weights bound it.
+template <typename T, int NB>
+__global__ __launch_bounds__(512) void ff_step_kernel(int rows, int D, int F, FfRows x, FfRows wg, FfRows wu, FfRows y,
+                                                      FfRows g, FfRows u) {
+  constexpr int WAVES = 8, KW = 32;    // K values of a product
+  __shared__ float sums[WAVES][2][NB][16][17];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4;
+  const int64_t f = (int64_t)blockIdx.x * 16 + l16;
+  f32x4 acc[2][NB];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto frag = [&](const FfRows& r, int64_t row, bool any, int k) -> typename Frag<T>::T {
+    const int n = any && D > k ? D - k : 0;
+    const T* p = static_cast<const T*>(r.p) + row * r.st + k;
+    if constexpr (sizeof(T) == 2) {
+      return __builtin_bit_cast(bf16x8, Piece<T>::raw(p, n));
+    } else {
+      const auto lo = Piece<T>::raw(p, n);
+      const auto hi = Piece<T>::raw(p + 4, n > 4 ? n - 4 : 0);
+      f32x8 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = Piece<T>::value(lo, e);
+        v[e + 4] = Piece<T>::value(hi, e);
+      }
+      return v;
+    }
+  };
+  for (int k = wave * KW; k < D; k += WAVES * KW) {
+    const int c = k + 8 * q;
+    const auto a0 = frag(wg, f, f < F, c), a1 = frag(wu, f, f < F, c);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const auto v = frag(x, 16 * b + l16, 16 * b + l16 < rows, c);
+      mma16(acc[0][b], a0, v);
+      mma16(acc[1][b], a1, v);
+    }
+  }
+  // the waves' sums in their order
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sums[wave][i][b][l16][4 * q + r] = acc[i][b][r];
+  __syncthreads();
+  for (int e = threadIdx.x; e < NB * 256; e += 512) {
+    const int b = e >> 8, m = (e >> 4) & 15, r = e & 15;
+    const int64_t col = (int64_t)blockIdx.x * 16 + r, row = 16 * b + m;
+    float gv = 0.f, uv = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      gv += sums[w][0][b][m][r];
+      uv += sums[w][1][b][m][r];
+    }
+    if (row < rows && col < F) {
+      auto put = [&](const FfRows& o, float v) {
+        if constexpr (sizeof(T) == 2) static_cast<__bf16*>(o.p)[row * o.st + col] = (__bf16)v;
+        else static_cast<float*>(o.p)[row * o.st + col] = v;
+      };
+      put(y, gv * sigmoid(gv) * uv);
+      if (g.p) {
+        put(g, gv);
+        put(u, uv);
+      }
+    }
+  }
+}
+
+// Three bfloat16 terms of a value, whose sum it is to float32's last digit; a value that is not
+// finite is its first term.
+__device__ __forceinline__ void terms(float v, __bf16 (&t)[3]) {
+  t[0] = (__bf16)v;
+  float rest = v - (float)t[0];
+  if (!(fabsf(rest) < __builtin_huge_valf())) rest = 0.f;
+  t[1] = (__bf16)rest;
+  t[2] = (__bf16)(rest - (float)t[1]);
+}
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+// A piece of values to the planes.
+template <typename T, int N>
+__device__ __forceinline__ void put_planes(uint16_t* to, int64_t plane, const float (&v)[N]) {
+  typedef __bf16 vec __attribute__((ext_vector_type(N)));
+  if constexpr (sizeof(T) == 2) {
+    vec r;
+#pragma unroll
+    for (int j = 0; j < N; ++j) r[j] = (__bf16)v[j];
+    *reinterpret_cast<vec*>(to) = r;
+  } else {
+    vec r[3];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      __bf16 t[3];
+      terms(v[j], t);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) r[q][j] = t[q];
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<vec*>(to + q * plane) = r[q];
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void ff_pack_kernel(int64_t rows, int cols, int ld, FfRows from, uint16_t* to) {
+  constexpr int N = Piece<T>::N;
+  const int per = ld / N;
+  const int64_t total = rows * per, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+    const int64_t row = i / per;
+    const int c = (int)(i % per) * N;
+    float v[N];
+    Piece<T>::load(static_cast<const T*>(from.p) + row * from.st + c, cols > c ? cols - c : 0, v);
+    put_planes<T, N>(to + row * ld + c, rows * ld, v);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void ff_parts_kernel(int64_t rows, int F, int ld, FfRows g, FfRows u, FfRows dy,
+                                                       uint16_t* to) {
+  constexpr int N = Piece<T>::N;
+  const int per = ld / N;
+  const int64_t total = rows * per, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+    const int64_t row = i / per;
+    const int c = (int)(i % per) * N, n = F > c ? F - c : 0;
+    float gv[N], uv[N], d[N], e[N];
+    Piece<T>::load(static_cast<const T*>(g.p) + row * g.st + c, n, gv);
+    Piece<T>::load(static_cast<const T*>(u.p) + row * u.st + c, n, uv);
+    Piece<T>::load(static_cast<const T*>(dy.p) + row * dy.st + c, n, d);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float s = sigmoid(gv[j]);
+      e[j] = d[j] * (gv[j] * s);
+      d[j] = d[j] * uv[j] * (s * (1.f + gv[j] * (1.f - s)));
+    }
+    put_planes<T, N>(to + row * 2 * ld + c, rows * 2 * ld, d);
+    put_planes<T, N>(to + (row * 2 + 1) * ld + c, rows * 2 * ld, e);
+  }
+}
+
+unsigned groups_of(int64_t n) {
+  const int64_t g = (n + 255) / 256;
+  return (unsigned)(g < 65536 ? g : 65536);
+}
+
+template <typename T>
+hipError_t step(int rows, int D, int F, FfRows x, FfRows wg, FfRows wu, FfRows y, FfRows g, FfRows u, hipStream_t st) {
+  const dim3 grid((F + 15) / 16), block(512);
+  switch ((rows + 15) / 16) {
+    case 1: hipLaunchKernelGGL((ff_step_kernel<T, 1>), grid, block, 0, st, rows, D, F, x, wg, wu, y, g, u); break;
+    case 2: hipLaunchKernelGGL((ff_step_kernel<T, 2>), grid, block, 0, st, rows, D, F, x, wg, wu, y, g, u); break;
+    case 3: hipLaunchKernelGGL((ff_step_kernel<T, 3>), grid, block, 0, st, rows, D, F, x, wg, wu, y, g, u); break;
+    default: hipLaunchKernelGGL((ff_step_kernel<T, 4>), grid, block, 0, st, rows, D, F, x, wg, wu, y, g, u); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_ff_step(int64_t rows, int D, int F, int dtype, FfRows x, FfRows wg, FfRows wu, FfRows y, FfRows g,
+                          FfRows u, hipStream_t st) {
+  return dtype == DLA_BF16 ? step<bf16_t>((int)rows, D, F, x, wg, wu, y, g, u, st)
+                           : step<float>((int)rows, D, F, x, wg, wu, y, g, u, st);
+}
+
+hipError_t launch_ff_pack(int64_t rows, int cols, int dtype, FfRows from, uint16_t* to, hipStream_t st) {
+  const int ld = (int)round_up(cols, 8), N = dtype == DLA_BF16 ? 8 : 4;
+  const dim3 grid(groups_of(rows * (ld / N))), block(256);
+  if (rows == 0) return hipSuccess;
+  if (dtype == DLA_BF16) hipLaunchKernelGGL(ff_pack_kernel<bf16_t>, grid, block, 0, st, rows, cols, ld, from, to);
+  else hipLaunchKernelGGL(ff_pack_kernel<float>, grid, block, 0, st, rows, cols, ld, from, to);
+  return hipGetLastError();
+}
+
+hipError_t launch_ff_parts(int64_t rows, int F, int dtype, FfRows g, FfRows u, FfRows dy, uint16_t* to, hipStream_t st) {
+  const int ld = (int)round_up(F, 8), N = dtype == DLA_BF16 ? 8 : 4;
+  const dim3 grid(groups_of(rows * (ld / N))), block(256);
+  if (rows == 0) return hipSuccess;
+  if (dtype == DLA_BF16) hipLaunchKernelGGL(ff_parts_kernel<bf16_t>, grid, block, 0, st, rows, F, ld, g, u, dy, to);
+  else hipLaunchKernelGGL(ff_parts_kernel<float>, grid, block, 0, st, rows, F, ld, g, u, dy, to);
+  return hipGetLastError();
+}
+
+}  // namespace dla

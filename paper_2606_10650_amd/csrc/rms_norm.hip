@@ -13,73 +13,11 @@
 // Rows may start at any element: a piece is read as it lies, whatever its alignment.
 #include "dla_common.h"
 #include "dla_train.h"
+#include "piece.h"
 #include "rms_norm.h"
 
 namespace dla {
 namespace {
-
-template <typename T>
-struct Piece {
-  static constexpr int N = 16 / (int)sizeof(T);
-  struct __attribute__((packed, aligned(sizeof(T)))) Raw {
-    uint32_t w[4];
-  };
-  // a piece as it lies, zero from element n on
-  __device__ static __forceinline__ Raw raw(const T* p, int n) {
-    if (n >= N) return *reinterpret_cast<const Raw*>(p);
-    Raw r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r.w[i] = 0u;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (i < n) {
-        if constexpr (sizeof(T) == 2) r.w[i >> 1] |= (uint32_t)p[i].x << (16 * (i & 1));
-        else r.w[i] = __float_as_uint(p[i]);
-      }
-    }
-    return r;
-  }
-  __device__ static __forceinline__ float value(const Raw& r, int i) {
-    if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? r.w[i >> 1] & 0xFFFF0000u : r.w[i >> 1] << 16);
-    else return __uint_as_float(r.w[i]);
-  }
-  __device__ static __forceinline__ void load(const T* p, int n, float (&x)[N]) {
-    const Raw r = raw(p, n);
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = value(r, i);
-  }
-  __device__ static __forceinline__ void store(T* p, int n, const float (&x)[N]) {
-    if constexpr (sizeof(T) == 2) {
-      if (n >= N) {
-        Raw r;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-          bf16x2 y;
-          y[0] = (__bf16)x[2 * i];
-          y[1] = (__bf16)x[2 * i + 1];
-          r.w[i] = __builtin_bit_cast(uint32_t, y);
-        }
-        *reinterpret_cast<Raw*>(p) = r;
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (i < n) reinterpret_cast<__bf16*>(p)[i] = (__bf16)x[i];
-      }
-    } else {
-      if (n >= N) {
-        Raw r;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.w[i] = __float_as_uint(x[i]);
-        *reinterpret_cast<Raw*>(p) = r;
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (i < n) p[i] = x[i];
-      }
-    }
-  }
-};
 
 // Eight-bit floating point (4 exponent, 3 mantissa bits, no infinity), round to nearest
 // even; |x| <= 448 or NaN.

@@ -1,0 +1,374 @@
+// The short causal convolution: z_t = bias + sum_j w_j x_{t - (W - 1) + j} per channel, y = silu(z);
+// and its backward pass.
+//
+// A thread holds a piece of channels (16 bytes of a row) with their taps in registers and walks
+// along a run of tokens with the last W - 1 inputs in registers too, so that an input is read
+// once but for the W - 1 in front of a run.  A document's start clears those registers.  The
+// backward pass forms z again and carries the W - 1 gradients that are not yet whole; behind its
+// run it reads W - 1 tokens more.  Bytes bound both.
+#include "piece.h"
+#include "short_conv.h"
+
+namespace dla {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+}
+
+__device__ __forceinline__ int length_of(const ConvArgs& a, int b) {
+  if (!a.lengths) return a.T;
+  const int n = a.lengths[b];
+  return n < 0 ? 0 : (n > a.T ? a.T : n);
+}
+
+// Taps and bias of a piece of channels.
+template <typename T, int W>
+struct Taps {
+  static constexpr int N = Piece<T>::N;
+  float w[W][N], bias[N];
+  __device__ __forceinline__ void load(const ConvArgs& a, int c, int n) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const int64_t at = (int64_t)(c + i) * W + j;
+        w[j][i] = i >= n ? 0.f : a.w_f32 ? static_cast<const float*>(a.w)[at] : to_f32(static_cast<const T*>(a.w)[at]);
+      }
+      bias[i] = 0.f;
+    }
+    if (a.bias) load_floats<T>(a.bias, a.w_f32, c, n, bias);
+  }
+};
+
+// The W - 1 inputs before a token, the latest last.
+template <typename T, int W>
+struct Window {
+  static constexpr int N = Piece<T>::N;
+  float x[W - 1][N];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[j][i] = 0.f;
+  }
+  __device__ __forceinline__ void push(const float (&v)[N]) {
+#pragma unroll
+    for (int j = 0; j + 1 < W - 1; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[j][i] = x[j + 1][i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[W - 2][i] = v[i];
+  }
+  // what token t of sequence b sees before its own start is looked at
+  __device__ __forceinline__ void before(const ConvArgs& a, int b, int t, int c, int n) {
+    clear();
+    float v[N];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+      const int p = t - (W - 1) + j;
+      if (p >= 0) {
+        if (a.starts && a.starts[(int64_t)b * a.T + p]) clear();
+        Piece<T>::load(static_cast<const T*>(a.x.p) + b * a.x.sb + p * a.x.st + c, n, v);
+        push(v);
+      } else if (a.state) {
+        Piece<T>::load(static_cast<const T*>(a.state) + ((int64_t)b * (W - 1) + W - 1 + p) * a.C + c, n, v);
+        push(v);
+      }
+    }
+  }
+};
+
+template <typename T, int W>
+__device__ __forceinline__ void convolve(const Taps<T, W>& k, const Window<T, W>& win,
+                                         const float (&x)[Piece<T>::N], float (&z)[Piece<T>::N]) {
+#pragma unroll
+  for (int i = 0; i < Piece<T>::N; ++i) {
+    z[i] = k.bias[i];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) z[i] += k.w[j][i] * win.x[j][i];
+    z[i] += k.w[W - 1][i] * x[i];
+  }
+}
+
+// Where a thread works: a piece of channels of a run of tokens of a sequence.
+struct Place {
+  int b, c, t0, t1;
+  bool any;
+};
+
+// A workgroup has `lanes` pieces side by side and 256 / lanes runs; one of the backward pass goes
+// on to the runs `pass` times all workgroups' on.
+__device__ __forceinline__ Place place_of(const ConvArgs& a, int N, int64_t pass) {
+  const int cols = (a.pieces + a.lanes - 1) / a.lanes, runs = 256 / a.lanes;
+  const int64_t run = (pass * a.groups + blockIdx.x / cols) * runs + threadIdx.x / a.lanes;
+  const int piece = (int)(blockIdx.x % cols) * a.lanes + threadIdx.x % a.lanes;
+  Place p;
+  p.any = run < (int64_t)a.B * a.chunks && piece < a.pieces;
+  p.b = (int)(run / a.chunks);
+  p.t0 = (int)(run % a.chunks) * a.per;
+  p.t1 = min(p.t0 + a.per, a.T);
+  p.c = piece * N;
+  return p;
+}
+
+template <typename T, int W>
+__global__ __launch_bounds__(256) void conv_kernel(ConvArgs a) {
+  constexpr int N = Piece<T>::N, G = 4;
+  using Raw = typename Piece<T>::Raw;
+  const Place p = place_of(a, N, 0);
+  if (!p.any) return;
+  const int n = a.C - p.c, len = length_of(a, p.b), end = min(p.t1, len);
+  const T* x = static_cast<const T*>(a.x.p) + p.b * a.x.sb + p.c;
+  T* y = static_cast<T*>(a.y.p) + p.b * a.y.sb + p.c;
+  const uint8_t* starts = a.starts ? a.starts + (int64_t)p.b * a.T : nullptr;
+  Taps<T, W> k;
+  k.load(a, p.c, n);
+  Window<T, W> win;
+  // (a run behind the sequence's end has nothing before it, and must not read the state)
+  if (p.t0 < len || p.t0 == 0) win.before(a, p.b, p.t0, p.c, n);
+  for (int t = p.t0; t < end; t += G) {
+    Raw raw[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) raw[g] = Piece<T>::raw(x + min(t + g, end - 1) * a.x.st, n);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (t + g < end) {
+        float v[N], z[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = Piece<T>::value(raw[g], i);
+        if (starts && starts[t + g]) win.clear();
+        convolve<T, W>(k, win, v, z);
+        win.push(v);
+        if (a.silu) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) z[i] *= sigmoid(z[i]);
+        }
+        Piece<T>::store(y + (t + g) * a.y.st, n, z);
+      }
+    }
+  }
+  if (end < p.t1) {
+    const float zero[N] = {};
+    for (int t = max(p.t0, end); t < p.t1; ++t) Piece<T>::store(y + t * a.y.st, n, zero);
+  }
+  // the first run's thread alone has read the given state, and writes the last one over it
+  if (a.state_out && p.t0 == 0) {
+    if (len > end) win.before(a, p.b, len, p.c, n);
+    T* s = static_cast<T*>(a.state_out) + (int64_t)p.b * (W - 1) * a.C + p.c;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) Piece<T>::store(s + (int64_t)j * a.C, n, win.x[j]);
+  }
+}
+
+template <typename T, int W>
+__global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
+  constexpr int N = Piece<T>::N;
+  __shared__ float sums[256 * N];
+  const int n = a.C - ((int)(blockIdx.x % ((a.pieces + a.lanes - 1) / a.lanes)) * a.lanes + (int)threadIdx.x % a.lanes) * N;
+  Taps<T, W> k;
+  if (n > 0) k.load(a, a.C - n, n);
+  float dw[W + 1][N];
+#pragma unroll
+  for (int j = 0; j <= W; ++j)
+#pragma unroll
+    for (int i = 0; i < N; ++i) dw[j][i] = 0.f;
+  for (int64_t pass = 0; pass < a.passes; ++pass) {
+    const Place p = place_of(a, N, pass);
+    if (!p.any) break;
+    const int len = length_of(a, p.b);
+    const T* x = static_cast<const T*>(a.x.p) + p.b * a.x.sb + p.c;
+    const T* dy = static_cast<const T*>(a.y.p) + p.b * a.y.sb + p.c;
+    T* dx = static_cast<T*>(a.dx.p) + p.b * a.dx.sb + p.c;
+    const uint8_t* starts = a.starts ? a.starts + (int64_t)p.b * a.T : nullptr;
+    Window<T, W> win;
+    win.before(a, p.b, min(p.t0, len), p.c, n);
+    float pend[W - 1][N];   // gradients of the W - 1 inputs before, the latest last
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) pend[j][i] = 0.f;
+    // Inputs before a token that its document has (W - 1: all there are room for).  Those of
+    // before the run have their gradients from the run before, but for the state's.
+    int age = W - 1;
+    if (starts)
+      for (int i = 0; i < W - 1; ++i)
+        if (p.t0 - 1 - i >= 0 && p.t0 <= len && starts[p.t0 - 1 - i]) {
+          age = i + 1;
+          break;
+        }
+    T* ds = a.dstate ? static_cast<T*>(a.dstate) + (int64_t)p.b * (W - 1) * a.C + p.c : nullptr;
+    // the gradient of input q of the sequence is whole
+    auto put = [&](int q, const float(&v)[N]) {
+      if (q >= p.t0 && q < p.t1) Piece<T>::store(dx + q * a.dx.st, n, v);
+      else if (q < 0 && p.t0 == 0 && ds) Piece<T>::store(ds + (int64_t)(W - 1 + q) * a.C, n, v);
+    };
+    const int last = min(min(p.t1, a.T - (W - 1)) + W - 1, len);   // t1 + W - 1 without leaving int32
+    int t = p.t0;
+    for (; t < last; ++t) {
+      float v[N], z[N], d[N];
+      Piece<T>::load(x + t * a.x.st, n, v);
+      Piece<T>::load(dy + t * a.y.st, n, d);
+      if (starts && starts[t]) {
+        win.clear();
+        age = 0;
+      }
+      if (a.silu) {
+        convolve<T, W>(k, win, v, z);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float s = sigmoid(z[i]);
+          d[i] *= s * (1.f + z[i] * (1.f - s));
+        }
+      }
+      if (t < p.t1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          dw[W][i] += d[i];
+          dw[W - 1][i] += d[i] * v[i];
+#pragma unroll
+          for (int j = 0; j < W - 1; ++j) dw[j][i] += d[i] * win.x[j][i];
+        }
+      }
+      win.push(v);
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+        if (W - 1 - j <= age) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) pend[j][i] += k.w[j][i] * d[i];
+        }
+      age = min(age + 1, W - 1);
+      put(t - (W - 1), pend[0]);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j) pend[j][i] = pend[j + 1][i];
+        pend[W - 2][i] = k.w[W - 1][i] * d[i];
+      }
+    }
+    if (p.t0 <= len) {
+      // the sequence's end: what the last state's gradient asks of the inputs that it shows
+      if (t == len && a.dstate_out) {
+        const T* g = static_cast<const T*>(a.dstate_out) + (int64_t)p.b * (W - 1) * a.C + p.c;
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j)
+          if (W - 1 - j <= age) {
+            float v[N];
+            Piece<T>::load(g + (int64_t)j * a.C, n, v);
+#pragma unroll
+            for (int i = 0; i < N; ++i) pend[j][i] += v[i];
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) put(t - (W - 1) + j, pend[j]);
+    }
+    const float zero[N] = {};
+    for (int q = max(p.t0, len); q < p.t1; ++q) Piece<T>::store(dx + q * a.dx.st, n, zero);
+  }
+  if (!a.part) return;
+  // the workgroup's runs one after the other into one sum
+  const int runs = 256 / a.lanes, lane = threadIdx.x % a.lanes;
+#pragma unroll
+  for (int j = 0; j <= W; ++j) {
+    if (runs > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < N; ++i) sums[i * 256 + threadIdx.x] = dw[j][i];
+      __syncthreads();
+      if (threadIdx.x < (unsigned)a.lanes) {
+        for (int r = 1; r < runs; ++r)
+#pragma unroll
+          for (int i = 0; i < N; ++i) dw[j][i] += sums[i * 256 + r * a.lanes + lane];
+      }
+    }
+  }
+  const int cols = (a.pieces + a.lanes - 1) / a.lanes;
+  const int piece = (int)(blockIdx.x % cols) * a.lanes + lane;
+  if (threadIdx.x < (unsigned)a.lanes && piece < a.pieces) {
+    float* part = a.part + ((int64_t)(blockIdx.x / cols) * a.C + piece * N) * (W + 1);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n)
+#pragma unroll
+        for (int j = 0; j <= W; ++j) part[i * (W + 1) + j] = dw[j][i];
+  }
+}
+
+// dw and dbias from the workgroups' parts: 32 columns a workgroup, 8 threads to a column, in a
+// fixed order, in float64
+__global__ __launch_bounds__(256) void conv_sum_kernel(const float* part, int parts, int C, int W, float* dw, float* db) {
+  __shared__ double sums[8][33];
+  const int col = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int64_t width = (int64_t)C * (W + 1), at = (int64_t)blockIdx.x * 32 + col;
+  double s = 0.;
+  if (at < width)
+    for (int i = r; i < parts; i += 8) s += part[i * width + at];
+  sums[r][col] = s;
+  __syncthreads();
+  if (r == 0 && at < width) {
+    for (int i = 1; i < 8; ++i) s += sums[i][col];
+    const int c = (int)(at / (W + 1)), j = (int)(at % (W + 1));
+    if (j < W) dw[(int64_t)c * W + j] = (float)s;
+    else if (db) db[c] = (float)s;
+  }
+}
+
+template <typename T, int W>
+hipError_t go(const ConvArgs& a, bool backward, float* dw, float* db, hipStream_t st) {
+  const int cols = (a.pieces + a.lanes - 1) / a.lanes;
+  const dim3 grid((unsigned)(cols * a.groups)), block(256);
+  if (!backward) {
+    if (grid.x) hipLaunchKernelGGL((conv_kernel<T, W>), grid, block, 0, st, a);
+  } else {
+    if (grid.x) hipLaunchKernelGGL((conv_backward_kernel<T, W>), grid, block, 0, st, a);
+    if (dw && a.C) {
+      const int64_t width = (int64_t)a.C * (W + 1);
+      hipLaunchKernelGGL(conv_sum_kernel, dim3((unsigned)((width + 31) / 32)), block, 0, st, a.part, (int)a.groups, a.C, W, dw, db);
+    }
+  }
+  return hipGetLastError();
+}
+
+hipError_t pick(const ConvArgs& a, int dtype, bool backward, float* dw, float* db, hipStream_t st) {
+  if (dtype == DLA_BF16) {
+    if (a.W == 2) return go<bf16_t, 2>(a, backward, dw, db, st);
+    if (a.W == 3) return go<bf16_t, 3>(a, backward, dw, db, st);
+    return go<bf16_t, 4>(a, backward, dw, db, st);
+  }
+  if (a.W == 2) return go<float, 2>(a, backward, dw, db, st);
+  if (a.W == 3) return go<float, 3>(a, backward, dw, db, st);
+  return go<float, 4>(a, backward, dw, db, st);
+}
+
+}  // namespace
+
+// Runs: as long as still fills the chip, so that few inputs are read twice and few parts of dw
+// are left.
+void plan_conv(ConvArgs& a, int dtype, bool backward) {
+  const int N = dtype == DLA_BF16 ? 8 : 4;
+  a.pieces = (int)(((int64_t)a.C + N - 1) / N);
+  a.lanes = 64;
+  while (a.lanes > 1 && a.lanes / 2 >= a.pieces) a.lanes /= 2;
+  const int64_t threads = backward ? 262144 : 524288, tokens = (int64_t)a.B * a.T;
+  int64_t runs = a.pieces ? threads / a.pieces : 1;   // wanted
+  if (runs < 1) runs = 1;
+  int64_t per = (tokens + runs - 1) / runs;
+  if (per < 8) per = 8;
+  if (per > a.T) per = a.T > 0 ? a.T : 1;
+  a.per = (int)per;
+  a.chunks = a.T > 0 ? (int)(((int64_t)a.T + per - 1) / per) : 1;
+  const int64_t each = 256 / a.lanes, groups = ((int64_t)a.B * a.chunks + each - 1) / each, most = runs / each + 1;
+  a.passes = backward && groups > most ? (int)((groups + most - 1) / most) : 1;
+  a.groups = (groups + a.passes - 1) / a.passes;
+}
+
+hipError_t launch_conv(const ConvArgs& a, int dtype, hipStream_t st) {
+  return pick(a, dtype, false, nullptr, nullptr, st);
+}
+
+hipError_t launch_conv_backward(const ConvArgs& a, int dtype, float* dw, float* db, hipStream_t st) {
+  return pick(a, dtype, true, dw, db, st);
+}
+
+}  // namespace dla

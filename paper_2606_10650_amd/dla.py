@@ -33,7 +33,13 @@ EXPORTED = ("dla_cache_layout_of", "dla_state_cache_alloc", "dla_cache_flags",
             # bound by paper_2606_10650_amd.train
             "dla_recurrence_workspace_size", "dla_recurrence_forward", "dla_recurrence_backward",
             "dla_rms_norm", "dla_rms_norm_fp8", "dla_rms_norm_workspace_size",
-            "dla_rms_norm_backward", "dla_adamw_step")
+            "dla_rms_norm_backward", "dla_adamw_step",
+            # bound by paper_2606_10650_amd.block
+            "dla_short_conv", "dla_short_conv_workspace_size", "dla_short_conv_backward",
+            "dla_gated_norm", "dla_gated_norm_workspace_size", "dla_gated_norm_backward",
+            "dla_token_logprobs_workspace_size", "dla_token_logprobs",
+            "dla_token_logprobs_backward", "dla_gated_ff_workspace_size", "dla_gated_ff",
+            "dla_gated_ff_backward")
 STATIC_SCRATCH_BYTES = 128 << 20   # DLA_STATIC_SCRATCH_BYTES
 
 
