@@ -168,7 +168,8 @@ dla_status dla_token_logprobs(const dla_logprobs_desc* desc, const dla_norm_rows
 /* The gradient of the logits from those of logprob, entropy and lse, float32 [rows] (NULL for
  * zero), and the forward pass's lse, logprob (with dlogprob) and entropy (with dentropy):
  *   dl_i = dlogprob ([i = token] - p_i) - dentropy p_i (log p_i + entropy) + dlse p_i
- * dlogits may be the logits' array. */
+ * p_i is exp(l_i - lse), off by |lse| 2^-24 of itself for lse's rounding.  dlogits may be the
+ * logits' array. */
 dla_status dla_token_logprobs_backward(const dla_logprobs_desc* desc, const dla_norm_rows* logits,
                                        const int64_t* tokens, const float* logprob,
                                        const float* lse, const float* entropy,

@@ -277,7 +277,7 @@ bool large(int kind, int64_t M, int64_t N) {
 
 // Parts of the sum over K: as many as still give every compute unit a tile, of at least 8 steps.
 int ff_split(int kind, int64_t M, int64_t N, int64_t K, int pairs) {
-  if (kind == 0 || large(kind, M, N)) return 1;
+  if (kind == 0 || M == 0 || large(kind, M, N)) return 1;
   const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128), steps = (K + kStep - 1) / kStep * pairs;
   int64_t s = 512 / tiles;
   if (s > steps / 8) s = steps / 8;

@@ -1,0 +1,222 @@
+"""The norm with gate, residual sum and next norm, and its backward pass, against their formulas in
+float64; and what is refused.
+
+Tolerances.  As the residual norm's: float32 sums of D squares, all of one sign, are off by at most
+D 2^-24 in any order and by sqrt(D) 2^-24 in a tree's, so 1e-5 of a row's norm holds for D <= 16384
+with room for the gate's sigmoid (at most (8 + 2 |z|) 2^-24) and the products; outputs in bfloat16 are
+rounded once, by 2^-8.  Gradients are differences of two terms, and are compared relative to both.
+"""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+TOL = {"bf16": 2.0 ** -8 + 1e-5, "f32": 1e-5}
+FORMS = [dict(), dict(gate=True), dict(residual=True, scale=0.5), dict(gate=True, residual=True, next=True, scale=0.25),
+         dict(residual=True, next=True), dict(next=True, gate=True)]
+
+
+def _block():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2606_10650_amd import block
+    return block
+
+
+def make(N, G, D, dtype, *, gate=False, residual=False, next=False, scale=1.0, per_group=False, wf32=False, seed=0):  # noqa: A002
+    gen = torch.Generator(device="cuda").manual_seed(seed + 7 * N + D)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    dt = DT[dtype]
+    wdt = torch.float32 if wf32 else dt
+    row = lambda f=1.0: (f * rnd(N, G, D)).to(dt)  # noqa: E731
+    s = dict(x=(torch.exp(2 * rnd(N, G, 1)) * rnd(N, G, D)).to(dt), gate=row(2.0) if gate else None,
+             residual=row(2.0) if residual else None, w=(1 + 0.2 * (rnd(G, D) if per_group else rnd(D))).to(wdt),
+             next=(1 + 0.2 * rnd(D)).to(wdt) if next else None, scale=scale, eps=1e-5, dh=row())
+    s["dy"] = row() if next else None
+    return s
+
+
+def formula(s):
+    """Outputs and gradients in float64, by automatic differentiation of the formula."""
+    v = {k: s[k].double().requires_grad_() for k in ("x", "gate", "residual", "w", "next") if s[k] is not None}
+    D = s["x"].shape[-1]
+    n = v["x"] / (v["x"].square().sum(-1, keepdim=True) / D + s["eps"]).sqrt() * v["w"]
+    b = n * v["gate"] * torch.sigmoid(v["gate"]) if "gate" in v else n
+    h = s["scale"] * b + (v["residual"] if "residual" in v else 0)
+    loss, y = (h * s["dh"].double()).sum(), None
+    if "next" in v:
+        y = v["next"] * h / (h.square().sum(-1, keepdim=True) / D + s["eps"]).sqrt()
+        loss = loss + (y * s["dy"].double()).sum()
+    loss.backward()
+    return h.detach(), None if y is None else y.detach(), {k: t.grad for k, t in v.items()}
+
+
+def call(block, s, **kw):
+    f = lambda t: t  # noqa: E731
+    h, y, rstd, y_rstd = block.gated_norm(s["x"], s["w"], s["gate"], s["residual"], scale=s["scale"],
+                                          next_weight=s["next"], eps=s["eps"])
+    g = block.gated_norm_backward(s["dh"], s["x"], s["w"], rstd, s["gate"], s["residual"], scale=s["scale"],
+                                  next_weight=s["next"], dy=s["dy"], y_rstd=y_rstd, **kw)
+    return h, y, rstd, y_rstd, dict(zip(("x", "gate", "residual", "w", "next"), g))
+
+
+def close(got, want, tol, terms=0.0):
+    """Row by row (of the last axis), but for `terms` relative to the reference's norm."""
+    assert torch.isfinite(got.double()).all()
+    err, norm = (got.double() - want).norm(dim=-1), want.norm(dim=-1) + terms
+    assert (err <= tol * norm + 1e-30).all(), ((err / (norm + 1e-30)).max().item(), tol)
+
+
+def check(block, s, dtype):
+    h, y, rstd, y_rstd, g = call(block, s)
+    H, Y, G = formula(s)
+    D = s["x"].shape[-1]
+    close(h, H, TOL[dtype])
+    X = s["x"].double()
+    close(rstd[..., None], (1 / (X.square().sum(-1) / D + s["eps"]).sqrt())[..., None], 1e-5)
+    R2 = 0.0
+    if Y is not None:
+        close(y, Y, TOL[dtype])
+        R2 = 1 / (H.square().sum(-1) / D + s["eps"]).sqrt()
+        close(y_rstd[:, None, None], R2[..., None], 1e-5)
+        R2 = R2 * (s["dy"].double() * s["next"].double()).norm(dim=-1)
+    # what reaches h: its own gradient and, with a next norm, two terms of size R2
+    into = s["dh"].double().norm(dim=-1) + 2 * R2
+    if s["residual"] is not None:
+        close(g["residual"], G["residual"], TOL[dtype], into)
+    else:
+        assert g["residual"] is s["dh"] or s["next"] is not None
+    w = s["w"].double().abs().amax()
+    act, slope, n = 1.0, None, (X * rstd.double()[..., None]).abs().amax(-1) * w
+    if s["gate"] is not None:
+        z = s["gate"].double()
+        act = (z * torch.sigmoid(z)).abs().amax(-1)
+        close(g["gate"], G["gate"], TOL[dtype], 1e-3 * s["scale"] * into * n * 1.1)
+    # dx: two terms, each of r scale w act into at most; what reaches h is off by 1e-5 of `into`
+    close(g["x"], G["x"], TOL[dtype], 2 * rstd.double() * s["scale"] * w * act * into)
+    # weights' gradients: sums of float32 terms over the rows, in float32 runs and float64 between
+    rows = lambda t: t.norm() if torch.is_tensor(t) else t  # noqa: E731
+    assert (g["w"].double() - G["w"]).norm() <= 2e-5 * ((s["scale"] * into * act * n / w).norm() + G["w"].norm())
+    if Y is not None:
+        n2 = (s["dy"].double() * H).norm(dim=-1) / (H.square().sum(-1) / D + s["eps"]).sqrt()
+        assert (g["next"].double() - G["next"]).norm() <= 2e-5 * (rows(n2) + G["next"].norm())
+
+
+@pytest.mark.parametrize("N,D", [(1, 1), (3, 2), (5, 7), (1, 64), (33, 65), (7, 512), (2, 1000), (1100, 1531), (1030, 2048),
+                                 (9, 2049), (5, 4100), (3, 8200), (2, 16384)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_rows(N, D, dtype, form):
+    block = _block()
+    check(block, make(N, 1, D, dtype, **FORMS[form], wf32=form % 2 == 1), dtype)
+
+
+@pytest.mark.parametrize("N,G,D", [(1, 2, 1), (4, 3, 64), (50, 16, 128), (9, 48, 64), (700, 5, 40), (2, 33, 300), (3, 7, 1000),
+                                   (2, 2, 5000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("per_group", [False, True])
+def test_groups(N, G, D, dtype, per_group):
+    block = _block()
+    for form in FORMS[:3]:
+        check(block, make(N, G, D, dtype, **form, per_group=per_group), dtype)
+
+
+def test_strides():
+    """Slices of wider projections at any element, tokens before heads, and a broadcast gate."""
+    block = _block()
+    s = make(37, 6, 48, "bf16", gate=True, residual=True, scale=0.5)
+    plain = call(block, s)
+    wide = torch.full((37, 6 * 48 + 5), float("nan"), dtype=torch.bfloat16, device="cuda")
+    v = dict(s)
+    for off in (0, 3, 5):
+        wide[:, off:off + 288] = s["gate"].flatten(1)
+        v["gate"] = wide[:, off:off + 288].unflatten(1, (6, 48))
+        v["x"] = s["x"].transpose(0, 1).contiguous().transpose(0, 1)      # groups outermost
+        v["dh"] = torch.nn.functional.pad(s["dh"], (1, 2))[..., 1:49]
+        got = call(block, v)
+        assert torch.equal(got[0], plain[0])
+        for k in ("x", "gate", "w"):
+            assert torch.equal(got[4][k], plain[4][k]), k
+    one = s["gate"][:1]
+    assert torch.equal(call(block, dict(s, gate=one.expand(37, -1, -1)))[0],
+                       call(block, dict(s, gate=one.expand(37, -1, -1).contiguous()))[0])
+
+
+@pytest.mark.parametrize("D", [128, 777, 4096])
+def test_range(D):
+    """Rows whose squares leave float32's range, a row of zeros, and rows with an infinity or NaN, which
+    leave the others as they are."""
+    block = _block()
+    s = make(8, 1, D, "f32", gate=True)
+    s["x"][1] *= 1e25
+    s["x"][2] *= 1e-30
+    s["x"][3] = 0
+    s["x"][4, 0, D // 2] = float("inf")
+    s["x"][5, 0, D - 1] = float("nan")
+    s["eps"] = 0.0
+    h, _, rstd, _ = block.gated_norm(s["x"], s["w"], s["gate"], eps=0.0)
+    ok = [0, 1, 2, 6, 7]
+    X = s["x"].double()[ok]
+    n = X / X.square().mean(-1, keepdim=True).sqrt() * s["w"].double()
+    z = s["gate"].double()[ok]
+    close(h[ok], n * z * torch.sigmoid(z), 1e-5)
+    assert not h[3].any() and rstd[3] == 0
+    assert torch.isnan(h[4]).any() and torch.isnan(h[5]).all()
+    dx, dgate, _, _, _ = block.gated_norm_backward(s["dh"], s["x"], s["w"], rstd, s["gate"])
+    assert torch.isfinite(dx[ok]).all() and torch.isfinite(dgate[ok]).all() and not dx[3].any()
+
+
+def test_in_place_and_same_bits():
+    """h over x and over the residual; gradients over their gradients' arrays; the same again and on
+    another stream."""
+    block = _block()
+    s = make(300, 1, 640, "bf16", gate=True, residual=True, next=True, scale=0.5)
+    a = call(block, s)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        b = call(block, s)
+    stream.synchronize()
+    for p, q in zip(a[:4], b[:4]):
+        assert torch.equal(p, q)
+    for k in a[4]:
+        assert torch.equal(a[4][k], b[4][k]), k
+    from paper_2606_10650_amd import train
+    L = block.lib()
+    row = lambda t: block._group_rows(t, s["x"], "t")  # noqa: E731
+    desc = block._gated_desc(s["x"], s["w"], s["next"], s["eps"], s["scale"])
+    for over in ("x", "residual"):
+        t = s[over].clone()
+        v = dict(s, **{over: t})
+        y = torch.empty_like(t)
+        assert L.dla_gated_norm(desc, row(v["x"]), row(v["gate"]), row(v["residual"]), s["w"].data_ptr(),
+                                s["next"].data_ptr(), row(t), row(y), None, None, train._stream(t.device)) == 0
+        assert torch.equal(t, a[0]) and torch.equal(y, a[1])
+
+
+def test_captured():
+    block = _block()
+    s = make(64, 1, 512, "bf16", gate=True, residual=True, next=True)
+    ws = torch.empty(block.gated_norm_workspace_bytes(64, 1, 512), dtype=torch.uint8, device="cuda")
+    call(block, s, workspace=ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call(block, s, workspace=ws)
+    for i in range(4):
+        for k in ("x", "gate", "residual", "dh", "dy"):
+            s[k].copy_(torch.randn(s[k].shape, device="cuda"))
+        want = call(block, s)
+        graph.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(got[:4], want[:4]):
+            assert torch.equal(p, q)
+        for k in want[4]:
+            assert torch.equal(got[4][k], want[4][k]), k
+
+
+def test_empty():
+    block = _block()
+    s = make(0, 1, 64, "f32", residual=True, next=True)
+    h, y, _, _, g = call(block, s)
+    assert h.numel() == 0 and y.numel() == 0 and not g["w"].any() and not g["next"].any()
