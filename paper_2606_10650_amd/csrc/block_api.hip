@@ -180,7 +180,7 @@ FfSpace space_of(const dla_ff_desc& d, bool backward, bool direct) {
   FfSpace s;
   memset(&s, 0, sizeof(s));
   s.split_dx = s.split_dw = 1;
-  if (!backward && d.rows <= kFfStepRows) return s;
+  if (d.rows == 0 || (!backward && d.rows <= kFfStepRows)) return s;
   size_t used = 0;
   auto take = [&](size_t bytes) {
     const size_t x = used;
@@ -210,11 +210,12 @@ FfSpace space_of(const dla_ff_desc& d, bool backward, bool direct) {
 void pairs_of(FfGemm& g, int planes, int sets) {
   static const uint8_t a[6] = {2, 0, 1, 1, 0, 0}, b[6] = {0, 2, 1, 0, 1, 0};
   g.pairs = 0;
+  g.ia = g.ib = 0;
   const int n = planes == 1 ? 1 : 6;
   for (int i = 0; i < n; ++i)
     for (int s = 0; s < sets; ++s) {
-      g.ia[g.pairs] = (uint8_t)(planes * s + (planes == 1 ? 0 : a[i]));
-      g.ib[g.pairs++] = (uint8_t)(planes * s + (planes == 1 ? 0 : b[i]));
+      g.ia |= (uint64_t)(planes * s + (planes == 1 ? 0 : a[i])) << (4 * g.pairs);
+      g.ib |= (uint64_t)(planes * s + (planes == 1 ? 0 : b[i])) << (4 * g.pairs++);
     }
 }
 

@@ -36,7 +36,7 @@ struct FfGemm {
   const uint16_t* b[kFfPlanes];
   const uint16_t* b2[kFfPlanes];
   int64_t lda, ldb;
-  uint8_t ia[kFfPairs], ib[kFfPairs];
+  uint64_t ia, ib;    // four bits a pair, the first in the lowest
   FfRows c, g, u;     // kind 0: c is y
   FfRows c2;          // kind 2: where the rows from `half` on go; each half has `rows` of them
   int64_t half, rows;

@@ -1,12 +1,12 @@
 // The products of the gated feed-forward block on the matrix units: bfloat16 operands, float32
-// sums.  Tiles of the operands go from memory straight into LDS, two steps of K at a time, while
-// the tiles before them are multiplied.
+// sums.  Tiles of the operands go through registers into LDS, two steps of K ahead, while the tiles
+// before them are multiplied.
 //
-// A tile of rows whose K values are contiguous lies in LDS as 64 values a row, its 16-byte pieces
-// exchanged by the row's number modulo 8, so that eight lanes that read a piece of eight rows
-// have all banks; a tile whose rows are K (an operand that is used transposed) as it lies in
-// memory, 64-byte units exchanged by the row modulo 4, and is transposed by the reads of 4 rows of
-// 16 columns.  What lies outside an operand is zero.
+// A tile of rows whose K values are contiguous lies in LDS as kStep values a row, its 16-byte pieces
+// exchanged by the row's number, so that sixteen lanes that read a piece of sixteen rows have all
+// banks; a tile whose rows are K (an operand that is used transposed) as it lies in memory, 64-byte
+// units exchanged by the row modulo 4, and is transposed by the reads of 4 rows of 16 columns.
+// What lies outside an operand is zero.
 #include "gated_ff.h"
 #include "mfma.h"
 
@@ -25,18 +25,20 @@ template <int R, bool ALONG>   // ALONG: K values are contiguous
 struct FfTile {
   static constexpr int BYTES = R * kStep * 2;
   static constexpr int PIECES = BYTES / 16;
+  static constexpr int PR = kStep / 8;   // pieces of a row, where K is contiguous
+  __device__ static __forceinline__ int swap(int row) { return (row / (16 / PR)) & (PR - 1); }
   // row and first column of the piece that lies at place p (ALONG: row, K value; else K value, column)
-  __device__ static __forceinline__ int row(int p) { return ALONG ? p >> 3 : p / (R / 8); }
+  __device__ static __forceinline__ int row(int p) { return ALONG ? p / PR : p / (R / 8); }
   __device__ static __forceinline__ int col(int p) {
-    if (ALONG) return ((p & 7) ^ ((p >> 3) & 7)) * 8;
+    if (ALONG) return ((p % PR) ^ swap(p / PR)) * 8;
     const int k = p / (R / 8);
     return ((p % (R / 8)) ^ ((k & 3) << 2)) * 8;
   }
   // operand of a 32 x 32 x 16 product: row r0 + lane % 32, K values 16 kk + 8 (lane / 32) + e
   __device__ static __forceinline__ bf16x8 frag(const char* t, int r0, int kk, int lane) {
     if constexpr (ALONG) {
-      const int r = r0 + (lane & 31), c = (2 * kk + (lane >> 5)) ^ (r & 7);
-      return *reinterpret_cast<const bf16x8*>(t + r * 128 + c * 16);
+      const int r = r0 + (lane & 31), c = (2 * kk + (lane >> 5)) ^ swap(r);
+      return *reinterpret_cast<const bf16x8*>(t + (r * PR + c) * 16);
     } else {
       typedef short s16x4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) s16x4 lds4;
@@ -51,7 +53,7 @@ struct FfTile {
 };
 
 // Where a thread's pieces of a tile come from: byte offsets from the tile's first element, or one
-// that is outside.  `rows` and `cols` are what the operand has from the tile's corner on.
+// that is outside.
 constexpr uint32_t kOutside = 0x80000000u;
 
 template <int R, bool ALONG, int THREADS>
@@ -60,73 +62,81 @@ struct FfLoad {
   static constexpr int N = Tile::PIECES / THREADS;
   static_assert(Tile::PIECES % THREADS == 0, "whole pieces per thread");
   uint32_t off[N];
-  // ALONG: the row is inside, whichever step; else the column
+  // `left`: rows (ALONG) or columns that the operand has from the tile's corner on; MIXED: 32 rows of
+  // one operand and of another in turn
+  template <bool MIXED>
   __device__ __forceinline__ void init(int64_t left, int64_t ld, int tid) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int p = i * THREADS + tid, r = Tile::row(p), c = Tile::col(p);
+      const int p = i * THREADS + tid, c = Tile::col(p);
+      int r = Tile::row(p);
+      if (MIXED) r = (r >> 6) * 32 + (r & 31);
       off[i] = (ALONG ? r : c) < left ? (uint32_t)((r * ld + c) * 2) : kOutside;
     }
   }
-  // the step from `base` on, of which `left` K values are the operand's
-  __device__ __forceinline__ void issue(const uint16_t* base, int64_t left, char* lds, int tid) const {
+  // Piece i of the step from `base` on, of which `left` K values are the operand's.
+  __device__ __forceinline__ u32x4 get(int i, const uint16_t* base, int64_t left, int tid) const {
     const __amdgpu_buffer_rsrc_t src =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), (short)0, 0x7FFFFFFF, 0x00020000);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
+    uint32_t o = off[i];
+    if (left < kStep) {
       const int p = i * THREADS + tid;
-      const int k = ALONG ? Tile::col(p) : Tile::row(p);
-      const uint32_t o = k < left ? off[i] : kOutside;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          src, (__attribute__((address_space(3))) void*)(lds + (i * THREADS + (tid & ~63)) * 16), 16, (int)o, 0, 0, 0);
+      if ((ALONG ? Tile::col(p) : Tile::row(p)) >= left) o = kOutside;
     }
+    return __builtin_amdgcn_raw_buffer_load_b128(src, (int)o, 0, 0);
   }
 };
 
-__device__ __forceinline__ void put(const FfRows& r, int64_t row, int64_t col, float v, int f32) {
-  if (f32) static_cast<float*>(r.p)[row * r.st + col] = v;
-  else static_cast<__bf16*>(r.p)[row * r.st + col] = (__bf16)v;
-}
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-// An element of C.
-template <int KIND>
-__device__ __forceinline__ void put_c(const FfGemm& p, int64_t m, int64_t n, float v) {
-  if constexpr (KIND == 2) {
-    const bool second = m >= p.half;
-    const int64_t row = second ? m - p.half : m;
-    const FfRows& r = second ? p.c2 : p.c;
-    if (row < p.rows && r.p) put(r, row, n, v, p.out_f32);
+// Row m and columns n .. n + 3 of a tile of C, where they are inside.
+__device__ __forceinline__ void put4(const FfRows& r, int64_t m, int64_t n, int64_t N, int f32, const float (&v)[4]) {
+  if (f32) {
+    float* p = static_cast<float*>(r.p) + m * r.st + n;
+    if (n + 4 <= N && ((uintptr_t)p & 15) == 0) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (n + e < N) p[e] = v[e];
   } else {
-    put(p.c, m, n, v, p.out_f32);
+    __bf16* p = static_cast<__bf16*>(r.p) + m * r.st + n;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < N) p[e] = (__bf16)v[e];
   }
 }
 
 // KIND as in gated_ff.h.  WM x WN waves, each with a tile of (TM / WM) x (TN / WN); of kind 0 the
 // tile's columns are TN / 2 of B and as many of B2, 32 in turn, so that a wave has g and u of the
 // same columns.
+//
+// The products' first operand is B's, so that a lane holds a row of C and four neighbours of its columns.
+// A wave reads its operands of 16 K values ahead of the products of the 16 before; those of a step's
+// first 16 follow the barrier that the step's last products are still to come behind, so that neither
+// the barrier nor LDS makes the matrix unit wait.
 template <int KIND, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, int tiles_m, int tiles_n) {
   constexpr int THREADS = 64 * WM * WN;
-  constexpr bool AL = KIND != 2, BL = KIND == 0;
+  constexpr bool AL = KIND != 2, BL = KIND == 0, MIXED = KIND == 0;
   using TA = FfTile<TM, AL>;
   using TB = FfTile<TN, BL>;
-  constexpr int SM = TM / WM / 32, SN = TN / WN / 32;
+  constexpr int SM = TM / WM / 32, SN = TN / WN / 32, KK = kStep / 16;
   constexpr int WIDTH = KIND == 0 ? TN / 2 : TN;    // columns of C that a tile has
+  constexpr int BUFFER = TA::BYTES + TB::BYTES;
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
 
   // workgroups that run together (every eighth on one die) have neighbouring tiles
-  const int64_t total = (int64_t)tiles_m * tiles_n * p.split;
+  const int64_t tiles = (int64_t)tiles_m * tiles_n, total = tiles * p.split;
   int64_t id = blockIdx.x;
   {
     const int64_t each = total / 8, rest = total % 8, x = id % 8, y = id / 8;
     id = x * each + (x < rest ? x : rest) + y;
   }
-  const int64_t tiles = (int64_t)tiles_m * tiles_n;
   const int part = (int)(id / tiles);
   id %= tiles;
-  constexpr int GROUP = 8;   // tiles of M that go through the tiles of N together
+  constexpr int GROUP = 4;   // tiles of M that go through the tiles of N together
   const int64_t g0 = id / ((int64_t)GROUP * tiles_n) * GROUP;
   const int gm = (int)(tiles_m - g0 < GROUP ? tiles_m - g0 : GROUP);
   const int64_t in = id - g0 * tiles_n;
@@ -134,47 +144,57 @@ __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, int til
 
   FfLoad<TM, AL, THREADS> la;
   FfLoad<TN, BL, THREADS> lb;
-  la.init(p.M - m0, p.lda, tid);
-  if constexpr (KIND == 0) {
-    // rows 64 i .. 64 i + 31 of the tile are B's 32 i .., the next 32 B2's
-#pragma unroll
-    for (int i = 0; i < lb.N; ++i) {
-      const int q = i * THREADS + tid, r = TB::row(q), n = (r >> 6) * 32 + (r & 31);
-      lb.off[i] = n < p.N - n0 ? (uint32_t)((n * p.ldb + TB::col(q)) * 2) : kOutside;
-    }
-  } else {
-    lb.init(p.N - n0, p.ldb, tid);
-  }
+  la.template init<false>(p.M - m0, p.lda, tid);
+  lb.template init<MIXED>(p.N - n0, p.ldb, tid);
 
   const int64_t ksteps = (p.K + kStep - 1) / kStep, steps = ksteps * p.pairs;
   const int64_t first = steps * part / p.split, last = steps * (part + 1) / p.split;
 
-  auto issue = [&](int64_t s, int buf) {
-    const int pair = (int)(s / ksteps);
-    const int64_t k0 = (s % ksteps) * kStep;
-    char* at = smem + buf * (TA::BYTES + TB::BYTES);
-    const uint16_t* a = p.a[p.ia[pair]];
-    la.issue(AL ? a + m0 * p.lda + k0 : a + k0 * p.lda + m0, p.K - k0, at, tid);
-    const uint16_t* b = p.b[p.ib[pair]];
-    if constexpr (KIND == 0) {
-      const uint16_t* b2 = p.b2[p.ib[pair]];
-      const __amdgpu_buffer_rsrc_t s1 = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint16_t*>(b + n0 * p.ldb + k0), (short)0, 0x7FFFFFFF, 0x00020000);
-      const __amdgpu_buffer_rsrc_t s2 = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint16_t*>(b2 + n0 * p.ldb + k0), (short)0, 0x7FFFFFFF, 0x00020000);
-#pragma unroll
-      for (int i = 0; i < lb.N; ++i) {
-        // a wave's 64 pieces are 8 rows, all of one operand
-        const int q = i * THREADS + tid;
-        const uint32_t o = TB::col(q) < p.K - k0 ? lb.off[i] : kOutside;
-        auto* to = (__attribute__((address_space(3))) void*)(at + TA::BYTES + (i * THREADS + (tid & ~63)) * 16);
-        if (((i * THREADS / 64 + wave) >> 2) & 1)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(s2, to, 16, (int)o, 0, 0, 0);
-        else
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(s1, to, 16, (int)o, 0, 0, 0);
-      }
+  // where the next step to ask for lies
+  const int64_t da = AL ? kStep : kStep * p.lda, db = BL ? kStep : kStep * p.ldb;
+  int pair = 0;
+  int64_t k = 0;
+  const uint16_t *pa = nullptr, *pb = nullptr, *pb2 = nullptr;
+  auto seek = [&]() {
+    const int ia = (int)(p.ia >> (4 * pair)) & 15, ib = (int)(p.ib >> (4 * pair)) & 15;
+    pa = p.a[ia] + (AL ? m0 * p.lda + k : k * p.lda + m0);
+    pb = p.b[ib] + (BL ? n0 * p.ldb + k : k * p.ldb + n0);
+    if (MIXED) pb2 = p.b2[ib] + n0 * p.ldb + k;
+  };
+  if (first < last) {
+    pair = (int)(first / ksteps);
+    k = (first - pair * ksteps) * kStep;
+    seek();
+  }
+  constexpr int PIECES = la.N + lb.N;    // of a step, per thread
+  int64_t todo = last - first;           // steps to ask for; those behind the last are zeros
+  u32x4 piece[PIECES];
+  auto get = [&](int i) {
+    const int64_t left = todo > 0 ? p.K - k : 0;
+    if (i < la.N) {
+      piece[i] = la.get(i, pa, left, tid);
     } else {
-      lb.issue(BL ? b + n0 * p.ldb + k0 : b + k0 * p.ldb + n0, p.K - k0, at + TA::BYTES, tid);
+      // (of kind 0 a wave's 64 pieces are of one operand)
+      const int j = i - la.N;
+      const bool second = MIXED && (((j * THREADS / 64 + wave) * (64 / TB::PR) >> 5) & 1);
+      piece[i] = lb.get(j, second ? pb2 : pb, left, tid);
+    }
+  };
+  auto put = [&](int i, int buf) {
+    const int at = i < la.N ? i * THREADS * 16 : TA::BYTES + (i - la.N) * THREADS * 16;
+    *reinterpret_cast<u32x4*>(smem + buf * BUFFER + at + tid * 16) = piece[i];
+  };
+  auto advance = [&]() {
+    --todo;
+    k += kStep;
+    if (k < p.K) {
+      pa += da;
+      pb += db;
+      if (MIXED) pb2 += db;
+    } else if (todo > 0) {
+      ++pair;
+      k = 0;
+      seek();
     }
   };
 
@@ -183,60 +203,142 @@ __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, int til
   for (int i = 0; i < SM; ++i)
 #pragma unroll
     for (int j = 0; j < SN; ++j) acc[i][j] = zero16();
-  if (first < last) issue(first, 0);
-  for (int64_t s = first; s < last; ++s) {
-    const int buf = (int)(s - first) & 1;
-    // this step's tiles have come, the other's are no longer read
-    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt 0
+  bf16x8 fa[2][SM], fb[2][SN];
+  auto read = [&](int buf, int kk, int to) {
+    const char* a = smem + buf * BUFFER;
+#pragma unroll
+    for (int j = 0; j < SN; ++j) fb[to][j] = TB::frag(a + TA::BYTES, wn * (TN / WN) + 32 * j, kk, lane);
+#pragma unroll
+    for (int i = 0; i < SM; ++i) fa[to][i] = TA::frag(a, wm * (TM / WM) + 32 * i, kk, lane);
+  };
+  auto products = [&](int of, int i) {
+#pragma unroll
+    for (int j = 0; j < SN; ++j) Frag<bf16_t>::mma(acc[i][j], fb[of][j], fa[of][i]);
+  };
+  const int n = (int)(last - first);
+  if (n > 0) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) get(i);
+    advance();
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) put(i, 0);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) get(i);
+    advance();
     __syncthreads();
-    if (s + 1 < last) issue(s + 1, buf ^ 1);
-    const char* a = smem + buf * (TA::BYTES + TB::BYTES);
-    const char* b = a + TA::BYTES;
+    read(0, 0, 0);
+    for (int s = 0; s < n; ++s) {
+      const int buf = s & 1;
+      // Between the products the next step's pieces go from registers to LDS, and those of the step after
+      // it are asked for.
 #pragma unroll
-    for (int kk = 0; kk < kStep / 16; ++kk) {
-      bf16x8 fa[SM], fb[SN];
+      for (int kk = 0; kk < KK; ++kk) {
+        if (kk + 1 < KK) {
+          read(buf, kk + 1, (kk + 1) & 1);
+        } else if (s + 1 < n) {
+          __syncthreads();
+          read(buf ^ 1, 0, 0);
+        }
 #pragma unroll
-      for (int i = 0; i < SM; ++i) fa[i] = TA::frag(a, wm * (TM / WM) + 32 * i, kk, lane);
+        for (int i = 0; i < SM; ++i) {
+          products(kk & 1, i);
+          constexpr int ROWS = SM * (KK - 1);   // all before the barrier
+          const int row = kk * SM + i;
+          __builtin_amdgcn_sched_barrier(0);
+          if (row < ROWS) {
 #pragma unroll
-      for (int j = 0; j < SN; ++j) fb[j] = TB::frag(b, wn * (TN / WN) + 32 * j, kk, lane);
-#pragma unroll
-      for (int i = 0; i < SM; ++i)
-#pragma unroll
-        for (int j = 0; j < SN; ++j) Frag<bf16_t>::mma(acc[i][j], fa[i], fb[j]);
-    }
-  }
-
-  const int l32 = lane & 31;
-#pragma unroll
-  for (int i = 0; i < SM; ++i) {
-    if constexpr (KIND == 0) {
-#pragma unroll
-      for (int j = 0; j < SN; j += 2) {
-        const int64_t n = n0 + (wn * (TN / WN) + 32 * j) / 2 + l32;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int64_t m = m0 + wm * (TM / WM) + 32 * i + out_row(e, lane);
-          if (m < p.M && n < p.N) {
-            const float g = acc[i][j][e], u = acc[i][j + 1][e];
-            put(p.c, m, n, silu(g) * u, p.out_f32);
-            if (p.g.p) {
-              put(p.g, m, n, g, p.out_f32);
-              put(p.u, m, n, u, p.out_f32);
-            }
+            for (int q = 0; q < PIECES; ++q)
+              if (q * ROWS / PIECES == row) {
+                put(q, buf ^ 1);
+                get(q);
+              }
+            if (row == ROWS - 1) advance();
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
       }
+    }
+  }
+
+  const int64_t mw = m0 + wm * (TM / WM), nw = n0 + wn * (WIDTH / WN);   // the wave's corner
+  const int l32 = lane & 31, half = lane >> 5;
+  if (p.split > 1) {
+    FfRows to;
+    to.p = p.part + (int64_t)part * p.M * p.N;
+    to.st = p.N;
+#pragma unroll
+    for (int i = 0; i < SM; ++i)
+#pragma unroll
+      for (int j = 0; j < SN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v[4] = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+          if (mw + 32 * i + l32 < p.M) put4(to, mw + 32 * i + l32, nw + 32 * j + 8 * e + 4 * half, p.N, 1, v);
+        }
+    return;
+  }
+  // A wave's columns of C, of one of the outputs, in rows of 64 bytes through LDS (80, so that eight lanes'
+  // pieces have other banks), so that memory is written 16 bytes a lane.
+  constexpr int LINE = 80;
+  static_assert(THREADS / 64 * 32 * LINE <= 2 * BUFFER, "a place for each wave");
+  __syncthreads();
+  char* mine = smem + wave * (32 * LINE);
+  auto out = [&](const FfRows& r, int64_t rows, int64_t m, int64_t c, auto value) {
+    // value(e): element e of the lane; its row is m + l32, its columns c + out_row(e, lane)
+    if (!r.p) return;
+    const bool pieces = !p.out_f32 && ((uintptr_t)r.p & 15) == 0 && r.st % 8 == 0;
+    if (!pieces) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v[4] = {value(4 * e), value(4 * e + 1), value(4 * e + 2), value(4 * e + 3)};
+        if ((uint64_t)(m + l32) < (uint64_t)rows) put4(r, m + l32, c + 8 * e + 4 * half, p.N, p.out_f32, v);
+      }
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bf16x4 v;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = (__bf16)value(4 * e + q);
+      *reinterpret_cast<bf16x4*>(mine + l32 * LINE + (8 * e + 4 * half) * 2) = v;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int row = 16 * t + (lane >> 2), col = 8 * (lane & 3);
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(mine + row * LINE + col * 2);
+      if ((uint64_t)(m + row) < (uint64_t)rows) {   // (m is below zero where a tile holds the end of one half)
+        __bf16* to = static_cast<__bf16*>(r.p) + (m + row) * r.st + c + col;
+        if (c + col + 8 <= p.N) *reinterpret_cast<bf16x8*>(to) = v;
+        else
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (c + col + q < p.N) to[q] = v[q];
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+#pragma unroll
+  for (int i = 0; i < SM; ++i) {
+    const int64_t m = mw + 32 * i;
+    if constexpr (KIND == 0) {
+#pragma unroll
+      for (int j = 0; j < SN; j += 2) {
+        const int64_t c = nw + 16 * j;
+        out(p.c, p.M, m, c, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; });
+        out(p.g, p.M, m, c, [&](int e) { return acc[i][j][e]; });
+        out(p.u, p.M, m, c, [&](int e) { return acc[i][j + 1][e]; });
+      }
     } else {
+      // of kind 2 a tile's 32 rows may belong to both halves, where these are not multiples of 32 long
 #pragma unroll
       for (int j = 0; j < SN; ++j) {
-        const int64_t n = n0 + wn * (TN / WN) + 32 * j + l32;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int64_t m = m0 + wm * (TM / WM) + 32 * i + out_row(e, lane);
-          if (m < p.M && n < p.N) {
-            if (p.split > 1) p.part[((int64_t)part * p.M + m) * p.N + n] = acc[i][j][e];
-            else put_c<KIND>(p, m, n, acc[i][j][e]);
-          }
+        auto value = [&](int e) { return acc[i][j][e]; };
+        if constexpr (KIND == 1) {
+          out(p.c, p.M, m, nw + 32 * j, value);
+        } else {
+          if (m < p.half) out(p.c, p.rows, m, nw + 32 * j, value);
+          if (m + 32 > p.half) out(p.c2, p.rows, m - p.half, nw + 32 * j, value);
         }
       }
     }
@@ -244,13 +346,29 @@ __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, int til
 }
 
 // C = the sum of the parts, in their order
-template <int KIND>
 __global__ __launch_bounds__(256) void ff_sum_kernel(FfGemm p) {
-  const int64_t n = p.M * p.N, step = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
-    float s = 0.f;
-    for (int k = 0; k < p.split; ++k) s += p.part[k * n + i];
-    put_c<KIND>(p, i / p.N, i % p.N, s);
+  const int64_t per = (p.N + 3) / 4, total = p.M * per, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+    const int64_t m = i / per, n = (i % per) * 4;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < p.split; ++k) {
+      const float* v = p.part + ((int64_t)k * p.M + m) * p.N + n;
+      if (p.N % 4 == 0) {
+        const float4 x = *reinterpret_cast<const float4*>(v);
+        s[0] += x.x;
+        s[1] += x.y;
+        s[2] += x.z;
+        s[3] += x.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n + e < p.N) s[e] += v[e];
+      }
+    }
+    const bool second = p.kind == 2 && m >= p.half;
+    const FfRows& r = second ? p.c2 : p.c;
+    const int64_t row = second ? m - p.half : m;
+    if (r.p && (p.kind != 2 || row < p.rows)) put4(r, row, n, p.N, p.out_f32, s);
   }
 }
 
@@ -298,10 +416,8 @@ hipError_t launch_ff_gemm(const FfGemm& p, hipStream_t st) {
     else r = go<2, 128, 128, 2, 2>(p, st);
   }
   if (r == hipSuccess && p.split > 1) {
-    const int64_t groups = (p.M * p.N + 255) / 256;
-    const dim3 grid((unsigned)(groups < 65536 ? groups : 65536)), block(256);
-    if (p.kind == 1) hipLaunchKernelGGL(ff_sum_kernel<1>, grid, block, 0, st, p);
-    else hipLaunchKernelGGL(ff_sum_kernel<2>, grid, block, 0, st, p);
+    const int64_t groups = (p.M * ((p.N + 3) / 4) + 255) / 256;
+    hipLaunchKernelGGL(ff_sum_kernel, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, st, p);
     r = hipGetLastError();
   }
   return r;
