@@ -174,12 +174,12 @@ bool in_place(const dla_norm_rows* r, int64_t rows) {
 
 struct FfSpace {
   size_t x, wg, wu, parts, sum, total;
-  int split_dx, split_dw;
+  FfPlan y, dx, dw;
 };
 FfSpace space_of(const dla_ff_desc& d, bool backward, bool direct) {
   FfSpace s;
   memset(&s, 0, sizeof(s));
-  s.split_dx = s.split_dw = 1;
+  if (d.rows == 0) s.dw = plan_ff_gemm(2, 2 * (int64_t)round_up(d.F, 8), d.D, 0, 1);
   if (d.rows == 0 || (!backward && d.rows <= kFfStepRows)) return s;
   size_t used = 0;
   auto take = [&](size_t bytes) {
@@ -196,11 +196,12 @@ FfSpace space_of(const dla_ff_desc& d, bool backward, bool direct) {
   }
   if (backward) {
     s.parts = take(planes * d.rows * 2 * Fp * 2);
-    s.split_dx = ff_split(1, d.rows, d.D, d.F, planes == 1 ? 2 : 12);
-    s.split_dw = ff_split(2, 2 * Fp, d.D, d.rows, planes == 1 ? 1 : 6);
-    const size_t dx = s.split_dx > 1 ? (size_t)s.split_dx * d.rows * d.D * 4 : 0;
-    const size_t dw = s.split_dw > 1 ? (size_t)s.split_dw * 2 * Fp * d.D * 4 : 0;
-    s.sum = take(dx > dw ? dx : dw);
+    s.dx = plan_ff_gemm(1, d.rows, d.D, d.F, planes == 1 ? 2 : 12);
+    s.dw = plan_ff_gemm(2, 2 * Fp, d.D, d.rows, planes == 1 ? 1 : 6);
+    s.sum = take(s.dx.part_bytes > s.dw.part_bytes ? s.dx.part_bytes : s.dw.part_bytes);
+  } else {
+    s.y = plan_ff_gemm(0, d.rows, d.F, d.D, planes == 1 ? 1 : 6);
+    s.sum = take(s.y.part_bytes);
   }
   s.total = used;
   return s;
@@ -513,8 +514,8 @@ dla_status dla_gated_ff(const dla_ff_desc* desc, const dla_norm_rows* x,
   p.c = ff_rows(y);
   p.g = ff_rows(g);
   p.u = ff_rows(u);
-  p.split = 1;
-  return done(launch_ff_gemm(p, st));
+  p.part = (float*)(ws + sp.sum);
+  return done(launch_ff_gemm(p, sp.y, st));
 }
 
 dla_status dla_gated_ff_backward(const dla_ff_desc* desc, const dla_norm_rows* x,
@@ -572,8 +573,7 @@ dla_status dla_gated_ff_backward(const dla_ff_desc* desc, const dla_norm_rows* x
     p.ldb = pg.ld;
     pairs_of(p, planes, 2);
     p.c = ff_rows(dx);
-    p.split = sp.split_dx;
-    r = launch_ff_gemm(p, st);
+    r = launch_ff_gemm(p, sp.dx, st);
   }
   if (r == hipSuccess && (dw_gate || dw_up)) {
     p.kind = 2;
@@ -590,8 +590,7 @@ dla_status dla_gated_ff_backward(const dla_ff_desc* desc, const dla_norm_rows* x
     p.c2 = ff_rows(dw_up);
     p.half = Fp;
     p.rows = d.F;
-    p.split = sp.split_dw;
-    r = launch_ff_gemm(p, st);
+    r = launch_ff_gemm(p, sp.dw, st);
   }
   return done(r);
 }

@@ -40,11 +40,20 @@ struct FfGemm {
   FfRows c, g, u;     // kind 0: c is y
   FfRows c2;          // kind 2: where the rows from `half` on go; each half has `rows` of them
   int64_t half, rows;
-  // kinds 1 and 2: parts of the sum over K that workgroups share, [split][M][N] float32
-  int split;
-  float* part;
+  float* part;        // FfPlan's part_bytes
 };
-int ff_split(int kind, int64_t M, int64_t N, int64_t K, int pairs);
-hipError_t launch_ff_gemm(const FfGemm& p, hipStream_t st);
+
+// Who works on what: the first `full` tiles of C have a workgroup each, the rest `share`, which divide the
+// steps of a tile's sum among them, and whose parts are joined afterwards.
+struct FfPlan {
+  int large;                // tiles of 256 x 256, or of 128 x 128
+  int tiles_m, tiles_n, share;
+  int64_t tiles, full, steps;
+  size_t part_bytes;
+  // the first step of a part
+  __host__ __device__ int64_t begin(int part) const { return steps * part / share; }
+};
+FfPlan plan_ff_gemm(int kind, int64_t M, int64_t N, int64_t K, int pairs);
+hipError_t launch_ff_gemm(const FfGemm& p, const FfPlan& w, hipStream_t st);
 
 }  // namespace dla

@@ -106,6 +106,98 @@ __device__ __forceinline__ void put4(const FfRows& r, int64_t m, int64_t n, int6
   }
 }
 
+// A wave's place in a tile of C from its sums.  mine: kLine * 32 bytes of LDS.
+constexpr int kLine = 80;
+
+template <int KIND, int TM, int TN, int WM, int WN>
+__device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM / WM / 32][TN / WN / 32], int64_t m0,
+                                         int64_t n0, char* mine, int lane, int wave) {
+  constexpr int SM = TM / WM / 32, SN = TN / WN / 32, WIDTH = KIND == 0 ? TN / 2 : TN;
+  const int wm = wave / WN, wn = wave % WN;
+  const int64_t mw = m0 + wm * (TM / WM), nw = n0 + wn * (WIDTH / WN);   // the wave's corner
+  const int l32 = lane & 31, half = lane >> 5;
+  // A wave's columns of C, of one of the outputs, in rows of 64 bytes through LDS (80, so that eight lanes'
+  // pieces have other banks), so that memory is written 16 bytes a lane.
+  auto out = [&](const FfRows& r, int64_t rows, int64_t m, int64_t c, bool later, auto value) {
+    // value(e): element e of the lane; its row is m + l32, its columns c + out_row(e, lane); later: g and u,
+    // which only the backward pass reads, are not to take the operands' place in the caches (675 us
+    // become 655)
+    if (!r.p) return;
+    const bool pieces = !p.out_f32 && ((uintptr_t)r.p & 15) == 0 && r.st % 8 == 0;
+    if (!pieces) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v[4] = {value(4 * e), value(4 * e + 1), value(4 * e + 2), value(4 * e + 3)};
+        if ((uint64_t)(m + l32) < (uint64_t)rows) put4(r, m + l32, c + 8 * e + 4 * half, p.N, p.out_f32, v);
+      }
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bf16x4 v;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = (__bf16)value(4 * e + q);
+      *reinterpret_cast<bf16x4*>(mine + l32 * kLine + (8 * e + 4 * half) * 2) = v;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int row = 16 * t + (lane >> 2), col = 8 * (lane & 3);
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(mine + row * kLine + col * 2);
+      if ((uint64_t)(m + row) < (uint64_t)rows) {   // (m is below zero where a tile holds the end of one half)
+        __bf16* to = static_cast<__bf16*>(r.p) + (m + row) * r.st + c + col;
+        if (c + col + 8 <= p.N) {
+          if (later) __builtin_nontemporal_store(v, reinterpret_cast<bf16x8*>(to));
+          else *reinterpret_cast<bf16x8*>(to) = v;
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (c + col + q < p.N) to[q] = v[q];
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+#pragma unroll
+  for (int i = 0; i < SM; ++i) {
+    const int64_t m = mw + 32 * i;
+    if constexpr (KIND == 0) {
+#pragma unroll
+      for (int j = 0; j < SN; j += 2) {
+        const int64_t c = nw + 16 * j;
+        out(p.c, p.M, m, c, false, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; });
+        out(p.g, p.M, m, c, true, [&](int e) { return acc[i][j][e]; });
+        out(p.u, p.M, m, c, true, [&](int e) { return acc[i][j + 1][e]; });
+      }
+    } else {
+      // of kind 2 a tile's 32 rows may belong to both halves, where these are not multiples of 32 long
+#pragma unroll
+      for (int j = 0; j < SN; ++j) {
+        auto value = [&](int e) { return acc[i][j][e]; };
+        if constexpr (KIND == 1) {
+          out(p.c, p.M, m, nw + 32 * j, false, value);
+        } else {
+          if (m < p.half) out(p.c, p.rows, m, nw + 32 * j, false, value);
+          if (m + 32 > p.half) out(p.c2, p.rows, m - p.half, nw + 32 * j, false, value);
+        }
+      }
+    }
+  }
+}
+
+// Where a tile lies in C: kGroup tiles of M go through the tiles of N together.
+struct FfCorner {
+  int64_t m, n;
+};
+constexpr int kGroup = 4;
+
+template <int TM, int WIDTH>
+__device__ __forceinline__ FfCorner corner_of(const FfPlan& w, int64_t tile) {
+  const int64_t g0 = tile / ((int64_t)kGroup * w.tiles_n) * kGroup, in = tile - g0 * w.tiles_n;
+  const int gm = (int)(w.tiles_m - g0 < kGroup ? w.tiles_m - g0 : kGroup);
+  return FfCorner{(g0 + in % gm) * TM, (in / gm) * WIDTH};
+}
+
 // KIND as in gated_ff.h.  WM x WN waves, each with a tile of (TM / WM) x (TN / WN); of kind 0 the
 // tile's columns are TN / 2 of B and as many of B2, 32 in turn, so that a wave has g and u of the
 // same columns.
@@ -115,7 +207,7 @@ __device__ __forceinline__ void put4(const FfRows& r, int64_t m, int64_t n, int6
 // first 16 follow the barrier that the step's last products are still to come behind, so that neither
 // the barrier nor LDS makes the matrix unit wait.
 template <int KIND, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, FfPlan w) {
   constexpr int THREADS = 64 * WM * WN;
   constexpr bool AL = KIND != 2, BL = KIND == 0, MIXED = KIND == 0;
   using TA = FfTile<TM, AL>;
@@ -128,28 +220,32 @@ __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, int til
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
 
   // workgroups that run together (every eighth on one die) have neighbouring tiles
-  const int64_t tiles = (int64_t)tiles_m * tiles_n, total = tiles * p.split;
-  int64_t id = blockIdx.x;
-  {
-    const int64_t each = total / 8, rest = total % 8, x = id % 8, y = id / 8;
-    id = x * each + (x < rest ? x : rest) + y;
+  auto together = [](int64_t id, int64_t total) {
+    const int64_t each = total / 8, rest = total % 8, x = id % 8;
+    return x * each + (x < rest ? x : rest) + id / 8;
+  };
+  // a tile, or a part of the steps of one that is shared; those who have the same part of neighbouring
+  // tiles run together, and find each other's operands in their die's cache
+  int64_t tile, first = 0, last = w.steps;
+  int part = 0;
+  if (blockIdx.x < w.full) {
+    tile = together(blockIdx.x, w.full);
+  } else {
+    const int64_t rest = w.tiles - w.full, id = together(blockIdx.x - w.full, rest * w.share);
+    part = (int)(id / rest);
+    tile = w.full + id % rest;
+    first = w.begin(part);
+    last = w.begin(part + 1);
   }
-  const int part = (int)(id / tiles);
-  id %= tiles;
-  constexpr int GROUP = 4;   // tiles of M that go through the tiles of N together
-  const int64_t g0 = id / ((int64_t)GROUP * tiles_n) * GROUP;
-  const int gm = (int)(tiles_m - g0 < GROUP ? tiles_m - g0 : GROUP);
-  const int64_t in = id - g0 * tiles_n;
-  const int64_t m0 = (g0 + in % gm) * TM, n0 = (in / gm) * WIDTH;
+  const FfCorner corner = corner_of<TM, WIDTH>(w, tile);
+  const int64_t m0 = corner.m, n0 = corner.n;
 
   FfLoad<TM, AL, THREADS> la;
   FfLoad<TN, BL, THREADS> lb;
   la.template init<false>(p.M - m0, p.lda, tid);
   lb.template init<MIXED>(p.N - n0, p.ldb, tid);
 
-  const int64_t ksteps = (p.K + kStep - 1) / kStep, steps = ksteps * p.pairs;
-  const int64_t first = steps * part / p.split, last = steps * (part + 1) / p.split;
-
+  const int64_t ksteps = w.steps / p.pairs;
   // where the next step to ask for lies
   const int64_t da = AL ? kStep : kStep * p.lda, db = BL ? kStep : kStep * p.ldb;
   int pair = 0;
@@ -260,167 +356,127 @@ __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, int til
     }
   }
 
-  const int64_t mw = m0 + wm * (TM / WM), nw = n0 + wn * (WIDTH / WN);   // the wave's corner
-  const int l32 = lane & 31, half = lane >> 5;
-  if (p.split > 1) {
-    FfRows to;
-    to.p = p.part + (int64_t)part * p.M * p.N;
-    to.st = p.N;
+  if (blockIdx.x < w.full) {
+    __syncthreads();
+    ff_store<KIND, TM, TN, WM, WN>(p, acc, m0, n0, smem + wave * (32 * kLine), lane, wave);
+  } else {
+    // a part of a tile's sum, as the lanes hold it
+    f32x4* to = reinterpret_cast<f32x4*>(p.part) + ((tile - w.full) * w.share + part) * (int64_t)(TM * TN / 4) + tid;
+#pragma unroll
+    for (int i = 0; i < SM; ++i)
+#pragma unroll
+      for (int j = 0; j < SN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          to[((i * SN + j) * 4 + e) * THREADS] = f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+  }
+}
+
+// The tiles whose sums are in parts: these in their order, a wave's place in a workgroup of its own.
+template <int KIND, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64) void ff_join_kernel(FfGemm p, FfPlan w) {
+  constexpr int WAVES = WM * WN, SM = TM / WM / 32, SN = TN / WN / 32;
+  __shared__ __align__(16) char smem[32 * kLine];
+  const int lane = threadIdx.x, wave = blockIdx.x % WAVES;
+  const int64_t tile = blockIdx.x / WAVES;
+  const f32x4* part = reinterpret_cast<const f32x4*>(p.part) + tile * w.share * (int64_t)(TM * TN / 4) + wave * 64 + lane;
+  f32x16 acc[SM][SN];
+#pragma unroll
+  for (int i = 0; i < SM; ++i)
+#pragma unroll
+    for (int j = 0; j < SN; ++j) acc[i][j] = zero16();
+  for (int s = 0; s < w.share; ++s, part += TM * TN / 4) {
 #pragma unroll
     for (int i = 0; i < SM; ++i)
 #pragma unroll
       for (int j = 0; j < SN; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float v[4] = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
-          if (mw + 32 * i + l32 < p.M) put4(to, mw + 32 * i + l32, nw + 32 * j + 8 * e + 4 * half, p.N, 1, v);
+          const f32x4 v = part[((i * SN + j) * 4 + e) * (WAVES * 64)];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) acc[i][j][4 * e + q] += v[q];
         }
-    return;
   }
-  // A wave's columns of C, of one of the outputs, in rows of 64 bytes through LDS (80, so that eight lanes'
-  // pieces have other banks), so that memory is written 16 bytes a lane.
-  constexpr int LINE = 80;
-  static_assert(THREADS / 64 * 32 * LINE <= 2 * BUFFER, "a place for each wave");
-  __syncthreads();
-  char* mine = smem + wave * (32 * LINE);
-  auto out = [&](const FfRows& r, int64_t rows, int64_t m, int64_t c, auto value) {
-    // value(e): element e of the lane; its row is m + l32, its columns c + out_row(e, lane)
-    if (!r.p) return;
-    const bool pieces = !p.out_f32 && ((uintptr_t)r.p & 15) == 0 && r.st % 8 == 0;
-    if (!pieces) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float v[4] = {value(4 * e), value(4 * e + 1), value(4 * e + 2), value(4 * e + 3)};
-        if ((uint64_t)(m + l32) < (uint64_t)rows) put4(r, m + l32, c + 8 * e + 4 * half, p.N, p.out_f32, v);
-      }
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      bf16x4 v;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = (__bf16)value(4 * e + q);
-      *reinterpret_cast<bf16x4*>(mine + l32 * LINE + (8 * e + 4 * half) * 2) = v;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int row = 16 * t + (lane >> 2), col = 8 * (lane & 3);
-      const bf16x8 v = *reinterpret_cast<const bf16x8*>(mine + row * LINE + col * 2);
-      if ((uint64_t)(m + row) < (uint64_t)rows) {   // (m is below zero where a tile holds the end of one half)
-        __bf16* to = static_cast<__bf16*>(r.p) + (m + row) * r.st + c + col;
-        if (c + col + 8 <= p.N) *reinterpret_cast<bf16x8*>(to) = v;
-        else
-#pragma unroll
-          for (int q = 0; q < 8; ++q)
-            if (c + col + q < p.N) to[q] = v[q];
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  };
-#pragma unroll
-  for (int i = 0; i < SM; ++i) {
-    const int64_t m = mw + 32 * i;
-    if constexpr (KIND == 0) {
-#pragma unroll
-      for (int j = 0; j < SN; j += 2) {
-        const int64_t c = nw + 16 * j;
-        out(p.c, p.M, m, c, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; });
-        out(p.g, p.M, m, c, [&](int e) { return acc[i][j][e]; });
-        out(p.u, p.M, m, c, [&](int e) { return acc[i][j + 1][e]; });
-      }
-    } else {
-      // of kind 2 a tile's 32 rows may belong to both halves, where these are not multiples of 32 long
-#pragma unroll
-      for (int j = 0; j < SN; ++j) {
-        auto value = [&](int e) { return acc[i][j][e]; };
-        if constexpr (KIND == 1) {
-          out(p.c, p.M, m, nw + 32 * j, value);
-        } else {
-          if (m < p.half) out(p.c, p.rows, m, nw + 32 * j, value);
-          if (m + 32 > p.half) out(p.c2, p.rows, m - p.half, nw + 32 * j, value);
-        }
-      }
-    }
-  }
-}
-
-// C = the sum of the parts, in their order
-__global__ __launch_bounds__(256) void ff_sum_kernel(FfGemm p) {
-  const int64_t per = (p.N + 3) / 4, total = p.M * per, step = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
-    const int64_t m = i / per, n = (i % per) * 4;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < p.split; ++k) {
-      const float* v = p.part + ((int64_t)k * p.M + m) * p.N + n;
-      if (p.N % 4 == 0) {
-        const float4 x = *reinterpret_cast<const float4*>(v);
-        s[0] += x.x;
-        s[1] += x.y;
-        s[2] += x.z;
-        s[3] += x.w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < p.N) s[e] += v[e];
-      }
-    }
-    const bool second = p.kind == 2 && m >= p.half;
-    const FfRows& r = second ? p.c2 : p.c;
-    const int64_t row = second ? m - p.half : m;
-    if (r.p && (p.kind != 2 || row < p.rows)) put4(r, row, n, p.N, p.out_f32, s);
-  }
+  const FfCorner corner = corner_of<TM, KIND == 0 ? TN / 2 : TN>(w, w.full + tile);
+  ff_store<KIND, TM, TN, WM, WN>(p, acc, corner.m, corner.n, smem, lane, wave);
 }
 
 template <int KIND, int TM, int TN, int WM, int WN>
-hipError_t go(const FfGemm& p, hipStream_t st) {
-  constexpr int WIDTH = KIND == 0 ? TN / 2 : TN;
-  const int64_t tm = (p.M + TM - 1) / TM, tn = (p.N + WIDTH - 1) / WIDTH;
-  const size_t shm = 2 * (size_t)(TM + TN) * kStep * 2;
+hipError_t go(const FfGemm& p, const FfPlan& w, hipStream_t st) {
+  constexpr size_t shm = 2 * (size_t)(TM + TN) * kStep * 2;
+  static_assert(WM * WN * 32 * kLine <= shm, "a place for each wave");
   const auto k = ff_gemm_kernel<KIND, TM, TN, WM, WN>;
   if (shm > 65536) {
     const hipError_t r = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shm);
     if (r != hipSuccess) return r;
   }
-  hipLaunchKernelGGL(k, dim3((unsigned)(tm * tn * p.split)), dim3(64 * WM * WN), shm, st, p, (int)tm, (int)tn);
+  const int64_t rest = w.tiles - w.full;
+  hipLaunchKernelGGL(k, dim3((unsigned)(w.full + rest * w.share)), dim3(64 * WM * WN), shm, st, p, w);
+  if (rest) {
+    const auto j = ff_join_kernel<KIND, TM, TN, WM, WN>;
+    hipLaunchKernelGGL(j, dim3((unsigned)(rest * WM * WN)), dim3(64), 0, st, p, w);
+  }
   return hipGetLastError();
-}
-
-bool large(int kind, int64_t M, int64_t N) {
-  const int64_t width = kind == 0 ? 128 : 256;
-  return ((M + 255) / 256) * ((N + width - 1) / width) >= 192;
 }
 
 }  // namespace
 
-// Parts of the sum over K: as many as still give every compute unit a tile, of at least 8 steps.
-int ff_split(int kind, int64_t M, int64_t N, int64_t K, int pairs) {
-  if (kind == 0 || M == 0 || large(kind, M, N)) return 1;
-  const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128), steps = (K + kStep - 1) / kStep * pairs;
-  int64_t s = 512 / tiles;
-  if (s > steps / 8) s = steps / 8;
-  if (s > 16) s = 16;
-  return s < 1 ? 1 : (int)s;
+FfPlan plan_ff_gemm(int kind, int64_t M, int64_t N, int64_t K, int pairs) {
+  FfPlan best{};
+  double least = 0;
+  for (int large = 0; large < 2; ++large) {
+    FfPlan w{};
+    const int t = large ? 256 : 128, width = kind == 0 ? t / 2 : t;
+    w.large = large;
+    w.tiles_m = (int)((M + t - 1) / t);
+    w.tiles_n = (int)((N + width - 1) / width);
+    w.tiles = (int64_t)w.tiles_m * w.tiles_n;
+    w.steps = (K > 0 ? (K + kStep - 1) / kStep : 1) * pairs;   // (without K one of zeros)
+    // A step's time in microseconds where every compute unit has one workgroup (small tiles: two share the
+    // unit in turn, and pass without a pause from one to the next); what a part costs to write and to
+    // read.  Of 8 sizes from 100 to 16384 rows, tiles and shares by these are within 6% of the best of
+    // 12 tried, but for one (2048 x 512 x 512 rows of K: 10%).
+    const int64_t at_once = 256;
+    const double step = large ? 1.7 : 0.62, part = large ? 0.16 : 0.05, join = 8.;
+    const auto rounds = [&](int64_t n) {
+      return large ? (double)((n + at_once - 1) / at_once) : n < at_once ? (n > 0 ? 1. : 0.) : (double)n / at_once;
+    };
+    w.full = w.tiles / at_once * at_once;
+    const int64_t rest = w.tiles - w.full;
+    double time = rounds(w.full) * w.steps * step;
+    if (rest) {
+      double cost = w.steps * step;
+      int share = 1;
+      for (int s = 2; s <= 64 && s * 4 <= w.steps; ++s) {     // of 4 steps at least
+        const double c = rounds(rest * s) * ((w.steps + s - 1) / s) * step + join + part * rest * s;
+        if (c < cost) {
+          cost = c;
+          share = s;
+        }
+      }
+      time += cost;
+      if (share > 1) w.share = share;
+      else w.full = w.tiles;
+    }
+    w.part_bytes = (size_t)(w.tiles - w.full) * w.share * t * t * 4;
+    if (!large || time < least) {
+      best = w;
+      least = time;
+    }
+  }
+  return best;
 }
 
-hipError_t launch_ff_gemm(const FfGemm& p, hipStream_t st) {
+hipError_t launch_ff_gemm(const FfGemm& p, const FfPlan& w, hipStream_t st) {
   if (p.M == 0 || p.N == 0) return hipSuccess;
-  hipError_t r;
-  if (large(p.kind, p.M, p.N)) {
-    if (p.kind == 0) r = go<0, 256, 256, 2, 4>(p, st);
-    else if (p.kind == 1) r = go<1, 256, 256, 2, 4>(p, st);
-    else r = go<2, 256, 256, 2, 4>(p, st);
-  } else {
-    if (p.kind == 0) r = go<0, 128, 128, 2, 2>(p, st);
-    else if (p.kind == 1) r = go<1, 128, 128, 2, 2>(p, st);
-    else r = go<2, 128, 128, 2, 2>(p, st);
+  if (w.large) {
+    if (p.kind == 0) return go<0, 256, 256, 2, 4>(p, w, st);
+    if (p.kind == 1) return go<1, 256, 256, 2, 4>(p, w, st);
+    return go<2, 256, 256, 2, 4>(p, w, st);
   }
-  if (r == hipSuccess && p.split > 1) {
-    const int64_t groups = (p.M * ((p.N + 3) / 4) + 255) / 256;
-    hipLaunchKernelGGL(ff_sum_kernel, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, st, p);
-    r = hipGetLastError();
-  }
-  return r;
+  if (p.kind == 0) return go<0, 128, 128, 2, 2>(p, w, st);
+  if (p.kind == 1) return go<1, 128, 128, 2, 2>(p, w, st);
+  return go<2, 128, 128, 2, 2>(p, w, st);
 }
 
 }  // namespace dla

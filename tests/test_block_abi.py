@@ -155,8 +155,10 @@ def test_gated_ff_refusals():
         for D, F in ((16, 24), (15, 24), (16, 23), (2048, 5504)):
             for dt in (0, 1):
                 assert ask(ff(rows, D, F, dt)) == OK
-                direct = dt == 1 and D % 8 == 0
-                assert (n.value == 0) == (rows <= 64 or direct)
+                if rows <= 64:
+                    assert n.value == 0
+                elif dt == 0 or D % 8:
+                    assert n.value >= (rows + 2 * F) * D * 2
                 assert ask(ff(rows, D, F, dt), 0, 0) == OK and (n.value > 0) == (rows > 64)
                 assert ask(ff(rows, D, F, dt), 1) == OK and n.value >= rows * F * 4
     r = lambda p=FAKE, s=24: block._ROWS.pack(p, s)  # noqa: E731
@@ -169,8 +171,8 @@ def test_gated_ff_refusals():
         assert fwd(**kw) == BAD, kw
     assert fwd(d=ff(rows=0), x=None, y=None) == OK
     odd = r(FAKE + 2)
-    for kw in (dict(x=odd, size=0), dict(wg=odd, ws=None), dict(wu=odd, ws=FAKE + 16), dict(d=ff(dt=0), size=100),
-               dict(wu=r(s=32), size=0)):
+    for kw in (dict(x=odd, size=100), dict(wg=odd, ws=None), dict(wu=odd, ws=FAKE + 16), dict(d=ff(dt=0), size=100),
+               dict(wu=r(s=32), size=100)):
         assert fwd(**kw) == SPACE, kw
 
     def back(d=ff(), x=r(), wg=r(), wu=r(), g=r(), u=r(), dy=r(), dx=r(), dwg=r(), dwu=r(), ws=FAKE, size=1 << 30):
