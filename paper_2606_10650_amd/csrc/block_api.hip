@@ -144,6 +144,28 @@ dla_status check(const dla_logprobs_desc* d) {
   return DLA_OK;
 }
 
+struct LogprobSpace {
+  size_t keys, total;
+};
+LogprobSpace space_of(const LogprobArgs& a) {
+  LogprobSpace s{0, 0};
+  if (a.parts <= 1 || a.rows == 0) return s;
+  s.keys = round_up((size_t)a.rows * a.parts * 12, 256);
+  s.total = s.keys + (size_t)a.rows * a.parts * a.top * 8;
+  return s;
+}
+
+LogprobArgs logprob_args(const dla_logprobs_desc& d) {
+  LogprobArgs a;
+  memset(&a, 0, sizeof(a));
+  a.rows = d.rows;
+  a.V = d.V;
+  a.top = d.top;
+  a.bf16 = d.dtype == DLA_BF16;
+  plan_logprobs(a, d.dtype);
+  return a;
+}
+
 // ---------------------------------------------------------------------------
 // feed-forward
 // ---------------------------------------------------------------------------
@@ -389,7 +411,7 @@ dla_status dla_token_logprobs_workspace_size(const dla_logprobs_desc* desc, size
   const dla_status s = check(desc);
   if (s != DLA_OK) return remember(s);
   if (!bytes) return remember(DLA_ERR_INVALID_ARG);
-  *bytes = 0;
+  *bytes = space_of(logprob_args(*desc)).total;
   return remember(DLA_OK);
 }
 
@@ -406,11 +428,11 @@ dla_status dla_token_logprobs(const dla_logprobs_desc* desc, const dla_norm_rows
   if (!rows_ok(logits, d.rows, d.V, size_of(d.dtype), false) || (logprob && !tokens) ||
       (d.top && (!top_ids || !top_logprobs)))
     return remember(DLA_ERR_INVALID_ARG);
-  LogprobArgs a;
-  memset(&a, 0, sizeof(a));
-  a.rows = d.rows;
-  a.V = d.V;
-  a.top = d.top;
+  LogprobArgs a = logprob_args(d);
+  const LogprobSpace sp = space_of(a);
+  if (!workspace_ok(workspace, workspace_bytes, sp.total)) return remember(DLA_ERR_WORKSPACE);
+  a.part_sums = (float*)workspace;
+  a.part_keys = (uint64_t*)((char*)workspace + sp.keys);
   a.l = logits->data;
   a.st = logits->stride;
   a.tokens = tokens;
