@@ -381,12 +381,6 @@ dla_status dla_gated_norm_backward(const dla_gated_norm_desc* desc, const dla_gr
         (dgate && !rows_ok(dgate, d, true)) || (dresidual && !rows_ok(dresidual, d, true)))
       return remember(DLA_ERR_INVALID_ARG);
     if (!rstd || (dy && !y_rstd)) return remember(DLA_ERR_INVALID_ARG);
-    const NormSpace sp = space_of(a);
-    if (dweight || dnext_weight) {
-      if (!workspace_ok(workspace, workspace_bytes, sp.total)) return remember(DLA_ERR_WORKSPACE);
-      a.dw_part = dweight ? (float*)workspace : nullptr;
-      a.dw2_part = dnext_weight ? (float*)((char*)workspace + sp.dw2) : nullptr;
-    }
     a.w = weight;
     a.w2 = next_weight;
     a.x = rows_of(x);
@@ -399,6 +393,13 @@ dla_status dla_gated_norm_backward(const dla_gated_norm_desc* desc, const dla_gr
     a.dx = rows_of(dx);
     a.dgate = rows_of(dgate);
     a.dres = rows_of(dresidual);
+    plan_gated_norm(a, d.dtype, true);
+    const NormSpace sp = space_of(a);
+    if (dweight || dnext_weight) {
+      if (!workspace_ok(workspace, workspace_bytes, sp.total)) return remember(DLA_ERR_WORKSPACE);
+      a.dw_part = dweight ? (float*)workspace : nullptr;
+      a.dw2_part = dnext_weight ? (float*)((char*)workspace + sp.dw2) : nullptr;
+    }
   }
   hipStream_t st = (hipStream_t)stream;
   hipError_t r = hipSuccess;

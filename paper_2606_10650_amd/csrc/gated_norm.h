@@ -26,7 +26,8 @@ struct GatedNormArgs {
   int64_t groups;
 };
 
-// Fills the last lines of the arguments; whether the size is one that kernels are for.
+// Fills the last lines of the arguments.  Of the backward pass with gate and next norm these are no larger than
+// without.
 void plan_gated_norm(GatedNormArgs& a, int dtype, bool backward);
 // Parts of dw and of dw2 of a backward pass, in floats.
 int64_t gated_norm_dw_parts(const GatedNormArgs& a);

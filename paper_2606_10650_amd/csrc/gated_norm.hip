@@ -28,9 +28,10 @@ __device__ __forceinline__ float over_group(float x, float* lds) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
-    x = lds[0];
+    const float* mine = lds + threadIdx.x / NT * (NT / 64);
+    x = mine[0];
 #pragma unroll
-    for (int i = 1; i < NT / 64; ++i) x += lds[i];
+    for (int i = 1; i < NT / 64; ++i) x += mine[i];
   }
   return x;
 }
@@ -46,10 +47,10 @@ __device__ __forceinline__ float rstd_of(const float (&v)[NP][N], int D, float e
   sum = over_group<NT>(sum, lds);
   float ms = sum / (float)D + eps, rstd = 1.f / sqrtf(ms);
   const bool out = !(ms >= 0x1p-100f && ms <= 0x1.fffffep127f);
-  // Squares that leave float32's range (in all threads of the group or in none; where a wave
-  // holds several groups all of them take part): once more with the values scaled by a power of
+  // Squares that leave float32's range (in all threads of the group or in none; where a wave or a
+  // workgroup holds several groups all of them take part): once more with the values scaled by a power of
   // two.  An infinity or NaN stays one.
-  if (NT < 64 ? __any(out) : out) {
+  if (NT < 64 ? __any(out) : NT == 128 ? __syncthreads_or(out) : out) {
     const float f = ms < 1.f ? 0x1p100f : 0x1p-80f;
     sum = 0.f;
 #pragma unroll
@@ -92,7 +93,7 @@ template <typename T, int NT, int NP>
 __global__ __launch_bounds__(NT > 256 ? NT : 256) void gated_norm_kernel(GatedNormArgs a) {
   constexpr int N = Piece<T>::N;
   using Raw = typename Piece<T>::Raw;
-  __shared__ float lds[NT > 64 ? NT / 64 : 1];
+  __shared__ float lds[(NT > 256 ? NT : 256) / 64];
   const Place<NT> p(a);
   const int tid = threadIdx.x % NT;
   // all lanes of a wave go round together: those without a row or group hold zeros
@@ -160,11 +161,18 @@ __device__ __forceinline__ void gather(float (&s)[N], int sub, int stride, int s
   }
 }
 
-template <typename T, int NT, int NP>
-__global__ __launch_bounds__(NT > 256 ? NT : 256) void gated_norm_backward_kernel(GatedNormArgs a) {
+// Waves a SIMD of the backward pass.  With gate and next norm a thread of 8 values needs more than a fourth of the
+// registers (65536 x 2048 bfloat16: within a fourth 683 us, within a third 4TIME).
+template <typename T>
+__host__ __device__ constexpr int waves_of(int nt, bool both) {
+  return sizeof(T) == 2 && both && nt <= 256 ? 3 : 4;
+}
+
+template <typename T, int NT, int NP, bool GATE, bool NEXT>
+__global__ __launch_bounds__(NT > 256 ? NT : 256, waves_of<T>(NT, GATE && NEXT)) void gated_norm_backward_kernel(GatedNormArgs a) {
   constexpr int N = Piece<T>::N, PER = Place<NT>::PER;
   using Raw = typename Piece<T>::Raw;
-  __shared__ float lds[NT > 64 ? NT / 64 : 1];
+  __shared__ float lds[(NT > 256 ? NT : 256) / 64];
   __shared__ float sums[PER > 1 ? PER * NT * N : 1];
   const Place<NT> p(a);
   const int tid = threadIdx.x % NT, side = a.G < PER ? a.G : PER, along = PER / side;
@@ -185,12 +193,12 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void gated_norm_backward_kerne
     for (int i = 0; i < NP; ++i) {
       const int c = (i * NT + tid) * N, n = any && a.D > c ? a.D - c : 0;
       x[i] = Piece<T>::raw(at<T>(a.x, row, p.g) + c, n);
-      z[i] = Piece<T>::raw(at<T>(a.gate, row, p.g) + c, a.gate.p ? n : 0);
+      z[i] = Piece<T>::raw(at<T>(a.gate, row, p.g) + c, GATE ? n : 0);
       const Raw q = Piece<T>::raw(at<T>(a.h, row, p.g) + c, a.h.p ? n : 0);
 #pragma unroll
       for (int j = 0; j < N; ++j) dh[i][j] = Piece<T>::value(q, j);
     }
-    if (a.w2 && a.y.p) {
+    if constexpr (NEXT) {
       // through the next norm: dh += r' (dy w' - n' mean(dy w' n'))
       r2 = any ? a.rstd2[row] : 0.f;
       float h[NP][N];
@@ -205,7 +213,7 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void gated_norm_backward_kerne
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           float b = Piece<T>::value(x[i], j) * r * w[j];
-          if (a.gate.p) {
+          if constexpr (GATE) {
             const float zj = Piece<T>::value(z[i], j);
             b *= zj * sigmoid(zj);
           }
@@ -236,7 +244,7 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void gated_norm_backward_kerne
       for (int j = 0; j < N; ++j) {
         const float nx = Piece<T>::value(x[i], j) * r;
         float db = a.scale * dh[i][j];
-        if (a.gate.p) {
+        if constexpr (GATE) {
           const float zj = Piece<T>::value(z[i], j), s = sigmoid(zj);
           dz[j] = db * nx * w[j] * (s * (1.f + zj * (1.f - s)));
           db *= zj * s;
@@ -245,7 +253,7 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void gated_norm_backward_kerne
         dh[i][j] = db * w[j];     // the gradient of n
         sum += dh[i][j] * nx;
       }
-      if (n > 0 && a.gate.p && a.dgate.p) Piece<T>::store(out<T>(a.dgate, row, p.g) + c, n, dz);
+      if (GATE && n > 0 && a.dgate.p) Piece<T>::store(out<T>(a.dgate, row, p.g) + c, n, dz);
     }
     const float mean = over_group<NT>(sum, lds) / (float)a.D;
 #pragma unroll
@@ -273,7 +281,7 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void gated_norm_backward_kerne
           if (p.sub == 0 && c + j < a.D) a.dw_part[(int64_t)blockIdx.x * a.D + c + j] = dw[i][j];
       }
     }
-    if (a.dw2_part) {
+    if (NEXT && a.dw2_part) {
       gather<NT, N, PER>(dw2[i], p.sub, 1, side * along, sums);
 #pragma unroll
       for (int j = 0; j < N; ++j)
@@ -308,56 +316,91 @@ __global__ __launch_bounds__(1024) void part_sum_kernel(const float* part, int64
 }
 
 template <typename T, int NT, int NP>
-hipError_t go(const GatedNormArgs& a, bool backward, hipStream_t st) {
+hipError_t forward(const GatedNormArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.groups * a.gcols)), block(NT > 256 ? NT : 256);
-  if (backward) hipLaunchKernelGGL((gated_norm_backward_kernel<T, NT, NP>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((gated_norm_kernel<T, NT, NP>), grid, block, 0, st, a);
+  hipLaunchKernelGGL((gated_norm_kernel<T, NT, NP>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
-// Threads that share a group of so many pieces: as few lanes as hold it, one piece each, up to a
-// wave with 4 pieces a lane where there are groups enough to fill the chip; else 256, or 1024.
-int threads_of(int64_t total, int pieces) {
+template <typename T, int NT, int NP>
+hipError_t backward(const GatedNormArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)(a.groups * a.gcols)), block(NT > 256 ? NT : 256);
+  if (a.w2 && a.y.p) {
+    if (a.gate.p) hipLaunchKernelGGL((gated_norm_backward_kernel<T, NT, NP, true, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((gated_norm_backward_kernel<T, NT, NP, false, true>), grid, block, 0, st, a);
+  } else {
+    if (a.gate.p) hipLaunchKernelGGL((gated_norm_backward_kernel<T, NT, NP, true, false>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((gated_norm_backward_kernel<T, NT, NP, false, false>), grid, block, 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+// Threads that share a group of so many pieces.  As few lanes as hold it with one piece each, up to a wave.
+// Past that the forward pass goes by waves of up to 4 pieces a lane where there are groups enough to
+// fill the chip, else by 256 threads, or 1024; the backward pass, with seven rows' pieces at hand, by one
+// piece a thread (16384 x 2048 bfloat16 with a next norm: by waves 230 us).
+int threads_of(int64_t total, int pieces, bool back) {
   if (pieces <= 64) {
     int nt = 8;
     while (nt < pieces) nt *= 2;
     return nt;
   }
+  if (back) return pieces <= 128 ? 128 : pieces <= 256 ? 256 : pieces <= 512 ? 512 : 1024;
   if (pieces <= 256 && total >= 1024) return 64;
   return pieces <= 1024 ? 256 : 1024;
 }
 
 template <typename T>
-hipError_t pick(const GatedNormArgs& a, bool backward, hipStream_t st) {
-  const int pieces = (a.D + Piece<T>::N - 1) / Piece<T>::N;
-  switch (threads_of(a.rows * a.G, pieces)) {
-    case 8: return go<T, 8, 1>(a, backward, st);
-    case 16: return go<T, 16, 1>(a, backward, st);
-    case 32: return go<T, 32, 1>(a, backward, st);
+hipError_t pick(const GatedNormArgs& a, bool back, hipStream_t st) {
+  const int pieces = (a.D + Piece<T>::N - 1) / Piece<T>::N, nt = threads_of(a.rows * a.G, pieces, back);
+  if (back) {
+    switch (nt) {
+      case 8: return backward<T, 8, 1>(a, st);
+      case 16: return backward<T, 16, 1>(a, st);
+      case 32: return backward<T, 32, 1>(a, st);
+      case 64: return backward<T, 64, 1>(a, st);
+      case 128: return backward<T, 128, 1>(a, st);
+      case 256: return backward<T, 256, 1>(a, st);
+      case 512: return backward<T, 512, 1>(a, st);
+      default:
+        if (pieces <= 1024) return backward<T, 1024, 1>(a, st);
+        if (pieces <= 2048) return backward<T, 1024, 2>(a, st);
+        return backward<T, 1024, 4>(a, st);
+    }
+  }
+  switch (nt) {
+    case 8: return forward<T, 8, 1>(a, st);
+    case 16: return forward<T, 16, 1>(a, st);
+    case 32: return forward<T, 32, 1>(a, st);
     case 64:
-      if (pieces <= 64) return go<T, 64, 1>(a, backward, st);
-      if (pieces <= 128) return go<T, 64, 2>(a, backward, st);
-      return go<T, 64, 4>(a, backward, st);
+      if (pieces <= 64) return forward<T, 64, 1>(a, st);
+      if (pieces <= 128) return forward<T, 64, 2>(a, st);
+      return forward<T, 64, 4>(a, st);
     case 256:
-      if (pieces <= 256) return go<T, 256, 1>(a, backward, st);
-      if (pieces <= 512) return go<T, 256, 2>(a, backward, st);
-      return go<T, 256, 4>(a, backward, st);
+      if (pieces <= 256) return forward<T, 256, 1>(a, st);
+      if (pieces <= 512) return forward<T, 256, 2>(a, st);
+      return forward<T, 256, 4>(a, st);
     default:
-      if (pieces <= 2048) return go<T, 1024, 2>(a, backward, st);
-      return go<T, 1024, 4>(a, backward, st);
+      if (pieces <= 2048) return forward<T, 1024, 2>(a, st);
+      return forward<T, 1024, 4>(a, st);
   }
 }
 
 }  // namespace
 
 void plan_gated_norm(GatedNormArgs& a, int dtype, bool backward) {
-  const int N = dtype == DLA_BF16 ? 8 : 4, pieces = (a.D + N - 1) / N, nt = threads_of(a.rows * a.G, pieces);
+  const int N = dtype == DLA_BF16 ? 8 : 4, pieces = (a.D + N - 1) / N, nt = threads_of(a.rows * a.G, pieces, backward);
   const int per = nt > 256 ? 1 : 256 / nt, side = a.G < per ? a.G : per, along = per / side;
   a.gcols = (a.G + per - 1) / per;
   a.groups = (a.rows + along - 1) / along;
-  // the forward pass: a workgroup for every row, up to what a launch takes; the backward pass: four
-  // workgroups a compute unit, so that few parts of dw are left
-  const int64_t most = (backward ? 1024 : (int64_t)1 << 21) / a.gcols + 1;
+  // The forward pass: a workgroup for every row, up to what a launch takes.  The backward pass, which leaves a
+  // part of dw a workgroup: as many as are there at once, and not one more.
+  // (8192 forward, which go on to other rows: 65536 x 16 heads of 128 bfloat16 174 us, one row each 215, 2048
+  // workgroups 200)
+  const bool both = a.gate.p && a.w2 && a.y.p;
+  const int waves = dtype == DLA_BF16 ? waves_of<bf16_t>(nt, both) : waves_of<float>(nt, both);
+  const int64_t slots = !backward ? 8192 : waves * 256 / (nt > 256 ? nt / 256 : 1);
+  const int64_t most = slots / a.gcols > 0 ? slots / a.gcols : 1;
   if (a.groups > most) a.groups = most;
 }
 
