@@ -54,6 +54,11 @@ def lib():
     return L
 
 
+def _call(call, device, *args):
+    lib()
+    _run(call, device, *args)
+
+
 def _bytes(call, *args):
     n = ctypes.c_size_t(0)
     _check(getattr(lib(), call)(*args, ctypes.byref(n)), call)
@@ -62,10 +67,12 @@ def _bytes(call, *args):
 
 def _work(workspace, need, device):
     """A workspace and its size, where one is needed."""
-    if not need:
-        return None, 0
-    workspace, size = _space(workspace, need, device)
-    return workspace, size
+    return _space(workspace, need, device) if need else (None, 0)
+
+
+def _new(t):
+    """A contiguous tensor like t."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _last(t, name):
@@ -122,15 +129,19 @@ def short_conv(x, weight, bias=None, *, activation: Optional[str] = "silu", stat
     the call, or None; lengths int32 [B]; starts [B, T], bool or uint8, where documents start.  state_out
     may be state.  Returns (out, state_out); out is contiguous unless given."""
     desc = _conv_desc(x, weight, bias, activation, state, lengths, starts)
+    B, T, C = x.shape
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    shape = (x.shape[0], weight.shape[1] - 1, x.shape[2])
+        out = _new(x)
+        rows = _CONV_ROWS.pack(out.data_ptr(), T * C, C)
+    else:
+        rows = _conv_rows(out, x, "out")
     if state_out is not None:
-        _like(state_out, shape, x.dtype, x.device, "state_out", True)
+        if state_out is not state:
+            _like(state_out, (B, weight.shape[1] - 1, C), x.dtype, x.device, "state_out", True)
     elif want_state:
-        state_out = torch.empty(shape, dtype=x.dtype, device=x.device)
-    _run2("dla_short_conv", x.device, desc, _conv_rows(x, x, "x"), weight.data_ptr(), _ptr(bias), _ptr(state),
-          _conv_rows(out, x, "out"), _ptr(state_out))
+        state_out = x.new_empty((B, weight.shape[1] - 1, C))
+    _call("dla_short_conv", x.device, desc, _conv_rows(x, x, "x"), weight.data_ptr(), _ptr(bias), _ptr(state), rows,
+          _ptr(state_out))
     return out, state_out
 
 
@@ -149,22 +160,16 @@ def short_conv_backward(x, weight, dout, bias=None, *, activation: Optional[str]
     desc = _conv_desc(x, weight, bias, activation, state, lengths, starts)
     (B, T, C), W, dev, f32 = x.shape, weight.shape[1], x.device, torch.float32
     _like(dstate, (B, W - 1, C), x.dtype, dev, "dstate", True)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    dw = torch.empty((C, W), dtype=f32, device=dev)
-    db = None if bias is None else torch.empty((C,), dtype=f32, device=dev)
+    dx, dw = _new(x), x.new_empty((C, W), dtype=f32)
+    db = None if bias is None else x.new_empty((C,), dtype=f32)
     ds = None
     if state is not None if want_dstate is None else want_dstate:
-        ds = torch.empty((B, W - 1, C), dtype=x.dtype, device=dev)
+        ds = x.new_empty((B, W - 1, C))
     workspace, size = _work(workspace, short_conv_workspace_bytes(B, T, C, W, x.dtype), dev)
-    _run2("dla_short_conv_backward", dev, desc, _conv_rows(x, x, "x"), weight.data_ptr(), _ptr(bias), _ptr(state),
-          _conv_rows(dout, x, "dout"), _ptr(dstate), _conv_rows(dx, x, "dx"), dw.data_ptr(), _ptr(db), _ptr(ds),
+    _call("dla_short_conv_backward", dev, desc, _conv_rows(x, x, "x"), weight.data_ptr(), _ptr(bias), _ptr(state),
+          _conv_rows(dout, x, "dout"), _ptr(dstate), _CONV_ROWS.pack(dx.data_ptr(), T * C, C), dw.data_ptr(), _ptr(db), _ptr(ds),
           _ptr(workspace), size)
     return dx, dw, db, ds
-
-
-def _run2(call, device, *args):
-    lib()
-    _run(call, device, *args)
 
 
 # ---------------------------------------------------------------------------
@@ -199,14 +204,16 @@ def gated_norm(x, weight, gate=None, residual=None, *, scale: float = 1.0, next_
     norm then unless G is 1); weight [D] or [G, D], next_weight [D].  Without gate b = n, without residual it is
     zero, without next_weight y is None.  Returns (h, y, rstd [N, G], y_rstd [N] or None)."""
     desc = _gated_desc(x, weight, next_weight, eps, scale)
-    dev, N = x.device, x.shape[0]
-    h = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    y = torch.empty(x.shape, dtype=x.dtype, device=dev) if next_weight is not None else None
-    rstd = torch.empty((N, x.shape[1] if x.dim() == 3 else 1), dtype=torch.float32, device=dev)
-    y_rstd = torch.empty((N,), dtype=torch.float32, device=dev) if next_weight is not None else None
-    _run2("dla_gated_norm", dev, desc, _group_rows(x, x, "x"), _group_rows(gate, x, "gate"),
-          _group_rows(residual, x, "residual"), weight.data_ptr(), _ptr(next_weight), _group_rows(h, x, "h"),
-          _group_rows(y, x, "y"), rstd.data_ptr(), _ptr(y_rstd))
+    shape = x.shape
+    N, D = shape[0], shape[-1]
+    G = shape[1] if len(shape) == 3 else 1
+    new = lambda t: _GROUP_ROWS.pack(t.data_ptr(), G * D, D)  # noqa: E731
+    h, rstd, y, y_rstd = _new(x), x.new_empty((N, G), dtype=torch.float32), None, None
+    if next_weight is not None:
+        y, y_rstd = _new(x), x.new_empty((N,), dtype=torch.float32)
+    _call("dla_gated_norm", x.device, desc, _group_rows(x, x, "x"), _group_rows(gate, x, "gate"),
+          _group_rows(residual, x, "residual"), weight.data_ptr(), _ptr(next_weight), new(h),
+          None if y is None else new(y), rstd.data_ptr(), _ptr(y_rstd))
     return h, y, rstd, y_rstd
 
 
@@ -232,16 +239,16 @@ def gated_norm_backward(dh, x, weight, rstd, gate=None, residual=None, *, scale:
         raise ValueError("dy needs y_rstd")
     if next_weight is None and dy is not None:
         raise ValueError("dy needs next_weight")
-    empty = lambda: torch.empty(x.shape, dtype=x.dtype, device=dev)  # noqa: E731
-    dx, dgate, dres = empty(), None if gate is None else empty(), empty() if through else dh
-    dw = torch.empty(weight.shape, dtype=f32, device=dev)
-    dw2 = None if next_weight is None else torch.empty(next_weight.shape, dtype=f32, device=dev)
-    G = x.shape[1] if x.dim() == 3 else 1
-    workspace, size = _work(workspace, gated_norm_workspace_bytes(N, G, x.shape[-1], x.dtype), dev)
-    _run2("dla_gated_norm_backward", dev, desc, _group_rows(x, x, "x"), _group_rows(gate, x, "gate"),
+    G, D = x.shape[1] if x.dim() == 3 else 1, x.shape[-1]
+    dx, dgate, dres = _new(x), None if gate is None else _new(x), _new(x) if through else dh
+    dw = x.new_empty(weight.shape, dtype=f32)
+    dw2 = None if next_weight is None else x.new_empty(next_weight.shape, dtype=f32)
+    new = lambda t: None if t is None else _GROUP_ROWS.pack(t.data_ptr(), G * D, D)  # noqa: E731
+    workspace, size = _work(workspace, gated_norm_workspace_bytes(N, G, D, x.dtype), dev)
+    _call("dla_gated_norm_backward", dev, desc, _group_rows(x, x, "x"), _group_rows(gate, x, "gate"),
           _group_rows(residual, x, "residual"), weight.data_ptr(), _ptr(next_weight), rstd.data_ptr(), _ptr(y_rstd),
-          _group_rows(dh, x, "dh"), _group_rows(dy, x, "dy"), _group_rows(dx, x, "dx"), _group_rows(dgate, x, "dgate"),
-          _group_rows(dres, x, "dresidual") if through else None, dw.data_ptr(), _ptr(dw2), _ptr(workspace), size)
+          _group_rows(dh, x, "dh"), _group_rows(dy, x, "dy"), new(dx), new(dgate), new(dres) if through else None,
+          dw.data_ptr(), _ptr(dw2), _ptr(workspace), size)
     return dx, dgate, dres, dw, dw2
 
 
@@ -267,11 +274,11 @@ def token_logprobs(logits, tokens=None, *, top: int = 0, entropy: bool = False, 
     lse [N], entropy [N] or None, ids int64 [N, top] or None, logprobs [N, top] or None), all but ids float32; logprob
     is None without tokens."""
     desc, dev, N = _logits(logits, tokens, top), logits.device, logits.shape[0]
-    f = lambda *s: torch.empty(s, dtype=torch.float32, device=dev)  # noqa: E731
+    f = lambda *s: logits.new_empty(s, dtype=torch.float32)  # noqa: E731
     lp, lse, ent = None if tokens is None else f(N), f(N), f(N) if entropy else None
-    ids, tops = (torch.empty((N, top), dtype=torch.int64, device=dev), f(N, top)) if top else (None, None)
+    ids, tops = (logits.new_empty((N, top), dtype=torch.int64), f(N, top)) if top else (None, None)
     workspace, size = _work(workspace, _logprobs_bytes(*logits.shape, top, logits.dtype), dev)
-    _run2("dla_token_logprobs", dev, desc, _logit_rows(logits, "logits"), _ptr(tokens), _ptr(lp), lse.data_ptr(),
+    _call("dla_token_logprobs", dev, desc, _logit_rows(logits, "logits"), _ptr(tokens), _ptr(lp), lse.data_ptr(),
           _ptr(ent), _ptr(ids), _ptr(tops), _ptr(workspace), size)
     return lp, lse, ent, ids, tops
 
@@ -291,10 +298,10 @@ def token_logprobs_backward(logits, tokens, logprob, lse, dlogprob=None, *, entr
                     ("dentropy", dentropy), ("dlse", dlse)):
         _like(t, (N,), f32, dev, name, True)
     if dlogits is None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        dlogits = _new(logits)
     else:
         _like(dlogits, logits.shape, logits.dtype, dev, "dlogits")
-    _run2("dla_token_logprobs_backward", dev, desc, _logit_rows(logits, "logits"), _ptr(tokens), _ptr(logprob),
+    _call("dla_token_logprobs_backward", dev, desc, _logit_rows(logits, "logits"), _ptr(tokens), _ptr(logprob),
           _ptr(lse), _ptr(entropy), _ptr(dlogprob), _ptr(dentropy), _ptr(dlse), _logit_rows(dlogits, "dlogits"))
     return dlogits
 
@@ -334,14 +341,18 @@ def gated_ff(x, w_gate, w_up, *, out=None, want_parts: bool = False, workspace=N
     Returns (y, parts): the products [2, N, F] that gated_ff_backward needs, or None."""
     N, D, F = _ff_sizes(x, w_gate, w_up)
     dev = x.device
+    new = lambda t: _ROWS.pack(t.data_ptr(), F)  # noqa: E731
     if out is None:
-        out = torch.empty((N, F), dtype=x.dtype, device=dev)
-    parts = torch.empty((2, N, F), dtype=x.dtype, device=dev) if want_parts else None
+        out = x.new_empty((N, F))
+        y = new(out)
+    else:
+        y = _ff_rows(out, (N, F), x, "out")
+    parts = x.new_empty((2, N, F)) if want_parts else None
     rows = _ff_rows(x, (N, D), x, "x"), _ff_rows(w_gate, (F, D), x, "w_gate"), _ff_rows(w_up, (F, D), x, "w_up")
     need = gated_ff_workspace_bytes(N, D, F, x.dtype, aligned=_aligned(x, w_gate, w_up))
     workspace, size = _work(workspace, need, dev)
-    _run2("dla_gated_ff", dev, _FF.pack(N, D, F, _dtype_code(x.dtype)), *rows, _ff_rows(out, (N, F), x, "out"),
-          *([_ff_rows(p, (N, F), x, "parts") for p in parts] if want_parts else (None, None)), _ptr(workspace), size)
+    _call("dla_gated_ff", dev, _FF.pack(N, D, F, _dtype_code(x.dtype)), *rows, y,
+          *(map(new, parts) if want_parts else (None, None)), _ptr(workspace), size)
     return out, parts
 
 
@@ -353,11 +364,10 @@ def gated_ff_backward(x, w_gate, w_up, parts, dy, *, workspace=None):
     rows = _ff_rows(x, (N, D), x, "x"), _ff_rows(w_gate, (F, D), x, "w_gate"), _ff_rows(w_up, (F, D), x, "w_up")
     if parts.shape != (2, N, F):
         raise ValueError(f"parts {tuple(parts.shape)}, not {(2, N, F)}")
-    empty = lambda *s: torch.empty(s, dtype=x.dtype, device=dev)  # noqa: E731
-    dx, dwg, dwu = empty(N, D), empty(F, D), empty(F, D)
+    dx, dwg, dwu = x.new_empty((N, D)), x.new_empty((F, D)), x.new_empty((F, D))
     need = gated_ff_workspace_bytes(N, D, F, x.dtype, backward=True, aligned=_aligned(x, w_gate, w_up))
     workspace, size = _work(workspace, need, dev)
-    _run2("dla_gated_ff_backward", dev, _FF.pack(N, D, F, _dtype_code(x.dtype)), *rows,
+    _call("dla_gated_ff_backward", dev, _FF.pack(N, D, F, _dtype_code(x.dtype)), *rows,
           _ff_rows(parts[0], (N, F), x, "parts"), _ff_rows(parts[1], (N, F), x, "parts"), _ff_rows(dy, (N, F), x, "dy"),
           _ff_rows(dx, (N, D), x, "dx"), _ff_rows(dwg, (F, D), x, "dw_gate"), _ff_rows(dwu, (F, D), x, "dw_up"),
           _ptr(workspace), size)

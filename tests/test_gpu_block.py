@@ -1,0 +1,243 @@
+"""The operators around the recurrence together: the differentiable functions against direct calls, a model of
+whole blocks against its formulas in float64, its steps token by token, and two calls at once."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def _block():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2606_10650_amd import block
+    return block
+
+
+def _rnd(seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return lambda *s: torch.randn(s, generator=gen, device="cuda")
+
+
+def _same(leaf, want):
+    assert leaf.grad is not None and torch.equal(leaf.grad, want)
+
+
+def _no_second(out, leaf):
+    g, = torch.autograd.grad(out.sum(), leaf, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
+def test_short_conv_function():
+    block, rnd = _block(), _rnd(1)
+    x, w, b, S = (t.requires_grad_() for t in (rnd(2, 30, 24), rnd(24, 4), rnd(24), rnd(2, 3, 24)))
+    starts = torch.rand((2, 30), device="cuda") < 0.2
+    do, dS = rnd(2, 30, 24), rnd(2, 3, 24)
+    for use_out, use_state in ((1, 1), (1, 0), (0, 1)):
+        for t in (x, w, b, S):
+            t.grad = None
+        out, last = block.ShortConv.apply(x, w, b, "silu", S, None, starts)
+        # a gradient with its last axis strided
+        loss = use_out * (out * do.transpose(1, 2).contiguous().transpose(1, 2)).sum() if use_out else 0.0
+        loss = loss + ((last * dS).sum() if use_state else 0.0)
+        loss.backward()
+        with torch.no_grad():
+            want = block.short_conv_backward(x, w, do if use_out else torch.zeros_like(do), b, state=S, starts=starts,
+                                             dstate=dS if use_state else None)
+        for leaf, g in zip((x, w, b, S), want):
+            _same(leaf, g)
+    _no_second(block.ShortConv.apply(x, w)[0], x)
+    # an input with its last axis strided, and a broadcast gradient
+    t = rnd(2, 24, 30).requires_grad_()
+    block.ShortConv.apply(t.transpose(1, 2), w)[0].sum().backward()
+    with torch.no_grad():
+        want = block.short_conv_backward(t.transpose(1, 2).contiguous(), w, torch.ones(2, 30, 24, device="cuda"))[0]
+    _same(t, want.transpose(1, 2))
+
+
+@pytest.mark.parametrize("heads", [True, False])
+def test_gated_norm_function(heads):
+    block, rnd = _block(), _rnd(2)
+    shape = (3, 5, 4, 32) if heads else (3, 5, 64)
+    x, z, res = (rnd(*shape).requires_grad_() for _ in range(3))
+    w = (rnd(4, 32) if heads else rnd(64)).requires_grad_()
+    w2 = None if heads else rnd(64).requires_grad_()
+    dh, dy = rnd(*shape), rnd(*shape)
+    rows = lambda t: t.reshape(-1, *shape[-w.dim():])  # noqa: E731
+    for use in ((1, 1), (1, 0), (0, 1))[:1 if heads else 3]:
+        for t in (x, z, res, w, w2):
+            if t is not None:
+                t.grad = None
+        h, y = block.GatedNorm.apply(x, w, z, res, 0.5, w2)
+        assert h.shape == shape and (y is None) == heads
+        loss = (h * dh).sum() * use[0] if use[0] else 0.0
+        if use[1] and not heads:
+            loss = loss + (y * dy).sum()
+        loss.backward()
+        with torch.no_grad():
+            _, _, rstd, y_rstd = block.gated_norm(rows(x), w, rows(z), rows(res), scale=0.5, next_weight=w2)
+            want = block.gated_norm_backward(rows(dh) if use[0] else torch.zeros_like(rows(dh)), rows(x), w, rstd, rows(z),
+                                             rows(res), scale=0.5, next_weight=w2, y_rstd=y_rstd,
+                                             dy=rows(dy) if use[1] and not heads else None)
+        for leaf, g in zip((x, z, res, w), want):
+            _same(leaf, g.reshape(leaf.shape))
+        if w2 is not None:
+            _same(w2, want[4])
+    _no_second(block.GatedNorm.apply(x, w, z)[0], x)
+
+
+def test_gated_ff_function():
+    block, rnd = _block(), _rnd(3)
+    for N in ((4,), (5, 30)):
+        x, wg, wu = (t.to(torch.bfloat16).requires_grad_() for t in (rnd(*N, 40), rnd(56, 40), rnd(56, 40)))
+        dy = rnd(*N, 56).to(torch.bfloat16)
+        y = block.GatedFF.apply(x, wg, wu)
+        assert y.shape == dy.shape
+        (y * dy).sum().backward()
+        with torch.no_grad():
+            flat = x.reshape(-1, 40)
+            _, parts = block.gated_ff(flat, wg, wu, want_parts=True)
+            want = block.gated_ff_backward(flat, wg, wu, parts, dy.reshape(-1, 56))
+        for leaf, g in zip((x, wg, wu), want):
+            _same(leaf, g.reshape(leaf.shape))
+        _no_second(block.GatedFF.apply(x, wg, wu), x)
+
+
+def test_token_logprobs_function():
+    block, rnd = _block(), _rnd(4)
+    l = rnd(3, 7, 100).requires_grad_()
+    tok = torch.randint(-20, 100, (3, 7), device="cuda")
+    a, b, c = rnd(3, 7), rnd(3, 7), rnd(3, 7)
+    lp, ent, lse = block.TokenLogprobs.apply(l, tok)
+    (lp * a + ent * b + lse * c).sum().backward()
+    L = l.detach().double().requires_grad_()
+    logp = torch.log_softmax(L, -1)
+    want = torch.where(tok >= 0, logp.gather(-1, tok.clamp(min=0)[..., None])[..., 0], 0.0)
+    ((want * a) + -(logp.exp() * logp).sum(-1) * b + torch.logsumexp(L, -1) * c).sum().backward()
+    # float32 probabilities to 2^-19 of themselves, times weights and log probabilities of order ten
+    assert (l.grad - L.grad).norm() <= 1e-5 * L.grad.norm()
+    l.grad = None
+    block.TokenLogprobs.apply(l, tok)[0].mean().backward()     # a broadcast gradient
+    assert torch.isfinite(l.grad).all() and not l.grad[tok < 0].any()
+    _no_second(block.TokenLogprobs.apply(l, tok)[0], l)
+
+
+def _model(**kw):
+    _block()
+    from paper_2606_10650_amd.train_example import Model
+    return Model(48, layers=2, heads=2, d=64, width=72, full=True, **kw)
+
+
+def _formula(p, m, tokens):
+    """Logits of whole sequences in float64, token by token in the recurrence."""
+    s, (B, T) = 0.5 ** 0.5, tokens.shape
+    norm = lambda x, w: w * x / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt()  # noqa: E731
+    unit = lambda x: x / x.norm(dim=-1, keepdim=True).clamp(min=1e-12)  # noqa: E731
+    h = p["embed"][tokens]
+    y = norm(h, p["0.norm"])
+    for i in range(m.layers):
+        x = torch.nn.functional.pad(y @ p[f"{i}.qkv"].t(), (0, 0, 3, 0))
+        x = sum(x[:, j:j + T] * p[f"{i}.conv"][:, j] for j in range(4))
+        q, k, v = (x * torch.sigmoid(x)).unflatten(-1, (3, m.heads, m.d)).unbind(2)
+        q, k = unit(q), unit(k)
+        g = torch.nn.functional.logsigmoid(y @ p[f"{i}.gate"].t() + 5.0)
+        S, o = 0.0, []
+        for t in range(T):
+            S = g[:, t].exp()[..., None, None] * S + k[:, t, :, :, None] * v[:, t, :, None]
+            o.append(m.d ** 0.5 * (S * q[:, t, :, :, None]).sum(-2))
+        z = (y @ p[f"{i}.z"].t()).unflatten(-1, (m.heads, m.d))
+        o = norm(torch.stack(o, 1), p[f"{i}.heads"]) * z * torch.sigmoid(z)
+        h = h + s * norm(o.flatten(2) @ p[f"{i}.out"].t(), p[f"{i}.post"])
+        y = norm(h, p[f"{i}.ff_norm"])
+        a, b = y @ p[f"{i}.ff_gate"].t(), y @ p[f"{i}.ff_up"].t()
+        h = h + s * norm((a * torch.sigmoid(a) * b) @ p[f"{i}.ff_down"].t(), p[f"{i}.ff_post"])
+        y = norm(h, p[f"{i + 1}.norm" if i + 1 < m.layers else "norm"])
+    return y @ p["embed"].t()
+
+
+def _against_formulas(m, values, grads):
+    """Relative to a tensor's norm: logits, loss, and every parameter's gradient."""
+    rnd = torch.Generator(device="cuda").manual_seed(7)
+    tokens = torch.randint(0, 48, (3, 21), generator=rnd, device="cuda")
+    answers = torch.randint(0, 48, (3, 21), generator=rnd, device="cuda")
+    answers[0, :5] = -100
+    p = {k: v.detach().double().requires_grad_() for k, v in m.params.items()}
+    want = _formula(p, m, tokens)
+    logp = torch.log_softmax(want, -1).gather(-1, answers.clamp(min=0)[..., None])[..., 0]
+    loss = -torch.where(answers >= 0, logp, 0.0).mean()
+    loss.backward()
+    logits = m(tokens)
+    assert (logits - want).norm() <= values * want.norm()
+    got = m.loss(logits, answers)
+    assert abs(got.item() - loss.item()) <= values * loss.item()
+    got.backward()
+    for k, v in m.params.items():
+        err = (v.grad.double() - p[k].grad).norm() / p[k].grad.norm()
+        assert err <= grads, (k, err.item())
+
+
+def test_model_against_its_formulas():
+    """In bfloat16.  A layer's forward pass rounds 17 times (the norms' two outputs each, projections, q and k, the
+    recurrence's state, the parts of the feed-forward block), its backward pass the gradients of as many, each by
+    2^-8 at most and, over the mantissas, 2^-9.3 in the mean square, of parts that norms keep at a size of one.  To
+    the logits of two layers that is sqrt(34) 2^-9.3 = 0.009 where errors are independent: 0.05 has room for
+    five times that.  Gradients have 72 roundings on their way; where a parameter's come to it by one path and
+    add up, as an embedding's through the first norm, 72 2^-9.3 = 0.114."""
+    _against_formulas(_model(), 0.05, 0.12)
+
+
+def test_float32_model_against_its_formulas():
+    """The same in float32: 72 roundings of 2^-24, sums of up to 144 products of 2^-24 each, and of float32 products
+    in bfloat16 terms 2^-22: 72 (144 2^-24 + 2^-22) = 6.4e-4 where all add up."""
+    m = _model()
+    for k, v in m.params.items():
+        m.params[k] = v.detach().float().requires_grad_()
+    _against_formulas(m, 7e-4, 7e-4)
+
+
+def test_model_token_by_token():
+    """Steps with carried states against whole sequences: the same operators on the same values, with other
+    sums' orders (products of a few rows, the recurrence's steps), so each bfloat16 may round to its other
+    neighbour: as far off as two runs of the above may be from their formula."""
+    m = _model(seed=3)
+    tokens = torch.randint(0, 48, (5, 40), generator=torch.Generator(device="cuda").manual_seed(8), device="cuda")
+    with torch.no_grad():
+        whole, carried = m(tokens), {}
+        single = torch.stack([m.step(tokens[:, t], carried) for t in range(40)], 1)
+    assert (single - whole).norm() <= 0.1 * whole.norm()
+
+
+@pytest.mark.parametrize("states", ["f32", "fp8"])
+def test_example_runs(states):
+    _block()
+    from paper_2606_10650_amd import train_example
+    said = []
+    losses, off, same = train_example.main(3, states, say=said.append, full=True)
+    assert len(losses) == 3 and all(x == x for x in losses) and off < 0.1 and any("entropy" in s for s in said)
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with its own workspace, as each alone."""
+    block, rnd = _block(), _rnd(9)
+    ins = []
+    for i in range(2):
+        x, w = rnd(700, 256).to(torch.bfloat16), rnd(512, 256).to(torch.bfloat16)
+        l, tok = rnd(3, 100000), torch.randint(0, 100000, (3,), device="cuda")
+        ins.append((x, w, rnd(512, 256).to(torch.bfloat16), rnd(700, 512).to(torch.bfloat16), l, tok))
+
+    def run(x, wg, wu, dy, l, tok):
+        y, parts = block.gated_ff(x, wg, wu, want_parts=True)
+        return (y, *block.gated_ff_backward(x, wg, wu, parts, dy), *block.token_logprobs(l, tok, top=20, entropy=True))
+
+    alone = [run(*v) for v in ins]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ins]
+    got = [[], []]
+    for _ in range(3):
+        for i, (s, v) in enumerate(zip(streams, ins)):
+            with torch.cuda.stream(s):
+                got[i].append(run(*v))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(out, alone[i]))
