@@ -180,9 +180,9 @@ dla_status dla_token_logprobs_backward(const dla_logprobs_desc* desc, const dla_
 /*
  * The gated feed-forward block:
  *   g = x w_gate^T,  u = x w_up^T,  y = u g / (1 + exp(-g))
- * x [rows][D], w_gate and w_up [F][D], g, u and y [rows][F], all of dtype, each a set of rows
- * `stride` elements apart (at least the row's length; inputs may repeat rows), contiguous in
- * themselves.
+ * x [rows][D], w_gate and w_up [F][D] and y [rows][F] of dtype, g and u [rows][F] float32, each a
+ * set of rows `stride` elements apart (at least the row's length; inputs may repeat rows),
+ * contiguous in themselves.
  *
  * 0 <= rows <= 2^31 - 257, 1 <= D, F <= 65536.  Sums are float32.  Of bfloat16 inputs every
  * product is exact; y is formed from unrounded g and u.  float32 inputs are taken as sums of
@@ -203,7 +203,8 @@ typedef struct {
 dla_status dla_gated_ff_workspace_size(const dla_ff_desc* desc, int32_t backward, int32_t aligned,
                                        size_t* bytes);
 
-/* g, u: where the parts that the backward pass needs go, rounded to dtype, or both NULL. */
+/* g, u: where the parts that the backward pass needs go, or both NULL.  (Rounded to bfloat16 they
+ * would add as much to the gradients' errors as dg's and du's rounding does.) */
 dla_status dla_gated_ff(const dla_ff_desc* desc, const dla_norm_rows* x,
                         const dla_norm_rows* w_gate, const dla_norm_rows* w_up,
                         const dla_norm_rows* y, const dla_norm_rows* g, const dla_norm_rows* u,

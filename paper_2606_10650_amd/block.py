@@ -338,7 +338,7 @@ def gated_ff_workspace_bytes(N: int, D: int, F: int, dtype=torch.bfloat16, *, ba
 
 def gated_ff(x, w_gate, w_up, *, out=None, want_parts: bool = False, workspace=None):
     """y = silu(x w_gate^T) * (x w_up^T) (dla_gated_ff).  x: [N, D], w_gate and w_up [F, D], last axes contiguous.
-    Returns (y, parts): the products [2, N, F] that gated_ff_backward needs, or None."""
+    Returns (y, parts): the products [2, N, F], float32, that gated_ff_backward needs, or None."""
     N, D, F = _ff_sizes(x, w_gate, w_up)
     dev = x.device
     new = lambda t: _ROWS.pack(t.data_ptr(), F)  # noqa: E731
@@ -347,7 +347,7 @@ def gated_ff(x, w_gate, w_up, *, out=None, want_parts: bool = False, workspace=N
         y = new(out)
     else:
         y = _ff_rows(out, (N, F), x, "out")
-    parts = x.new_empty((2, N, F)) if want_parts else None
+    parts = x.new_empty((2, N, F), dtype=torch.float32) if want_parts else None
     rows = _ff_rows(x, (N, D), x, "x"), _ff_rows(w_gate, (F, D), x, "w_gate"), _ff_rows(w_up, (F, D), x, "w_up")
     need = gated_ff_workspace_bytes(N, D, F, x.dtype, aligned=_aligned(x, w_gate, w_up))
     workspace, size = _work(workspace, need, dev)
@@ -362,13 +362,12 @@ def gated_ff_backward(x, w_gate, w_up, parts, dy, *, workspace=None):
     N, D, F = _ff_sizes(x, w_gate, w_up)
     dev = x.device
     rows = _ff_rows(x, (N, D), x, "x"), _ff_rows(w_gate, (F, D), x, "w_gate"), _ff_rows(w_up, (F, D), x, "w_up")
-    if parts.shape != (2, N, F):
-        raise ValueError(f"parts {tuple(parts.shape)}, not {(2, N, F)}")
+    _like(parts, (2, N, F), torch.float32, dev, "parts", True)
     dx, dwg, dwu = x.new_empty((N, D)), x.new_empty((F, D)), x.new_empty((F, D))
     need = gated_ff_workspace_bytes(N, D, F, x.dtype, backward=True, aligned=_aligned(x, w_gate, w_up))
     workspace, size = _work(workspace, need, dev)
     _call("dla_gated_ff_backward", dev, _FF.pack(N, D, F, _dtype_code(x.dtype)), *rows,
-          _ff_rows(parts[0], (N, F), x, "parts"), _ff_rows(parts[1], (N, F), x, "parts"), _ff_rows(dy, (N, F), x, "dy"),
+          _ROWS.pack(parts.data_ptr(), F), _ROWS.pack(parts.data_ptr() + 4 * N * F, F), _ff_rows(dy, (N, F), x, "dy"),
           _ff_rows(dx, (N, D), x, "dx"), _ff_rows(dwg, (F, D), x, "dw_gate"), _ff_rows(dwu, (F, D), x, "dw_up"),
           _ptr(workspace), size)
     return dx, dwg, dwu

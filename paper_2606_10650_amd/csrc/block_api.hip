@@ -500,8 +500,8 @@ dla_status dla_gated_ff(const dla_ff_desc* desc, const dla_norm_rows* x,
   const int e = size_of(d.dtype);
   if (d.rows == 0) return remember(DLA_OK);
   if (!rows_ok(x, d.rows, d.D, e, false) || !rows_ok(w_gate, d.F, d.D, e, false) || !rows_ok(w_up, d.F, d.D, e, false) ||
-      !rows_ok(y, d.rows, d.F, e, true) || (g && !rows_ok(g, d.rows, d.F, e, true)) ||
-      (u && !rows_ok(u, d.rows, d.F, e, true)) || !g != !u)
+      !rows_ok(y, d.rows, d.F, e, true) || (g && !rows_ok(g, d.rows, d.F, 4, true)) ||
+      (u && !rows_ok(u, d.rows, d.F, 4, true)) || !g != !u)
     return remember(DLA_ERR_INVALID_ARG);
   hipStream_t st = (hipStream_t)stream;
   if (d.rows <= kFfStepRows)
@@ -554,8 +554,8 @@ dla_status dla_gated_ff_backward(const dla_ff_desc* desc, const dla_norm_rows* x
   if ((dw_gate && !rows_ok(dw_gate, d.F, d.D, e, true)) || (dw_up && !rows_ok(dw_up, d.F, d.D, e, true)))
     return remember(DLA_ERR_INVALID_ARG);
   if (d.rows && (!rows_ok(x, d.rows, d.D, e, false) || !rows_ok(w_gate, d.F, d.D, e, false) ||
-                 !rows_ok(w_up, d.F, d.D, e, false) || !rows_ok(g, d.rows, d.F, e, false) ||
-                 !rows_ok(u, d.rows, d.F, e, false) || !rows_ok(dy, d.rows, d.F, e, false) ||
+                 !rows_ok(w_up, d.F, d.D, e, false) || !rows_ok(g, d.rows, d.F, 4, false) ||
+                 !rows_ok(u, d.rows, d.F, 4, false) || !rows_ok(dy, d.rows, d.F, e, false) ||
                  (dx && !rows_ok(dx, d.rows, d.D, e, true))))
     return remember(DLA_ERR_INVALID_ARG);
   hipStream_t st = (hipStream_t)stream;

@@ -19,7 +19,7 @@ hipError_t launch_ff_step(int64_t rows, int D, int F, int dtype, FfRows x, FfRow
 // plane, of float32 three, their terms from the largest down, each plane rows round_up(cols, 8) long.
 hipError_t launch_ff_pack(int64_t rows, int cols, int dtype, FfRows from, uint16_t* to, hipStream_t st);
 
-// dg and du from g, u and dy: planes as above of rows with round_up(F, 8) values of dg, then as
+// dg and du from g and u, float32, and dy: planes as above of rows with round_up(F, 8) values of dg, then as
 // many of du.
 hipError_t launch_ff_parts(int64_t rows, int F, int dtype, FfRows g, FfRows u, FfRows dy, uint16_t* to, hipStream_t st);
 
@@ -37,7 +37,7 @@ struct FfGemm {
   const uint16_t* b2[kFfPlanes];
   int64_t lda, ldb;
   uint64_t ia, ib;    // four bits a pair, the first in the lowest
-  FfRows c, g, u;     // kind 0: c is y
+  FfRows c, g, u;     // kind 0: c is y; g and u are float32
   FfRows c2;          // kind 2: where the rows from `half` on go; each half has `rows` of them
   int64_t half, rows;
   float* part;        // FfPlan's part_bytes

@@ -95,14 +95,12 @@ __global__ __launch_bounds__(512) void ff_step_kernel(int rows, int D, int F, Ff
       uv += sums[w][1][b][m][r];
     }
     if (row < rows && col < F) {
-      auto put = [&](const FfRows& o, float v) {
-        if constexpr (sizeof(T) == 2) static_cast<__bf16*>(o.p)[row * o.st + col] = (__bf16)v;
-        else static_cast<float*>(o.p)[row * o.st + col] = v;
-      };
-      put(y, gv * sigmoid(gv) * uv);
+      const float v = gv * sigmoid(gv) * uv;
+      if constexpr (sizeof(T) == 2) static_cast<__bf16*>(y.p)[row * y.st + col] = (__bf16)v;
+      else static_cast<float*>(y.p)[row * y.st + col] = v;
       if (g.p) {
-        put(g, gv);
-        put(u, uv);
+        static_cast<float*>(g.p)[row * g.st + col] = gv;
+        static_cast<float*>(u.p)[row * u.st + col] = uv;
       }
     }
   }
@@ -167,8 +165,18 @@ __global__ __launch_bounds__(256) void ff_parts_kernel(int64_t rows, int F, int 
     const int64_t row = i / per;
     const int c = (int)(i % per) * N, n = F > c ? F - c : 0;
     float gv[N], uv[N], d[N], e[N];
-    Piece<T>::load(static_cast<const T*>(g.p) + row * g.st + c, n, gv);
-    Piece<T>::load(static_cast<const T*>(u.p) + row * u.st + c, n, uv);
+#pragma unroll
+    for (int h = 0; h < N; h += 4) {
+      float x[4], y[4];
+      const int left = n > h ? n - h : 0;
+      Piece<float>::load(static_cast<const float*>(g.p) + row * g.st + c + h, left, x);
+      Piece<float>::load(static_cast<const float*>(u.p) + row * u.st + c + h, left, y);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        gv[h + j] = x[j];
+        uv[h + j] = y[j];
+      }
+    }
     Piece<T>::load(static_cast<const T*>(dy.p) + row * dy.st + c, n, d);
 #pragma unroll
     for (int j = 0; j < N; ++j) {

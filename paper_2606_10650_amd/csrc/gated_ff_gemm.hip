@@ -107,7 +107,7 @@ __device__ __forceinline__ void put4(const FfRows& r, int64_t m, int64_t n, int6
 }
 
 // A wave's place in a tile of C from its sums.  mine: kLine * 32 bytes of LDS.
-constexpr int kLine = 80;
+constexpr int kLine = 144;
 
 template <int KIND, int TM, int TN, int WM, int WN>
 __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM / WM / 32][TN / WN / 32], int64_t m0,
@@ -116,47 +116,55 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
   const int wm = wave / WN, wn = wave % WN;
   const int64_t mw = m0 + wm * (TM / WM), nw = n0 + wn * (WIDTH / WN);   // the wave's corner
   const int l32 = lane & 31, half = lane >> 5;
-  // A wave's columns of C, of one of the outputs, in rows of 64 bytes through LDS (80, so that eight lanes'
-  // pieces have other banks), so that memory is written 16 bytes a lane.
-  auto out = [&](const FfRows& r, int64_t rows, int64_t m, int64_t c, bool later, auto value) {
+  // A wave's columns of C, of one of the outputs, through LDS in rows of kLine bytes (so that eight lanes' pieces
+  // have other banks), so that memory is written 16 bytes a lane.
+  auto out = [&](const FfRows& r, int f32, int64_t rows, int64_t m, int64_t c, bool later, auto value) {
     // value(e): element e of the lane; its row is m + l32, its columns c + out_row(e, lane); later: g and u,
-    // which only the backward pass reads, are not to take the operands' place in the caches (675 us
-    // become 655)
+    // which only the backward pass reads, are not to take the operands' place in the caches (with both in
+    // bfloat16 675 us became 655)
     if (!r.p) return;
-    const bool pieces = !p.out_f32 && ((uintptr_t)r.p & 15) == 0 && r.st % 8 == 0;
+    const bool pieces = ((uintptr_t)r.p & 15) == 0 && r.st % (f32 ? 4 : 8) == 0;
     if (!pieces) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float v[4] = {value(4 * e), value(4 * e + 1), value(4 * e + 2), value(4 * e + 3)};
-        if ((uint64_t)(m + l32) < (uint64_t)rows) put4(r, m + l32, c + 8 * e + 4 * half, p.N, p.out_f32, v);
+        if ((uint64_t)(m + l32) < (uint64_t)rows) put4(r, m + l32, c + 8 * e + 4 * half, p.N, f32, v);
       }
       return;
     }
+    auto pass = [&](auto type) {
+      using T = decltype(type);
+      constexpr int N = 16 / (int)sizeof(T), PER = 32 / N;      // values of a piece, pieces of a row
+      typedef T four __attribute__((ext_vector_type(4)));
+      typedef T vec __attribute__((ext_vector_type(N)));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      bf16x4 v;
+      for (int e = 0; e < 4; ++e) {
+        four v;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = (__bf16)value(4 * e + q);
-      *reinterpret_cast<bf16x4*>(mine + l32 * kLine + (8 * e + 4 * half) * 2) = v;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int q = 0; q < 4; ++q) v[q] = (T)value(4 * e + q);
+        *reinterpret_cast<four*>(mine + l32 * kLine + (8 * e + 4 * half) * (int)sizeof(T)) = v;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int row = 16 * t + (lane >> 2), col = 8 * (lane & 3);
-      const bf16x8 v = *reinterpret_cast<const bf16x8*>(mine + row * kLine + col * 2);
-      if ((uint64_t)(m + row) < (uint64_t)rows) {   // (m is below zero where a tile holds the end of one half)
-        __bf16* to = static_cast<__bf16*>(r.p) + (m + row) * r.st + c + col;
-        if (c + col + 8 <= p.N) {
-          if (later) __builtin_nontemporal_store(v, reinterpret_cast<bf16x8*>(to));
-          else *reinterpret_cast<bf16x8*>(to) = v;
-        } else {
+      for (int t = 0; t < PER / 2; ++t) {
+        const int row = (64 / PER) * t + lane / PER, col = N * (lane % PER);
+        const vec v = *reinterpret_cast<const vec*>(mine + row * kLine + col * (int)sizeof(T));
+        if ((uint64_t)(m + row) < (uint64_t)rows) {   // (m is below zero where a tile holds the end of one half)
+          T* to = static_cast<T*>(r.p) + (m + row) * r.st + c + col;
+          if (c + col + N <= p.N) {
+            if (later) __builtin_nontemporal_store(v, reinterpret_cast<vec*>(to));
+            else *reinterpret_cast<vec*>(to) = v;
+          } else {
 #pragma unroll
-          for (int q = 0; q < 8; ++q)
-            if (c + col + q < p.N) to[q] = v[q];
+            for (int q = 0; q < N; ++q)
+              if (c + col + q < p.N) to[q] = v[q];
+          }
         }
       }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    if (f32) pass(0.f);
+    else pass((__bf16)0.f);
   };
 #pragma unroll
   for (int i = 0; i < SM; ++i) {
@@ -165,9 +173,9 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
 #pragma unroll
       for (int j = 0; j < SN; j += 2) {
         const int64_t c = nw + 16 * j;
-        out(p.c, p.M, m, c, false, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; });
-        out(p.g, p.M, m, c, true, [&](int e) { return acc[i][j][e]; });
-        out(p.u, p.M, m, c, true, [&](int e) { return acc[i][j + 1][e]; });
+        out(p.c, p.out_f32, p.M, m, c, false, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; });
+        out(p.g, 1, p.M, m, c, true, [&](int e) { return acc[i][j][e]; });
+        out(p.u, 1, p.M, m, c, true, [&](int e) { return acc[i][j + 1][e]; });
       }
     } else {
       // of kind 2 a tile's 32 rows may belong to both halves, where these are not multiples of 32 long
@@ -175,10 +183,10 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
       for (int j = 0; j < SN; ++j) {
         auto value = [&](int e) { return acc[i][j][e]; };
         if constexpr (KIND == 1) {
-          out(p.c, p.M, m, nw + 32 * j, false, value);
+          out(p.c, p.out_f32, p.M, m, nw + 32 * j, false, value);
         } else {
-          if (m < p.half) out(p.c, p.rows, m, nw + 32 * j, false, value);
-          if (m + 32 > p.half) out(p.c2, p.rows, m - p.half, nw + 32 * j, false, value);
+          if (m < p.half) out(p.c, p.out_f32, p.rows, m, nw + 32 * j, false, value);
+          if (m + 32 > p.half) out(p.c2, p.out_f32, p.rows, m - p.half, nw + 32 * j, false, value);
         }
       }
     }

@@ -229,3 +229,5 @@ def test_binding_refusals():
         block.gated_ff_backward(x, w, w, z(2, 5, 23), z(5, 24))
     with pytest.raises(ValueError):
         block.gated_ff_backward(x, w, w, z(2, 5, 24), z(5, 23))
+    with pytest.raises(ValueError):
+        block.gated_ff_backward(x, w, w, z(2, 5, 24, dtype=BF16), z(5, 24))
