@@ -184,7 +184,7 @@ dla_status dla_token_logprobs_backward(const dla_logprobs_desc* desc, const dla_
  * set of rows `stride` elements apart (at least the row's length; inputs may repeat rows),
  * contiguous in themselves.
  *
- * 0 <= rows <= 2^31 - 257, 1 <= D, F <= 65536.  Sums are float32.  Of bfloat16 inputs every
+ * 0 <= rows <= 2^30, 1 <= D, F <= 65536.  Sums are float32.  Of bfloat16 inputs every
  * product is exact; y is formed from unrounded g and u.  float32 inputs are taken as sums of
  * three bfloat16 terms, the largest first, and products of terms below 2^-24 of the whole are
  * left out: results are float32's to about 2^-22 of the sum of the products' magnitudes.  Of
@@ -197,9 +197,11 @@ typedef struct {
   int32_t dtype; /* dla_dtype */
 } dla_ff_desc;
 
-/* Workspace of a forward (backward = 0) or backward pass, in bytes.  aligned: whether data and
- * strides of every input are multiples of 16 bytes (of bfloat16, such arrays are read in
- * place; others, and float32, are first copied to the workspace). */
+/* Workspace of a forward (backward = 0) or backward pass, in bytes.  aligned: whether x and the
+ * weights start at multiples of 16 bytes, as do their rows, these at most 2^21 elements apart and
+ * both weights' equally far.  (Of bfloat16 such arrays with D, and for the backward pass F, a
+ * multiple of 8 are read in place; others, and float32, are first copied to the workspace.)  A call
+ * of up to 64 rows forward needs none. */
 dla_status dla_gated_ff_workspace_size(const dla_ff_desc* desc, int32_t backward, int32_t aligned,
                                        size_t* bytes);
 

@@ -242,20 +242,26 @@ void pairs_of(FfGemm& g, int planes, int sets) {
     }
 }
 
-// An operand's planes: in place, or packed into the workspace.
+// An operand's planes: in place, or to be packed into the workspace.
 struct FfPlanes {
-  const uint16_t* p;
-  int64_t ld, plane;
+  const uint16_t* p = nullptr;
+  int64_t ld = 0, plane = 0;
 };
-hipError_t planes_of(FfPlanes& o, bool direct, const dla_norm_rows* r, int64_t rows, int cols, int dtype, char* to,
-                     hipStream_t st) {
+FfPlanes planes_of(bool direct, const dla_norm_rows* r, int64_t rows, int cols, char* to, FfPack& pack) {
+  FfPlanes o;
   if (direct) {
-    o = FfPlanes{static_cast<const uint16_t*>(r->data), rows <= 1 ? cols : r->stride, 0};
-    return hipSuccess;
+    o.p = static_cast<const uint16_t*>(r->data);
+    o.ld = rows <= 1 ? cols : r->stride;
+  } else {
+    o.p = reinterpret_cast<const uint16_t*>(to);
+    o.ld = (int64_t)round_up(cols, 8);
+    o.plane = rows * o.ld;
+    pack.rows = rows;
+    pack.cols = cols;
+    pack.from = ff_rows(r);
+    pack.to = reinterpret_cast<uint16_t*>(to);
   }
-  const int64_t ld = (int64_t)round_up(cols, 8);
-  o = FfPlanes{reinterpret_cast<const uint16_t*>(to), ld, rows * ld};
-  return launch_ff_pack(rows, cols, dtype, ff_rows(r), reinterpret_cast<uint16_t*>(to), st);
+  return o;
 }
 
 }  // namespace
@@ -514,10 +520,11 @@ dla_status dla_gated_ff(const dla_ff_desc* desc, const dla_norm_rows* x,
   if (!workspace_ok(workspace, workspace_bytes, sp.total)) return remember(DLA_ERR_WORKSPACE);
   char* ws = (char*)workspace;
   const int planes = d.dtype == DLA_BF16 ? 1 : 3;
-  FfPlanes px, pg, pu;
-  hipError_t r = planes_of(px, direct, x, d.rows, d.D, d.dtype, ws + sp.x, st);
-  if (r == hipSuccess) r = planes_of(pg, direct, w_gate, d.F, d.D, d.dtype, ws + sp.wg, st);
-  if (r == hipSuccess) r = planes_of(pu, direct, w_up, d.F, d.D, d.dtype, ws + sp.wu, st);
+  FfPacks packs;
+  const FfPlanes px = planes_of(direct, x, d.rows, d.D, ws + sp.x, packs.set[0]);
+  const FfPlanes pg = planes_of(direct, w_gate, d.F, d.D, ws + sp.wg, packs.set[1]);
+  const FfPlanes pu = planes_of(direct, w_up, d.F, d.D, ws + sp.wu, packs.set[2]);
+  const hipError_t r = launch_ff_pack(packs, d.dtype, st);
   if (r != hipSuccess) return done(r);
   FfGemm p;
   memset(&p, 0, sizeof(p));
@@ -566,13 +573,17 @@ dla_status dla_gated_ff_backward(const dla_ff_desc* desc, const dla_norm_rows* x
   char* ws = (char*)workspace;
   const int planes = d.dtype == DLA_BF16 ? 1 : 3;
   const int64_t Fp = (int64_t)round_up(d.F, 8);
-  FfPlanes px{nullptr, 0, 0}, pg = px, pu = px;
+  FfPlanes px, pg, pu;
   uint16_t* parts = (uint16_t*)(ws + sp.parts);
   hipError_t r = hipSuccess;
   if (d.rows) {
-    r = planes_of(px, direct, x, d.rows, d.D, d.dtype, ws + sp.x, st);
-    if (r == hipSuccess && dx) r = planes_of(pg, direct, w_gate, d.F, d.D, d.dtype, ws + sp.wg, st);
-    if (r == hipSuccess && dx) r = planes_of(pu, direct, w_up, d.F, d.D, d.dtype, ws + sp.wu, st);
+    FfPacks packs;
+    px = planes_of(direct, x, d.rows, d.D, ws + sp.x, packs.set[0]);
+    if (dx) {
+      pg = planes_of(direct, w_gate, d.F, d.D, ws + sp.wg, packs.set[1]);
+      pu = planes_of(direct, w_up, d.F, d.D, ws + sp.wu, packs.set[2]);
+    }
+    r = launch_ff_pack(packs, d.dtype, st);
     if (r == hipSuccess) r = launch_ff_parts(d.rows, d.F, d.dtype, ff_rows(g), ff_rows(u), ff_rows(dy), parts, st);
     if (r != hipSuccess) return done(r);
   }

@@ -17,7 +17,17 @@ hipError_t launch_ff_step(int64_t rows, int D, int F, int dtype, FfRows x, FfRow
 
 // Rows of `cols` values as bfloat16 rows of round_up(cols, 8), zeros behind the last: of bfloat16 one
 // plane, of float32 three, their terms from the largest down, each plane rows round_up(cols, 8) long.
-hipError_t launch_ff_pack(int64_t rows, int cols, int dtype, FfRows from, uint16_t* to, hipStream_t st);
+// Up to three sets of rows at once.
+struct FfPack {
+  int64_t rows = 0;
+  int cols = 0;
+  FfRows from;
+  uint16_t* to = nullptr;
+};
+struct FfPacks {
+  FfPack set[3];
+};
+hipError_t launch_ff_pack(const FfPacks& sets, int dtype, hipStream_t st);
 
 // dg and du from g and u, float32, and dy: planes as above of rows with round_up(F, 8) values of dg, then as
 // many of du.

@@ -142,16 +142,17 @@ __device__ __forceinline__ void put_planes(uint16_t* to, int64_t plane, const fl
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void ff_pack_kernel(int64_t rows, int cols, int ld, FfRows from, uint16_t* to) {
+__global__ __launch_bounds__(256) void ff_pack_kernel(FfPacks sets) {
   constexpr int N = Piece<T>::N;
-  const int per = ld / N;
-  const int64_t total = rows * per, step = (int64_t)gridDim.x * 256;
+  const FfPack& p = sets.set[blockIdx.y];
+  const int ld = (p.cols + 7) & ~7, per = ld / N;
+  const int64_t total = p.rows * per, step = (int64_t)gridDim.x * 256;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
     const int64_t row = i / per;
     const int c = (int)(i % per) * N;
     float v[N];
-    Piece<T>::load(static_cast<const T*>(from.p) + row * from.st + c, cols > c ? cols - c : 0, v);
-    put_planes<T, N>(to + row * ld + c, rows * ld, v);
+    Piece<T>::load(static_cast<const T*>(p.from.p) + row * p.from.st + c, p.cols > c ? p.cols - c : 0, v);
+    put_planes<T, N>(p.to + row * ld + c, p.rows * ld, v);
   }
 }
 
@@ -214,12 +215,16 @@ hipError_t launch_ff_step(int64_t rows, int D, int F, int dtype, FfRows x, FfRow
                            : step<float>((int)rows, D, F, x, wg, wu, y, g, u, st);
 }
 
-hipError_t launch_ff_pack(int64_t rows, int cols, int dtype, FfRows from, uint16_t* to, hipStream_t st) {
-  const int ld = (int)round_up(cols, 8), N = dtype == DLA_BF16 ? 8 : 4;
-  const dim3 grid(groups_of(rows * (ld / N))), block(256);
-  if (rows == 0) return hipSuccess;
-  if (dtype == DLA_BF16) hipLaunchKernelGGL(ff_pack_kernel<bf16_t>, grid, block, 0, st, rows, cols, ld, from, to);
-  else hipLaunchKernelGGL(ff_pack_kernel<float>, grid, block, 0, st, rows, cols, ld, from, to);
+hipError_t launch_ff_pack(const FfPacks& sets, int dtype, hipStream_t st) {
+  int64_t most = 0;
+  for (const FfPack& p : sets.set) {
+    const int64_t n = p.rows * (int64_t)(round_up(p.cols, 8) / (dtype == DLA_BF16 ? 8 : 4));
+    if (n > most) most = n;
+  }
+  if (most == 0) return hipSuccess;
+  const dim3 grid(groups_of(most), 3), block(256);
+  if (dtype == DLA_BF16) hipLaunchKernelGGL(ff_pack_kernel<bf16_t>, grid, block, 0, st, sets);
+  else hipLaunchKernelGGL(ff_pack_kernel<float>, grid, block, 0, st, sets);
   return hipGetLastError();
 }
 

@@ -7,6 +7,8 @@
 // banks; a tile whose rows are K (an operand that is used transposed) as it lies in memory, 64-byte
 // units exchanged by the row modulo 4, and is transposed by the reads of 4 rows of 16 columns.
 // What lies outside an operand is zero.
+#include <type_traits>
+
 #include "gated_ff.h"
 #include "mfma.h"
 
@@ -109,7 +111,7 @@ __device__ __forceinline__ void put4(const FfRows& r, int64_t m, int64_t n, int6
 // A wave's place in a tile of C from its sums.  mine: kLine * 32 bytes of LDS.
 constexpr int kLine = 144;
 
-template <int KIND, int TM, int TN, int WM, int WN>
+template <int KIND, int TM, int TN, int WM, int WN, bool F32>
 __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM / WM / 32][TN / WN / 32], int64_t m0,
                                          int64_t n0, char* mine, int lane, int wave) {
   constexpr int SM = TM / WM / 32, SN = TN / WN / 32, WIDTH = KIND == 0 ? TN / 2 : TN;
@@ -118,8 +120,10 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
   const int l32 = lane & 31, half = lane >> 5;
   // A wave's columns of C, of one of the outputs, through LDS in rows of kLine bytes (so that eight lanes' pieces
   // have other banks), so that memory is written 16 bytes a lane.
-  auto out = [&](const FfRows& r, int f32, int64_t rows, int64_t m, int64_t c, bool later, auto value) {
-    // value(e): element e of the lane; its row is m + l32, its columns c + out_row(e, lane); later: g and u,
+  auto out = [&](auto kind, const FfRows& r, int64_t rows, int64_t m, int64_t c, auto value) {
+    using T = decltype(kind);
+    constexpr bool f32 = sizeof(T) == 4, later = f32 && KIND == 0;
+    // value(e): element e of the lane; its row is m + l32, its columns c + out_row(e, lane); g and u,
     // which only the backward pass reads, are not to take the operands' place in the caches (with both in
     // bfloat16 675 us became 655)
     if (!r.p) return;
@@ -132,8 +136,7 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
       }
       return;
     }
-    auto pass = [&](auto type) {
-      using T = decltype(type);
+    {
       constexpr int N = 16 / (int)sizeof(T), PER = 32 / N;      // values of a piece, pieces of a row
       typedef T four __attribute__((ext_vector_type(4)));
       typedef T vec __attribute__((ext_vector_type(N)));
@@ -162,10 +165,9 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    };
-    if (f32) pass(0.f);
-    else pass((__bf16)0.f);
+    }
   };
+  const typename std::conditional<F32, float, __bf16>::type type{};
 #pragma unroll
   for (int i = 0; i < SM; ++i) {
     const int64_t m = mw + 32 * i;
@@ -173,9 +175,9 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
 #pragma unroll
       for (int j = 0; j < SN; j += 2) {
         const int64_t c = nw + 16 * j;
-        out(p.c, p.out_f32, p.M, m, c, false, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; });
-        out(p.g, 1, p.M, m, c, true, [&](int e) { return acc[i][j][e]; });
-        out(p.u, 1, p.M, m, c, true, [&](int e) { return acc[i][j + 1][e]; });
+        out(type, p.c, p.M, m, c, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; });
+        out(0.f, p.g, p.M, m, c, [&](int e) { return acc[i][j][e]; });
+        out(0.f, p.u, p.M, m, c, [&](int e) { return acc[i][j + 1][e]; });
       }
     } else {
       // of kind 2 a tile's 32 rows may belong to both halves, where these are not multiples of 32 long
@@ -183,10 +185,10 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
       for (int j = 0; j < SN; ++j) {
         auto value = [&](int e) { return acc[i][j][e]; };
         if constexpr (KIND == 1) {
-          out(p.c, p.out_f32, p.M, m, nw + 32 * j, false, value);
+          out(type, p.c, p.M, m, nw + 32 * j, value);
         } else {
-          if (m < p.half) out(p.c, p.out_f32, p.rows, m, nw + 32 * j, false, value);
-          if (m + 32 > p.half) out(p.c2, p.out_f32, p.rows, m - p.half, nw + 32 * j, false, value);
+          if (m < p.half) out(type, p.c, p.rows, m, nw + 32 * j, value);
+          if (m + 32 > p.half) out(type, p.c2, p.rows, m - p.half, nw + 32 * j, value);
         }
       }
     }
@@ -214,7 +216,7 @@ __device__ __forceinline__ FfCorner corner_of(const FfPlan& w, int64_t tile) {
 // A wave reads its operands of 16 K values ahead of the products of the 16 before; those of a step's
 // first 16 follow the barrier that the step's last products are still to come behind, so that neither
 // the barrier nor LDS makes the matrix unit wait.
-template <int KIND, int TM, int TN, int WM, int WN>
+template <int KIND, int TM, int TN, int WM, int WN, bool F32>
 __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, FfPlan w) {
   constexpr int THREADS = 64 * WM * WN;
   constexpr bool AL = KIND != 2, BL = KIND == 0, MIXED = KIND == 0;
@@ -366,7 +368,7 @@ __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, FfPlan 
 
   if (blockIdx.x < w.full) {
     __syncthreads();
-    ff_store<KIND, TM, TN, WM, WN>(p, acc, m0, n0, smem + wave * (32 * kLine), lane, wave);
+    ff_store<KIND, TM, TN, WM, WN, F32>(p, acc, m0, n0, smem + wave * (32 * kLine), lane, wave);
   } else {
     // a part of a tile's sum, as the lanes hold it
     f32x4* to = reinterpret_cast<f32x4*>(p.part) + ((tile - w.full) * w.share + part) * (int64_t)(TM * TN / 4) + tid;
@@ -380,40 +382,40 @@ __global__ __launch_bounds__(64 * WM * WN) void ff_gemm_kernel(FfGemm p, FfPlan 
   }
 }
 
-// The tiles whose sums are in parts: these in their order, a wave's place in a workgroup of its own.
-template <int KIND, int TM, int TN, int WM, int WN>
+// The tiles whose sums are in parts: these in their order, 32 rows of a wave's place in a workgroup of its own.
+template <int KIND, int TM, int TN, int WM, int WN, bool F32>
 __global__ __launch_bounds__(64) void ff_join_kernel(FfGemm p, FfPlan w) {
   constexpr int WAVES = WM * WN, SM = TM / WM / 32, SN = TN / WN / 32;
   __shared__ __align__(16) char smem[32 * kLine];
-  const int lane = threadIdx.x, wave = blockIdx.x % WAVES;
-  const int64_t tile = blockIdx.x / WAVES;
-  const f32x4* part = reinterpret_cast<const f32x4*>(p.part) + tile * w.share * (int64_t)(TM * TN / 4) + wave * 64 + lane;
-  f32x16 acc[SM][SN];
+  const int lane = threadIdx.x, i = blockIdx.x % SM, wave = blockIdx.x / SM % WAVES;
+  const int64_t tile = blockIdx.x / (SM * WAVES);
+  const f32x4* part = reinterpret_cast<const f32x4*>(p.part) + tile * w.share * (int64_t)(TM * TN / 4) +
+                      i * (SN * 4 * WAVES * 64) + wave * 64 + lane;
+  f32x16 acc[1][SN];
 #pragma unroll
-  for (int i = 0; i < SM; ++i)
-#pragma unroll
-    for (int j = 0; j < SN; ++j) acc[i][j] = zero16();
+  for (int j = 0; j < SN; ++j) acc[0][j] = zero16();
+#pragma unroll 2
   for (int s = 0; s < w.share; ++s, part += TM * TN / 4) {
 #pragma unroll
-    for (int i = 0; i < SM; ++i)
+    for (int j = 0; j < SN; ++j)
 #pragma unroll
-      for (int j = 0; j < SN; ++j)
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 v = part[(j * 4 + e) * (WAVES * 64)];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f32x4 v = part[((i * SN + j) * 4 + e) * (WAVES * 64)];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) acc[i][j][4 * e + q] += v[q];
-        }
+        for (int q = 0; q < 4; ++q) acc[0][j][4 * e + q] += v[q];
+      }
   }
   const FfCorner corner = corner_of<TM, KIND == 0 ? TN / 2 : TN>(w, w.full + tile);
-  ff_store<KIND, TM, TN, WM, WN>(p, acc, corner.m, corner.n, smem, lane, wave);
+  // (as if the tile were 32 rows a wave)
+  const int64_t m0 = corner.m + wave / WN * (TM / WM - 32) + 32 * i;
+  ff_store<KIND, 32 * WM, TN, WM, WN, F32>(p, acc, m0, corner.n, smem, lane, wave);
 }
 
-template <int KIND, int TM, int TN, int WM, int WN>
+template <int KIND, int TM, int TN, int WM, int WN, bool F32>
 hipError_t go(const FfGemm& p, const FfPlan& w, hipStream_t st) {
   constexpr size_t shm = 2 * (size_t)(TM + TN) * kStep * 2;
   static_assert(WM * WN * 32 * kLine <= shm, "a place for each wave");
-  const auto k = ff_gemm_kernel<KIND, TM, TN, WM, WN>;
+  const auto k = ff_gemm_kernel<KIND, TM, TN, WM, WN, F32>;
   if (shm > 65536) {
     const hipError_t r = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shm);
     if (r != hipSuccess) return r;
@@ -421,10 +423,22 @@ hipError_t go(const FfGemm& p, const FfPlan& w, hipStream_t st) {
   const int64_t rest = w.tiles - w.full;
   hipLaunchKernelGGL(k, dim3((unsigned)(w.full + rest * w.share)), dim3(64 * WM * WN), shm, st, p, w);
   if (rest) {
-    const auto j = ff_join_kernel<KIND, TM, TN, WM, WN>;
-    hipLaunchKernelGGL(j, dim3((unsigned)(rest * WM * WN)), dim3(64), 0, st, p, w);
+    const auto j = ff_join_kernel<KIND, TM, TN, WM, WN, F32>;
+    hipLaunchKernelGGL(j, dim3((unsigned)(rest * WM * WN * (TM / WM / 32))), dim3(64), 0, st, p, w);
   }
   return hipGetLastError();
+}
+
+template <bool F32>
+hipError_t pick(const FfGemm& p, const FfPlan& w, hipStream_t st) {
+  if (w.large) {
+    if (p.kind == 0) return go<0, 256, 256, 2, 4, F32>(p, w, st);
+    if (p.kind == 1) return go<1, 256, 256, 2, 4, F32>(p, w, st);
+    return go<2, 256, 256, 2, 4, F32>(p, w, st);
+  }
+  if (p.kind == 0) return go<0, 128, 128, 2, 2, F32>(p, w, st);
+  if (p.kind == 1) return go<1, 128, 128, 2, 2, F32>(p, w, st);
+  return go<2, 128, 128, 2, 2, F32>(p, w, st);
 }
 
 }  // namespace
@@ -477,14 +491,7 @@ FfPlan plan_ff_gemm(int kind, int64_t M, int64_t N, int64_t K, int pairs) {
 
 hipError_t launch_ff_gemm(const FfGemm& p, const FfPlan& w, hipStream_t st) {
   if (p.M == 0 || p.N == 0) return hipSuccess;
-  if (w.large) {
-    if (p.kind == 0) return go<0, 256, 256, 2, 4>(p, w, st);
-    if (p.kind == 1) return go<1, 256, 256, 2, 4>(p, w, st);
-    return go<2, 256, 256, 2, 4>(p, w, st);
-  }
-  if (p.kind == 0) return go<0, 128, 128, 2, 2>(p, w, st);
-  if (p.kind == 1) return go<1, 128, 128, 2, 2>(p, w, st);
-  return go<2, 128, 128, 2, 2>(p, w, st);
+  return p.out_f32 ? pick<true>(p, w, st) : pick<false>(p, w, st);
 }
 
 }  // namespace dla

@@ -326,19 +326,27 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
   }
 }
 
-// dw and dbias from the workgroups' parts: 32 columns a workgroup, 8 threads to a column, in a
-// fixed order, in float64
-__global__ __launch_bounds__(256) void conv_sum_kernel(const float* part, int parts, int C, int W, float* dw, float* db) {
-  __shared__ double sums[8][33];
+// dw and dbias from the workgroups' parts: 32 columns a workgroup, 32 threads to a column, in a fixed order, in
+// float64
+__global__ __launch_bounds__(1024) void conv_sum_kernel(const float* part, int64_t parts, int C, int W, float* dw, float* db) {
+  __shared__ double sums[32][33];
   const int col = threadIdx.x & 31, r = threadIdx.x >> 5;
   const int64_t width = (int64_t)C * (W + 1), at = (int64_t)blockIdx.x * 32 + col;
   double s = 0.;
-  if (at < width)
-    for (int i = r; i < parts; i += 8) s += part[i * width + at];
+  if (at < width) {
+    int64_t i = r;
+    for (; i + 96 < parts; i += 128) {
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = part[(i + 32 * j) * width + at];
+      s += ((double)x[0] + x[1]) + ((double)x[2] + x[3]);
+    }
+    for (; i < parts; i += 32) s += part[i * width + at];
+  }
   sums[r][col] = s;
   __syncthreads();
   if (r == 0 && at < width) {
-    for (int i = 1; i < 8; ++i) s += sums[i][col];
+    for (int i = 1; i < 32; ++i) s += sums[i][col];
     const int c = (int)(at / (W + 1)), j = (int)(at % (W + 1));
     if (j < W) dw[(int64_t)c * W + j] = (float)s;
     else if (db) db[c] = (float)s;
@@ -355,7 +363,8 @@ hipError_t go(const ConvArgs& a, bool backward, float* dw, float* db, hipStream_
     if (grid.x) hipLaunchKernelGGL((conv_backward_kernel<T, W>), grid, block, 0, st, a);
     if (dw && a.C) {
       const int64_t width = (int64_t)a.C * (W + 1);
-      hipLaunchKernelGGL(conv_sum_kernel, dim3((unsigned)((width + 31) / 32)), block, 0, st, a.part, (int)a.groups, a.C, W, dw, db);
+      hipLaunchKernelGGL(conv_sum_kernel, dim3((unsigned)((width + 31) / 32)), dim3(1024), 0, st, a.part,
+                         a.groups, a.C, W, dw, db);
     }
   }
   return hipGetLastError();

@@ -146,7 +146,7 @@ def test_gradient_against_differences():
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_same_bits_streams_and_graph(dtype):
     block = _block()
-    for N, D, F in ((5, 200, 100), (700, 328, 520)):
+    for N, D, F in ((5, 200, 100), (700, 328, 520), (4100, 520, 1544)):
         x, wg, wu, dy = make(N, D, F, dtype)
         ws = torch.empty(block.gated_ff_workspace_bytes(N, D, F, DT[dtype], backward=True), dtype=torch.uint8, device="cuda")
         a = call(block, x, wg, wu, dy, workspace=ws)

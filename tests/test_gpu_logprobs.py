@@ -153,6 +153,23 @@ def test_odd_rows(V):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [5, 600])
+def test_far_from_the_first_logits(dtype, N):
+    """Rows whose first logits say nothing of the others: shut out, far below, far above."""
+    block = _block()
+    l, tok, dlp, dent, dlse = make(N, 20000, dtype)
+    l[0, :9000] = -INF
+    l[0, 9000:] -= 300
+    l[1, :9000] -= 100
+    l[2, 9000:] -= 100
+    l[3, :] = -INF
+    l[3, 19999] = -50.0
+    l[4, 9000:] = -INF
+    out = check_forward(block, l, tok, 20)
+    check_backward(block, l, tok, *out, dlp, dent, dlse, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [2000, 50000, 100000])
 def test_many_reach_the_bound(dtype, V):
     """Rising logits, whose largest all lie with few threads, and one value over and over."""

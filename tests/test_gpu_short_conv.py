@@ -146,6 +146,27 @@ def test_long_runs(dtype):
         check(run(block, s, True), s, True, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_runs_than_workgroups(dtype):
+    """So many sequences that a workgroup of the backward pass takes several; without a state or documents the
+    formula is a sum over shifted arrays."""
+    block = _block()
+    B, T, C, W = 300000, 2, 8, 3
+    s = make(B, T, C, W, dtype)
+    out, _ = block.short_conv(s["x"], s["w"], activation=None)
+    dx, dw, _, _ = block.short_conv_backward(s["x"], s["w"], s["dy"], activation=None)
+    x, w, dy = (s[k].double() for k in ("x", "w", "dy"))
+    off = lambda mag: 2 * W * U * mag + HALF[dtype] * 1.001 * mag + 2.0 ** -126  # noqa: E731
+    z = x * w[:, 2] + torch.nn.functional.pad(x, (0, 0, 1, 0))[:, :T] * w[:, 1]
+    mag = (x * w[:, 2]).abs() + (torch.nn.functional.pad(x, (0, 0, 1, 0))[:, :T] * w[:, 1]).abs()
+    assert ((out.double() - z).abs() <= off(mag)).all()
+    next_ = torch.nn.functional.pad(dy, (0, 0, 0, 1))[:, 1:]
+    assert ((dx.double() - dy * w[:, 2] - next_ * w[:, 1]).abs() <= off((dy * w[:, 2]).abs() + (next_ * w[:, 1]).abs())).all()
+    want = torch.stack([torch.zeros(C, dtype=torch.float64, device="cuda"), (dy[:, 1] * x[:, 0]).sum(0), (dy * x).sum((0, 1))], 1)
+    # a thread adds up few terms in float32, the rest is float64: 64 2^-24 of the terms' magnitudes
+    assert ((dw.double() - want).abs() <= 64 * U * (dy.abs().sum((0, 1)) * x.abs().max())[:, None]).all()
+
+
 def test_strides_and_slices():
     """Slices of a wider projection at any element, transposed and broadcast sequences."""
     block = _block()
