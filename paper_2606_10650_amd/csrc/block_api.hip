@@ -201,7 +201,8 @@ struct FfSpace {
 FfSpace space_of(const dla_ff_desc& d, bool backward, bool direct) {
   FfSpace s;
   memset(&s, 0, sizeof(s));
-  if (d.rows == 0) s.dw = plan_ff_gemm(2, 2 * (int64_t)round_up(d.F, 8), d.D, 0, 1);
+  const int planes = d.dtype == DLA_BF16 ? 1 : 3;
+  if (d.rows == 0) s.dw = plan_ff_gemm(2, 2 * (int64_t)round_up(d.F, 8), d.D, 0, planes == 1 ? 1 : 6);
   if (d.rows == 0 || (!backward && d.rows <= kFfStepRows)) return s;
   size_t used = 0;
   auto take = [&](size_t bytes) {
@@ -209,7 +210,6 @@ FfSpace space_of(const dla_ff_desc& d, bool backward, bool direct) {
     used = round_up(used + bytes, 256);
     return x;
   };
-  const int planes = d.dtype == DLA_BF16 ? 1 : 3;
   const size_t Dp = round_up(d.D, 8), Fp = round_up(d.F, 8);
   if (!direct) {
     s.x = take(planes * d.rows * Dp * 2);

@@ -491,6 +491,8 @@ FfPlan plan_ff_gemm(int kind, int64_t M, int64_t N, int64_t K, int pairs) {
 
 hipError_t launch_ff_gemm(const FfGemm& p, const FfPlan& w, hipStream_t st) {
   if (p.M == 0 || p.N == 0) return hipSuccess;
+  // the plan is for as many pairs, each with whole steps: the kernel divides by the steps of one
+  if (p.pairs < 1 || w.steps < p.pairs || w.steps % p.pairs) return hipErrorInvalidValue;
   return p.out_f32 ? pick<true>(p, w, st) : pick<false>(p, w, st);
 }
 

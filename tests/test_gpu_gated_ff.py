@@ -177,9 +177,14 @@ def test_float32_range():
     check(call(block, x * s, wg / s, wu / s, dy), x * s, wg / s, wu / s, dy, "f32")
 
 
-def test_empty():
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,F", [(16, 24), (1, 1), (300, 521), (4096, 2100)])
+def test_empty(D, F, dtype):
+    """No rows: weight gradients of zeros, also where their memory held something else."""
     block = _block()
-    for dtype in ("bf16", "f32"):
-        x, wg, wu, dy = make(0, 16, 24, dtype)
-        y, parts, dx, dwg, dwu = call(block, x, wg, wu, dy)
-        assert y.shape == (0, 24) and dx.shape == (0, 16) and not dwg.any() and not dwu.any()
+    x, wg, wu, dy = make(0, D, F, dtype)
+    torch.full((2, F, D), float("nan"), dtype=DT[dtype], device="cuda")
+    y, parts, dx, dwg, dwu = call(block, x, wg, wu, dy)
+    assert y.shape == (0, F) and dx.shape == (0, D) and parts.shape == (2, 0, F)
+    for t in (dwg, dwu):
+        assert torch.equal(t, torch.zeros_like(t))
