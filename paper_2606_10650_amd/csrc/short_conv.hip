@@ -135,6 +135,10 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a) {
   if (p.t0 < len || p.t0 == 0) win.before(a, p.b, p.t0, p.c, n);
   for (int t = p.t0; t < end; t += G) {
     Raw raw[G];
+    uint8_t first[G] = {};
+    if (starts)
+#pragma unroll
+      for (int g = 0; g < G; ++g) first[g] = starts[min(t + g, end - 1)];
 #pragma unroll
     for (int g = 0; g < G; ++g) raw[g] = Piece<T>::raw(x + min(t + g, end - 1) * a.x.st, n);
 #pragma unroll
@@ -143,7 +147,7 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a) {
         float v[N], z[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = Piece<T>::value(raw[g], i);
-        if (starts && starts[t + g]) win.clear();
+        if (first[g]) win.clear();
         convolve<T, W>(k, win, v, z);
         win.push(v);
         if (a.silu) {
@@ -213,7 +217,11 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
     const int last = min(min(p.t1, a.T - (W - 1)) + W - 1, len);   // t1 + W - 1 without leaving int32
     // groups of tokens, the next group's on its way; behind the last token the last one again
     Raw rx[G], rd[G];
+    uint8_t rs[G] = {};
     auto fetch = [&](int t) {
+      if (starts)
+#pragma unroll
+        for (int g = 0; g < G; ++g) rs[g] = starts[min(t + g, last - 1)];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const int64_t q = min(t + g, last - 1);
@@ -224,10 +232,12 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
     if (p.t0 < last) fetch(p.t0);
     for (int t = p.t0; t < last; t += G) {
       Raw cx[G], cd[G];
+      uint8_t first[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         cx[g] = rx[g];
         cd[g] = rd[g];
+        first[g] = rs[g];
       }
       if (t + G < last) fetch(t + G);
 #pragma unroll
@@ -239,7 +249,7 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
             v[i] = Piece<T>::value(cx[g], i);
             d[i] = Piece<T>::value(cd[g], i);
           }
-          if (starts && starts[t + g]) {
+          if (first[g]) {
             win.clear();
             age = 0;
           }
