@@ -7,10 +7,14 @@
 // backward pass forms z again and carries the W - 1 gradients that are not yet whole; behind its
 // run it reads W - 1 tokens more.
 //
-// Bytes bound the forward pass (4 x 16384 tokens of 6144 bfloat16 channels: 1.6 GB in 370 us, 4.4 TB/s); the
-// backward pass (2.4 GB in 630 us, 3.8 TB/s) its arithmetic as well: 37 vector operations a value, and
-// registers for two waves a SIMD.  Channels by fours, for twice the waves, took 760 us; loads a token
-// ahead in place of a group 710.
+// Bytes bound both passes: 4 x 16384 tokens of 6144 bfloat16 channels, forward 1.6 GB and backward 2.4 GB, take
+// 852 us together, 4.7 TB/s of the 5.1 that a copy reaches.  So that the next group of tokens is on its way while
+// one is worked on, all that it needs comes with it, the starts of documents too (read token by token, each
+// waited for behind the loads of the next group: 1024 us), and backward a group inside its run and its
+// document goes without the checks of the others (both 872).  The backward pass has registers for two waves a
+// SIMD; channels by fours, for twice the waves, took a fifth longer.
+#include <type_traits>
+
 #include "piece.h"
 #include "short_conv.h"
 
@@ -133,14 +137,26 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a) {
   Window<T, W> win;
   // (a run behind the sequence's end has nothing before it, and must not read the state)
   if (p.t0 < len || p.t0 == 0) win.before(a, p.b, p.t0, p.c, n);
-  for (int t = p.t0; t < end; t += G) {
-    Raw raw[G];
-    uint8_t first[G] = {};
+  // groups of tokens, the next group's on its way; behind the last token the last one again
+  Raw next[G];
+  uint8_t start[G] = {};
+  auto fetch = [&](int t) {
     if (starts)
 #pragma unroll
-      for (int g = 0; g < G; ++g) first[g] = starts[min(t + g, end - 1)];
+      for (int g = 0; g < G; ++g) start[g] = starts[min(t + g, end - 1)];
 #pragma unroll
-    for (int g = 0; g < G; ++g) raw[g] = Piece<T>::raw(x + min(t + g, end - 1) * a.x.st, n);
+    for (int g = 0; g < G; ++g) next[g] = Piece<T>::raw(x + min(t + g, end - 1) * a.x.st, n);
+  };
+  if (p.t0 < end) fetch(p.t0);
+  for (int t = p.t0; t < end; t += G) {
+    Raw raw[G];
+    uint8_t first[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      raw[g] = next[g];
+      first[g] = start[g];
+    }
+    if (t + G < end) fetch(t + G);
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       if (t + g < end) {
@@ -215,6 +231,56 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
       else if (q < 0 && p.t0 == 0 && ds) Piece<T>::store(ds + (int64_t)(W - 1 + q) * a.C, n, v);
     };
     const int last = min(min(p.t1, a.T - (W - 1)) + W - 1, len);   // t1 + W - 1 without leaving int32
+    // WHOLE: the run's own token, all inputs that it sees of its document and of the run
+    auto token = [&](int t, const Raw& rawx, const Raw& rawd, bool first, auto kind) {
+      constexpr bool WHOLE = decltype(kind)::value;
+      float v[N], z[N], d[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        v[i] = Piece<T>::value(rawx, i);
+        d[i] = Piece<T>::value(rawd, i);
+      }
+      if (!WHOLE && first) {
+        win.clear();
+        age = 0;
+      }
+      if (a.silu) {
+        convolve<T, W>(k, win, v, z);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float s = sigmoid(z[i]);
+          d[i] *= s * (1.f + z[i] * (1.f - s));
+        }
+      }
+      if (WHOLE || t < p.t1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          dw[W][i] += d[i];
+          dw[W - 1][i] += d[i] * v[i];
+#pragma unroll
+          for (int j = 0; j < W - 1; ++j) dw[j][i] += d[i] * win.x[j][i];
+        }
+      }
+      win.push(v);
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+        if (WHOLE || W - 1 - j <= age) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) pend[j][i] += k.w[j][i] * d[i];
+        }
+      if constexpr (WHOLE) {
+        Piece<T>::store(dx + (int64_t)(t - (W - 1)) * a.dx.st, N, pend[0]);
+      } else {
+        age = min(age + 1, W - 1);
+        put(t - (W - 1), pend[0]);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j) pend[j][i] = pend[j + 1][i];
+        pend[W - 2][i] = k.w[W - 1][i] * d[i];
+      }
+    };
     // groups of tokens, the next group's on its way; behind the last token the last one again
     Raw rx[G], rd[G];
     uint8_t rs[G] = {};
@@ -240,52 +306,17 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
         first[g] = rs[g];
       }
       if (t + G < last) fetch(t + G);
+      bool whole = n >= N && age == W - 1 && t - (W - 1) >= p.t0 && t + G <= last && t + G <= p.t1;
 #pragma unroll
-      for (int g = 0; g < G; ++g)
-        if (t + g < last) {
-          float v[N], z[N], d[N];
+      for (int g = 0; g < G; ++g) whole = whole && !first[g];
+      if (whole) {
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            v[i] = Piece<T>::value(cx[g], i);
-            d[i] = Piece<T>::value(cd[g], i);
-          }
-          if (first[g]) {
-            win.clear();
-            age = 0;
-          }
-          if (a.silu) {
-            convolve<T, W>(k, win, v, z);
+        for (int g = 0; g < G; ++g) token(t + g, cx[g], cd[g], false, std::true_type());
+      } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-              const float s = sigmoid(z[i]);
-              d[i] *= s * (1.f + z[i] * (1.f - s));
-            }
-          }
-          if (t + g < p.t1) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-              dw[W][i] += d[i];
-              dw[W - 1][i] += d[i] * v[i];
-#pragma unroll
-              for (int j = 0; j < W - 1; ++j) dw[j][i] += d[i] * win.x[j][i];
-            }
-          }
-          win.push(v);
-#pragma unroll
-          for (int j = 0; j < W - 1; ++j)
-            if (W - 1 - j <= age) {
-#pragma unroll
-              for (int i = 0; i < N; ++i) pend[j][i] += k.w[j][i] * d[i];
-            }
-          age = min(age + 1, W - 1);
-          put(t + g - (W - 1), pend[0]);
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-#pragma unroll
-            for (int j = 0; j + 1 < W - 1; ++j) pend[j][i] = pend[j + 1][i];
-            pend[W - 2][i] = k.w[W - 1][i] * d[i];
-          }
-        }
+        for (int g = 0; g < G; ++g)
+          if (t + g < last) token(t + g, cx[g], cd[g], first[g], std::false_type());
+      }
     }
     const int t = max(p.t0, last);   // the token behind those that were looked at
     if (p.t0 <= len) {
@@ -393,8 +424,8 @@ hipError_t pick(const ConvArgs& a, int dtype, bool backward, float* dw, float* d
 
 }  // namespace
 
-// Runs.  4 x 16384 tokens of 6144 bfloat16 channels, backward: 504 workgroups 630 us, 516 (four more than there
-// is room for) 1030; twice as many 670.
+// Runs.  4 x 16384 tokens of 6144 bfloat16 channels, backward: 504 workgroups, all there at once; 516, four more
+// than there is room for, took 1.6 times as long, twice as many, each half as long, 1.06 times.
 void plan_conv(ConvArgs& a, int dtype, bool backward) {
   const int N = dtype == DLA_BF16 ? 8 : 4;
   a.pieces = (int)(((int64_t)a.C + N - 1) / N);
