@@ -72,8 +72,13 @@ struct Piece {
 template <typename T>
 __device__ __forceinline__ void load_floats(const void* p, int f32, int64_t i, int n, float (&x)[Piece<T>::N]) {
   if (sizeof(T) == 4 || f32) {
+    using P = Piece<float>;
 #pragma unroll
-    for (int j = 0; j < Piece<T>::N; ++j) x[j] = j < n ? static_cast<const float*>(p)[i + j] : 0.f;
+    for (int q = 0; q < Piece<T>::N; q += P::N) {
+      const P::Raw r = P::raw(static_cast<const float*>(p) + i + q, n - q);
+#pragma unroll
+      for (int j = 0; j < P::N; ++j) x[q + j] = P::value(r, j);
+    }
   } else {
     Piece<T>::load(static_cast<const T*>(p) + i, n, x);
   }

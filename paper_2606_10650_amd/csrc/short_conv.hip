@@ -8,11 +8,12 @@
 // run it reads W - 1 tokens more.
 //
 // Bytes bound both passes: 4 x 16384 tokens of 6144 bfloat16 channels, forward 1.6 GB and backward 2.4 GB, take
-// 852 us together, 4.7 TB/s of the 5.1 that a copy reaches.  So that the next group of tokens is on its way while
+// 830 us together, 4.9 TB/s of the 5.1 that a copy reaches.  So that the next group of tokens is on its way while
 // one is worked on, all that it needs comes with it, the starts of documents too (read token by token, each
 // waited for behind the loads of the next group: 1024 us), and backward a group inside its run and its
-// document goes without the checks of the others (both 872).  The backward pass has registers for two waves a
-// SIMD; channels by fours, for twice the waves, took a fifth longer.
+// document goes without the checks of the others (872).  A run's taps come by whole pieces (one by one 850;
+// one token of 64 sequences 5.4 us, one by one 8.4).  The backward pass has registers for two waves a SIMD;
+// channels by fours, for twice the waves, took a fifth longer.
 #include <type_traits>
 
 #include "piece.h"
@@ -38,16 +39,25 @@ struct Taps {
   static constexpr int N = Piece<T>::N;
   float w[W][N], bias[N];
   __device__ __forceinline__ void load(const ConvArgs& a, int c, int n) {
+    if (a.w_f32) load_as<float>(a, c, n);
+    else load_as<T>(a, c, n);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-#pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const int64_t at = (int64_t)(c + i) * W + j;
-        w[j][i] = i >= n ? 0.f : a.w_f32 ? static_cast<const float*>(a.w)[at] : to_f32(static_cast<const T*>(a.w)[at]);
-      }
-      bias[i] = 0.f;
-    }
+    for (int i = 0; i < N; ++i) bias[i] = 0.f;
     if (a.bias) load_floats<T>(a.bias, a.w_f32, c, n, bias);
+  }
+  // the channels' taps lie one after the other, and come by pieces of 16 bytes
+  template <typename S>
+  __device__ __forceinline__ void load_as(const ConvArgs& a, int c, int n) {
+    using P = Piece<S>;
+    const S* from = static_cast<const S*>(a.w) + (int64_t)c * W;
+    const int all = min(n, N) * W;
+    typename P::Raw raw[N * W / P::N];
+#pragma unroll
+    for (int q = 0; q < N * W / P::N; ++q) raw[q] = P::raw(from + q * P::N, all - q * P::N);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) w[j][i] = P::value(raw[(i * W + j) / P::N], (i * W + j) % P::N);
   }
 };
 
@@ -70,22 +80,41 @@ struct Window {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[W - 2][i] = v[i];
   }
-  // what token t of sequence b sees before its own start is looked at
-  __device__ __forceinline__ void before(const ConvArgs& a, int b, int t, int c, int n) {
-    clear();
-    float v[N];
+  // What token t of sequence b sees before its own start is looked at: asked for, all of it before any is waited
+  // for, and taken.
+  struct Before {
+    typename Piece<T>::Raw raw[W - 1];
+    uint8_t start[W - 1];
+    __device__ __forceinline__ void fetch(const ConvArgs& a, int b, int t, int c, int n) {
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) {
-      const int p = t - (W - 1) + j;
-      if (p >= 0) {
-        if (a.starts && a.starts[(int64_t)b * a.T + p]) clear();
-        Piece<T>::load(static_cast<const T*>(a.x.p) + b * a.x.sb + p * a.x.st + c, n, v);
-        push(v);
-      } else if (a.state) {
-        Piece<T>::load(static_cast<const T*>(a.state) + ((int64_t)b * (W - 1) + W - 1 + p) * a.C + c, n, v);
-        push(v);
+      for (int j = 0; j < W - 1; ++j) {
+        const int p = t - (W - 1) + j;
+        const T* from = p >= 0 ? static_cast<const T*>(a.x.p) + b * a.x.sb + p * a.x.st + c
+                        : a.state ? static_cast<const T*>(a.state) + ((int64_t)b * (W - 1) + W - 1 + p) * a.C + c
+                                  : nullptr;
+        raw[j] = {};
+        if (from) raw[j] = Piece<T>::raw(from, n);
+        start[j] = 0;
+        if (p >= 0 && a.starts) start[j] = a.starts[(int64_t)b * a.T + p];
       }
     }
+  };
+  // Returns how many inputs before t its document has (W - 1: all there are room for).
+  __device__ __forceinline__ int take(const Before& o) {
+    clear();
+    int age = W - 1;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+      if (o.start[j]) {
+        clear();
+        age = W - 1 - j;
+      }
+      float v[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = Piece<T>::value(o.raw[j], i);
+      push(v);
+    }
+    return age;
   }
 };
 
@@ -132,11 +161,6 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a) {
   const T* x = static_cast<const T*>(a.x.p) + p.b * a.x.sb + p.c;
   T* y = static_cast<T*>(a.y.p) + p.b * a.y.sb + p.c;
   const uint8_t* starts = a.starts ? a.starts + (int64_t)p.b * a.T : nullptr;
-  Taps<T, W> k;
-  k.load(a, p.c, n);
-  Window<T, W> win;
-  // (a run behind the sequence's end has nothing before it, and must not read the state)
-  if (p.t0 < len || p.t0 == 0) win.before(a, p.b, p.t0, p.c, n);
   // groups of tokens, the next group's on its way; behind the last token the last one again
   Raw next[G];
   uint8_t start[G] = {};
@@ -147,7 +171,15 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a) {
 #pragma unroll
     for (int g = 0; g < G; ++g) next[g] = Piece<T>::raw(x + min(t + g, end - 1) * a.x.st, n);
   };
+  // all that the first token needs is asked for before any is waited for
+  Window<T, W> win;
+  typename Window<T, W>::Before before = {};
+  // (a run behind the sequence's end has nothing before it, and must not read the state)
+  if (p.t0 < len || p.t0 == 0) before.fetch(a, p.b, p.t0, p.c, n);
   if (p.t0 < end) fetch(p.t0);
+  Taps<T, W> k;
+  k.load(a, p.c, n);
+  win.take(before);
   for (int t = p.t0; t < end; t += G) {
     Raw raw[G];
     uint8_t first[G];
@@ -180,7 +212,10 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a) {
   }
   // the first run's thread alone has read the given state, and writes the last one over it
   if (a.state_out && p.t0 == 0) {
-    if (len > end) win.before(a, p.b, len, p.c, n);
+    if (len > end) {
+      before.fetch(a, p.b, len, p.c, n);
+      win.take(before);
+    }
     T* s = static_cast<T*>(a.state_out) + (int64_t)p.b * (W - 1) * a.C + p.c;
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) Piece<T>::store(s + (int64_t)j * a.C, n, win.x[j]);
@@ -209,21 +244,14 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
     T* dx = static_cast<T*>(a.dx.p) + p.b * a.dx.sb + p.c;
     const uint8_t* starts = a.starts ? a.starts + (int64_t)p.b * a.T : nullptr;
     Window<T, W> win;
-    win.before(a, p.b, min(p.t0, len), p.c, n);
+    typename Window<T, W>::Before before;
+    before.fetch(a, p.b, min(p.t0, len), p.c, n);
+    int age;
     float pend[W - 1][N];   // gradients of the W - 1 inputs before, the latest last
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
 #pragma unroll
       for (int i = 0; i < N; ++i) pend[j][i] = 0.f;
-    // Inputs before a token that its document has (W - 1: all there are room for).  Those of
-    // before the run have their gradients from the run before, but for the state's.
-    int age = W - 1;
-    if (starts)
-      for (int i = 0; i < W - 1; ++i)
-        if (p.t0 - 1 - i >= 0 && p.t0 <= len && starts[p.t0 - 1 - i]) {
-          age = i + 1;
-          break;
-        }
     T* ds = a.dstate ? static_cast<T*>(a.dstate) + (int64_t)p.b * (W - 1) * a.C + p.c : nullptr;
     // the gradient of input q of the sequence is whole
     auto put = [&](int q, const float(&v)[N]) {
@@ -296,6 +324,8 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
       }
     };
     if (p.t0 < last) fetch(p.t0);
+    // (inputs of before the run have their gradients from the run before, but for the state's)
+    age = win.take(before);
     for (int t = p.t0; t < last; t += G) {
       Raw cx[G], cd[G];
       uint8_t first[G];
@@ -359,11 +389,14 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a) {
   const int piece = (int)(blockIdx.x % cols) * a.lanes + lane;
   if (threadIdx.x < (unsigned)a.lanes && piece < a.pieces) {
     float* part = a.part + ((int64_t)(blockIdx.x / cols) * a.C + piece * N) * (W + 1);
+    const int all = min(n, N) * (W + 1);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < n)
+    for (int q = 0; q < N * (W + 1); q += 4) {
+      float v[4];
 #pragma unroll
-        for (int j = 0; j <= W; ++j) part[i * (W + 1) + j] = dw[j][i];
+      for (int e = 0; e < 4; ++e) v[e] = dw[(q + e) % (W + 1)][(q + e) / (W + 1)];
+      Piece<float>::store(part + q, all - q, v);
+    }
   }
 }
 
