@@ -38,7 +38,7 @@ hipError_t launch_ff_parts(int64_t rows, int F, int dtype, FfRows g, FfRows u, F
 //   kind 1: C = sum over pairs of A B, A [M][K], B [K][N]
 //   kind 2: C = sum over pairs of A^T B, A [K][M], B [K][N]
 // A pair names a plane of A and one of B.
-constexpr int kFfPairs = 12, kFfPlanes = 6;
+constexpr int kFfPlanes = 6;
 struct FfGemm {
   int kind, out_f32, pairs;
   int64_t M, N, K;

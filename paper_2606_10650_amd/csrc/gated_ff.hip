@@ -116,7 +116,6 @@ __device__ __forceinline__ void terms(float v, __bf16 (&t)[3]) {
   t[2] = (__bf16)(rest - (float)t[1]);
 }
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 // A piece of values to the planes.
 template <typename T, int N>

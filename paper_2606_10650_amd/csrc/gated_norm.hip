@@ -8,6 +8,10 @@
 // and goes along the rows with their sums in registers; a workgroup leaves one part of each, and
 // a second kernel adds the parts in a fixed order.  h is not read back in the backward pass but
 // formed again from x, gate and residual, so that nothing depends on how h was rounded.
+//
+// 65536 rows of 16 heads of 128 bfloat16 values with gate, forward 0.8 GB in 165 us, 4.9 TB/s, backward 1.3 GB in
+// 258, 5.2; 16384 rows of 2048 with residual and next norm, 0.27 GB in 60 to 70 and 0.4 GB in 100, 4.0.  64 such
+// rows take 5.4 us, nearly all of it waiting for two loads and two sums.
 #include "gated_norm.h"
 #include "piece.h"
 
@@ -162,7 +166,7 @@ __device__ __forceinline__ void gather(float (&s)[N], int sub, int stride, int s
 }
 
 // Waves a SIMD of the backward pass.  With gate and next norm a thread of 8 values needs more than a fourth of the
-// registers (65536 x 2048 bfloat16: within a fourth 683 us, within a third 4TIME).
+// registers (65536 x 2048 bfloat16: within a fourth 683 us, within a third 457).
 template <typename T>
 __host__ __device__ constexpr int waves_of(int nt, bool both) {
   return sizeof(T) == 2 && both && nt <= 256 ? 3 : 4;
