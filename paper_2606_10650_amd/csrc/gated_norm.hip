@@ -10,8 +10,8 @@
 // formed again from x, gate and residual, so that nothing depends on how h was rounded.
 //
 // 65536 rows of 16 heads of 128 bfloat16 values with gate, forward 0.8 GB in 165 us, 4.9 TB/s, backward 1.3 GB in
-// 258, 5.2; 16384 rows of 2048 with residual and next norm, 0.27 GB in 60 to 70 and 0.4 GB in 100, 4.0.  64 such
-// rows take 5.4 us, nearly all of it waiting for two loads and two sums.
+// 258, 5.2; 16384 rows of 2048 with residual and next norm, 0.27 GB in 61, 4.4, and 0.4 GB in 94, 4.3.  64 such rows
+// take 5.4 us, nearly all of it waiting for two loads and two sums.
 #include "gated_norm.h"
 #include "piece.h"
 
@@ -294,12 +294,20 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256, waves_of<T>(NT, GATE && NEXT))
   }
 }
 
-// dw[c] = the sum of the parts' column c: 32 columns a workgroup, 32 threads to a column, in a
-// fixed order, in float64
-__global__ __launch_bounds__(1024) void part_sum_kernel(const float* part, int64_t parts, int64_t width, float* dw) {
+// dw[c] = the sum of the parts' column c, of up to two weights: 32 columns a workgroup, 32 threads to a column,
+// in a fixed order, in float64
+struct PartSum {
+  const float* part;
+  int64_t parts, width;
+  float* dw;
+};
+__global__ __launch_bounds__(1024) void part_sum_kernel(PartSum p0, PartSum p1, unsigned blocks0) {
   __shared__ double sums[32][33];
+  const bool second = blockIdx.x >= blocks0;
+  const float* part = second ? p1.part : p0.part;
+  const int64_t parts = second ? p1.parts : p0.parts, width = second ? p1.width : p0.width;
   const int col = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int64_t c = (int64_t)blockIdx.x * 32 + col;
+  const int64_t c = (int64_t)(second ? blockIdx.x - blocks0 : blockIdx.x) * 32 + col;
   double s = 0.;
   if (c < width) {
     int64_t i = r;
@@ -315,7 +323,7 @@ __global__ __launch_bounds__(1024) void part_sum_kernel(const float* part, int64
   __syncthreads();
   if (r == 0 && c < width) {
     for (int i = 1; i < 32; ++i) s += sums[i][col];
-    dw[c] = (float)s;
+    (second ? p1.dw : p0.dw)[c] = (float)s;
   }
 }
 
@@ -339,24 +347,23 @@ hipError_t backward(const GatedNormArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Threads that share a group of so many pieces.  As few lanes as hold it with one piece each, up to a wave.
-// Past that the forward pass goes by waves of up to 4 pieces a lane where there are groups enough to
-// fill the chip, else by 256 threads, or 1024; the backward pass, with seven rows' pieces at hand, by one
-// piece a thread (16384 x 2048 bfloat16 with a next norm: by waves 230 us).
-int threads_of(int64_t total, int pieces, bool back) {
+// Threads that share a group of so many pieces: as few lanes as hold it with one piece each, up to a wave.  Past
+// that the forward pass takes 2 pieces a lane of a wave (with residual and next norm, 32768 x 700 bfloat16
+// 55 us; one piece of 128 threads 72), then a workgroup with up to 4 pieces a thread (16384 x 2048: 61; a wave with 4
+// pieces a lane 67); the backward pass, with seven rows' pieces at hand, one piece a thread (95; by waves 230).
+int threads_of(int pieces, bool back) {
   if (pieces <= 64) {
     int nt = 8;
     while (nt < pieces) nt *= 2;
     return nt;
   }
   if (back) return pieces <= 128 ? 128 : pieces <= 256 ? 256 : pieces <= 512 ? 512 : 1024;
-  if (pieces <= 256 && total >= 1024) return 64;
-  return pieces <= 1024 ? 256 : 1024;
+  return pieces <= 128 ? 64 : pieces <= 1024 ? 256 : 1024;
 }
 
 template <typename T>
 hipError_t pick(const GatedNormArgs& a, bool back, hipStream_t st) {
-  const int pieces = (a.D + Piece<T>::N - 1) / Piece<T>::N, nt = threads_of(a.rows * a.G, pieces, back);
+  const int pieces = (a.D + Piece<T>::N - 1) / Piece<T>::N, nt = threads_of(pieces, back);
   if (back) {
     switch (nt) {
       case 8: return backward<T, 8, 1>(a, st);
@@ -378,8 +385,7 @@ hipError_t pick(const GatedNormArgs& a, bool back, hipStream_t st) {
     case 32: return forward<T, 32, 1>(a, st);
     case 64:
       if (pieces <= 64) return forward<T, 64, 1>(a, st);
-      if (pieces <= 128) return forward<T, 64, 2>(a, st);
-      return forward<T, 64, 4>(a, st);
+      return forward<T, 64, 2>(a, st);
     case 256:
       if (pieces <= 256) return forward<T, 256, 1>(a, st);
       if (pieces <= 512) return forward<T, 256, 2>(a, st);
@@ -393,7 +399,7 @@ hipError_t pick(const GatedNormArgs& a, bool back, hipStream_t st) {
 }  // namespace
 
 void plan_gated_norm(GatedNormArgs& a, int dtype, bool backward) {
-  const int N = dtype == DLA_BF16 ? 8 : 4, pieces = (a.D + N - 1) / N, nt = threads_of(a.rows * a.G, pieces, backward);
+  const int N = dtype == DLA_BF16 ? 8 : 4, pieces = (a.D + N - 1) / N, nt = threads_of(pieces, backward);
   const int per = nt > 256 ? 1 : 256 / nt, side = a.G < per ? a.G : per, along = per / side;
   a.gcols = (a.G + per - 1) / per;
   a.groups = (a.rows + along - 1) / along;
@@ -415,13 +421,10 @@ hipError_t launch_gated_norm(const GatedNormArgs& a, int dtype, bool backward, h
 }
 
 hipError_t launch_gated_norm_dw(const GatedNormArgs& a, float* dw, float* dw2, hipStream_t st) {
-  if (dw) {
-    const int64_t width = a.per_group ? (int64_t)a.G * a.D : a.D, parts = a.rows ? gated_norm_dw_parts(a) : 0;
-    hipLaunchKernelGGL(part_sum_kernel, dim3((unsigned)((width + 31) / 32)), dim3(1024), 0, st, a.dw_part, parts, width, dw);
-  }
-  if (dw2)
-    hipLaunchKernelGGL(part_sum_kernel, dim3((unsigned)((a.D + 31) / 32)), dim3(1024), 0, st, a.dw2_part,
-                       a.rows ? a.groups * a.gcols : (int64_t)0, (int64_t)a.D, dw2);
+  const PartSum p0{a.dw_part, a.rows ? gated_norm_dw_parts(a) : 0, a.per_group ? (int64_t)a.G * a.D : a.D, dw};
+  const PartSum p1{a.dw2_part, a.rows ? a.groups * a.gcols : 0, a.D, dw2};
+  const unsigned blocks0 = dw ? (unsigned)((p0.width + 31) / 32) : 0, blocks1 = dw2 ? (unsigned)((p1.width + 31) / 32) : 0;
+  hipLaunchKernelGGL(part_sum_kernel, dim3(blocks0 + blocks1), dim3(1024), 0, st, p0, p1, blocks0);
   return hipGetLastError();
 }
 
