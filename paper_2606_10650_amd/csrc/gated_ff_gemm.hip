@@ -8,8 +8,9 @@
 // units exchanged by the row modulo 4, and is transposed by the reads of 4 rows of 16 columns.
 // What lies outside an operand is zero.
 //
-// What a compute unit gets from its die's cache, some 20 bytes a clock, bounds the products together with
-// the matrix units.  16384 rows, 2048 to 5504, bfloat16: forward (both projections) 715 us, 1030 TFLOP/s, dx
+// What bounds the products is the clock that the card's power allows (1.3 to 1.5 GHz on one card, at which the matrix
+// units are busy for 59, 75 and 68% of the cycles, forward, dx and dW), then what a compute unit gets from its
+// die's cache, some 20 bytes a clock.  16384 rows, 2048 to 5504, bfloat16: forward (both projections) 715 us, 1030 TFLOP/s, dx
 // 610, 1210, both dW 695, 1060; a large library product reaches 1380, of these shapes 1085, 1144 and 738.  Copies
 // straight from memory into LDS got in the way of its reads (dx 790 us); tiles asked for further ahead changed
 // nothing; tiles' sums shared unevenly, so that every unit has the same work, lost the operands that

@@ -546,7 +546,7 @@ hipError_t back(const LogprobArgs& a, hipStream_t st) {
 
 // Few rows are cut into parts that a workgroup holds in registers, at most 64, which is what a wave joins (with
 // alternatives, at most 1024 of these a row).  64 rows of 50304 bfloat16 with 20 alternatives
-// take 19 us so, 26 in parts twice as long.
+// take 18 us so, 26 in parts twice as long.
 void plan_logprobs(LogprobArgs& a, int dtype) {
   const int group = 2 * 256 * (dtype == DLA_BF16 ? 8 : 4);
   int64_t parts = a.rows < 512 ? (1024 + a.rows) / (a.rows + 1) : 1;
