@@ -422,7 +422,8 @@ hipError_t launch_gated_norm(const GatedNormArgs& a, int dtype, bool backward, h
 
 hipError_t launch_gated_norm_dw(const GatedNormArgs& a, float* dw, float* dw2, hipStream_t st) {
   const PartSum p0{a.dw_part, a.rows ? gated_norm_dw_parts(a) : 0, a.per_group ? (int64_t)a.G * a.D : a.D, dw};
-  const PartSum p1{a.dw2_part, a.rows ? a.groups * a.gcols : 0, a.D, dw2};
+  // (the kernel leaves parts of the next norm's weight where it goes through that norm)
+  const PartSum p1{a.dw2_part, a.rows && a.y.p ? a.groups * a.gcols : 0, a.D, dw2};
   const unsigned blocks0 = dw ? (unsigned)((p0.width + 31) / 32) : 0, blocks1 = dw2 ? (unsigned)((p1.width + 31) / 32) : 0;
   hipLaunchKernelGGL(part_sum_kernel, dim3(blocks0 + blocks1), dim3(1024), 0, st, p0, p1, blocks0);
   return hipGetLastError();

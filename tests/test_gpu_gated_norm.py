@@ -220,3 +220,21 @@ def test_empty():
     s = make(0, 1, 64, "f32", residual=True, next=True)
     h, y, _, _, g = call(block, s)
     assert h.numel() == 0 and y.numel() == 0 and not g["w"].any() and not g["next"].any()
+
+
+@pytest.mark.parametrize("D", [64, 700, 2048])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_next_norm_whose_output_has_no_gradient(D, dtype):
+    """Its weight's gradient is zero, whatever the workspace held, and the others are those without a next norm."""
+    block = _block()
+    x, res, dh = (torch.randn((40, D), device="cuda").to(DT[dtype]) for _ in range(3))
+    w, w2 = (torch.rand(D, device="cuda") + 0.5 for _ in range(2))
+    _, _, rstd, y_rstd = block.gated_norm(x, w, residual=res, next_weight=w2)
+    for rows in (40, 0):
+        ws = torch.full((max(256, block.gated_norm_workspace_bytes(40, 1, D, DT[dtype])) // 4,), float("nan"), device="cuda")
+        ins = dh[:rows], x[:rows], w, rstd[:rows]
+        dx, _, dres, dw, dw2 = block.gated_norm_backward(*ins, residual=res[:rows], next_weight=w2, y_rstd=y_rstd[:rows],
+                                                         workspace=ws.view(torch.uint8))
+        want = block.gated_norm_backward(*ins, residual=res[:rows])
+        assert torch.equal(dw2, torch.zeros_like(dw2))
+        assert torch.equal(dx, want[0]) and torch.equal(dw, want[3]) and torch.equal(dres, dh[:rows])
