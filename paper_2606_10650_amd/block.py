@@ -452,7 +452,7 @@ class GatedFF(torch.autograd.Function):
         y, parts = gated_ff(rows, w_gate, w_up, want_parts=True)
         ctx.save_for_backward(rows, w_gate, w_up, parts)
         ctx.shape = x.shape
-        return y.view(*x.shape[:-1], -1)
+        return y.view(*x.shape[:-1], w_gate.shape[0])
 
     @staticmethod
     @once_differentiable

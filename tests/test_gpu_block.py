@@ -103,6 +103,21 @@ def test_gated_ff_function():
         _no_second(block.GatedFF.apply(x, wg, wu), x)
 
 
+@pytest.mark.parametrize("shape", [(0,), (0, 5), (3, 0)])
+def test_functions_without_rows(shape):
+    """Outputs of their shapes, and gradients of zeros."""
+    block, rnd = _block(), _rnd(5)
+    x, wg, wu, w, w2 = (t.requires_grad_() for t in (rnd(*shape, 40), rnd(56, 40), rnd(56, 40), rnd(40), rnd(40)))
+    y = block.GatedFF.apply(x, wg, wu)
+    h, n = block.GatedNorm.apply(x, w, None, x.detach(), 1.0, w2)
+    lp, ent, lse = block.TokenLogprobs.apply(x, torch.zeros(shape, dtype=torch.int64, device="cuda"))
+    assert y.shape == (*shape, 56) and h.shape == n.shape == x.shape and lp.shape == ent.shape == lse.shape == shape
+    (y.sum() + h.sum() + n.sum() + lp.sum() + ent.sum() + lse.sum()).backward()
+    assert x.grad.shape == x.shape
+    for t in (wg, wu, w, w2):
+        assert torch.equal(t.grad, torch.zeros_like(t))
+
+
 def test_token_logprobs_function():
     block, rnd = _block(), _rnd(4)
     l = rnd(3, 7, 100).requires_grad_()
