@@ -80,6 +80,12 @@ def _last(t, name):
         raise ValueError(f"{name}: the last axis must be contiguous")
 
 
+def _apart(out, *inputs):
+    """An output that is not where an input is, which is still read when the first results are written."""
+    if out.numel() and any(out.data_ptr() == t.data_ptr() for t in inputs):
+        raise ValueError("out: the array of an input")
+
+
 def _weight(t, shape, like, name, code=None):
     """The type code of a contiguous weight of the given shape: the inputs' type or float32."""
     if t.shape != shape or not t.is_contiguous() or t.device != like.device or \
@@ -134,6 +140,7 @@ def short_conv(x, weight, bias=None, *, activation: Optional[str] = "silu", stat
         out = _new(x)
         rows = _CONV_ROWS.pack(out.data_ptr(), T * C, C)
     else:
+        _apart(out, x)
         rows = _conv_rows(out, x, "out")
     if state_out is not None:
         if state_out is not state:
@@ -346,6 +353,7 @@ def gated_ff(x, w_gate, w_up, *, out=None, want_parts: bool = False, workspace=N
         out = x.new_empty((N, F))
         y = new(out)
     else:
+        _apart(out, x, w_gate, w_up)
         y = _ff_rows(out, (N, F), x, "out")
     parts = x.new_empty((2, N, F), dtype=torch.float32) if want_parts else None
     rows = _ff_rows(x, (N, D), x, "x"), _ff_rows(w_gate, (F, D), x, "w_gate"), _ff_rows(w_up, (F, D), x, "w_up")

@@ -231,3 +231,14 @@ def test_binding_refusals():
         block.gated_ff_backward(x, w, w, z(2, 5, 24), z(5, 23))
     with pytest.raises(ValueError):
         block.gated_ff_backward(x, w, w, z(2, 5, 24, dtype=BF16), z(5, 24))
+
+
+def test_outputs_apart_from_inputs():
+    """An output in an input's place is refused: other runs and tiles still read it."""
+    x, w = torch.zeros(1, 8, 16), torch.zeros(16, 4)
+    with pytest.raises(ValueError, match="array of an input"):
+        block.short_conv(x, w, out=x)
+    a, g = torch.zeros(4, 16), torch.zeros(16, 16)
+    for out in (a, g[:4]):
+        with pytest.raises(ValueError, match="array of an input"):
+            block.gated_ff(a, g, torch.zeros(16, 16), out=out)
