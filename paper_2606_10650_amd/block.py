@@ -29,6 +29,8 @@ _LOGPROBS = struct.Struct("q3i")         # dla_logprobs_desc
 _FF = struct.Struct("q3i")               # dla_ff_desc
 _ROWS = struct.Struct("Pq")              # dla_norm_rows
 
+_code = functools.lru_cache(maxsize=None)(_dtype_code)   # a dictionary's look-up
+
 
 @functools.lru_cache(maxsize=None)
 def lib():
@@ -76,7 +78,7 @@ def _new(t):
 
 
 def _last(t, name):
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
+    if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
         raise ValueError(f"{name}: the last axis must be contiguous")
 
 
@@ -88,13 +90,15 @@ def _apart(out, *inputs):
 
 def _weight(t, shape, like, name, code=None):
     """The type code of a contiguous weight of the given shape: the inputs' type or float32."""
+    dtype = t.dtype
     if t.shape != shape or not t.is_contiguous() or t.device != like.device or \
-            t.dtype not in (like.dtype, torch.float32):
+            (dtype != like.dtype and dtype != torch.float32):
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, not contiguous {like.dtype} or float32 "
                          f"{tuple(shape)} on {like.device}")
-    if code is not None and _dtype_code(t.dtype) != code:
-        raise ValueError(f"{name}: {t.dtype}: weights of one type are wanted")
-    return _dtype_code(t.dtype)
+    own = _code(dtype)
+    if code is not None and own != code:
+        raise ValueError(f"{name}: {dtype}: weights of one type are wanted")
+    return own
 
 
 # ---------------------------------------------------------------------------
@@ -118,7 +122,7 @@ def _conv_desc(x, weight, bias, activation, state, lengths, starts):
     if starts is not None and starts.dtype == torch.bool:
         starts = starts.view(torch.uint8)
     _like(starts, (B, T), torch.uint8, dev, "starts", True)
-    return _CONV.pack(B, T, C, W, _dtype_code(x.dtype), code, _ACTIVATIONS[activation],
+    return _CONV.pack(B, T, C, W, _code(x.dtype), code, _ACTIVATIONS[activation],
                       0 if lengths is None else lengths.data_ptr(), 0 if starts is None else starts.data_ptr())
 
 
@@ -155,7 +159,7 @@ def short_conv(x, weight, bias=None, *, activation: Optional[str] = "silu", stat
 @functools.lru_cache(maxsize=4096)
 def short_conv_workspace_bytes(B: int, T: int, C: int, W: int, dtype=torch.bfloat16) -> int:
     """Workspace of short_conv_backward."""
-    code = _dtype_code(dtype)
+    code = _code(dtype)
     return _bytes("dla_short_conv_workspace_size", _CONV.pack(B, T, C, W, code, code, 0, 0, 0))
 
 
@@ -202,7 +206,7 @@ def _gated_desc(x, weight, next_weight, eps, scale):
         _weight(next_weight, (D,), x, "next_weight", code)
         if G != 1:
             raise ValueError("next_weight: a next norm is over rows of one group")
-    return _NORM.pack(N, G, D, _dtype_code(x.dtype), code, int(per_group), eps, scale)
+    return _NORM.pack(N, G, D, _code(x.dtype), code, int(per_group), eps, scale)
 
 
 def gated_norm(x, weight, gate=None, residual=None, *, scale: float = 1.0, next_weight=None, eps: float = 1e-6):
@@ -227,7 +231,7 @@ def gated_norm(x, weight, gate=None, residual=None, *, scale: float = 1.0, next_
 @functools.lru_cache(maxsize=4096)
 def gated_norm_workspace_bytes(N: int, G: int, D: int, dtype=torch.bfloat16) -> int:
     """Workspace of gated_norm_backward, whichever weights there are."""
-    code = _dtype_code(dtype)
+    code = _code(dtype)
     return max(_bytes("dla_gated_norm_workspace_size", _NORM.pack(N, G, D, code, code, per_group, 0.0, 1.0))
                for per_group in (0, 1))
 
@@ -272,7 +276,7 @@ def _logits(logits, tokens, top):
         raise ValueError(f"logits {tuple(logits.shape)}: rows [N, V] are wanted")
     N, V = logits.shape
     _like(tokens, (N,), torch.int64, logits.device, "tokens", True)
-    return _LOGPROBS.pack(N, V, top, _dtype_code(logits.dtype))
+    return _LOGPROBS.pack(N, V, top, _code(logits.dtype))
 
 
 def token_logprobs(logits, tokens=None, *, top: int = 0, entropy: bool = False, workspace=None):
@@ -292,7 +296,7 @@ def token_logprobs(logits, tokens=None, *, top: int = 0, entropy: bool = False, 
 
 @functools.lru_cache(maxsize=4096)
 def _logprobs_bytes(N, V, top, dtype):
-    return _bytes("dla_token_logprobs_workspace_size", _LOGPROBS.pack(N, V, top, _dtype_code(dtype)))
+    return _bytes("dla_token_logprobs_workspace_size", _LOGPROBS.pack(N, V, top, _code(dtype)))
 
 
 def token_logprobs_backward(logits, tokens, logprob, lse, dlogprob=None, *, entropy=None, dentropy=None, dlse=None,
@@ -340,7 +344,7 @@ def _aligned(x, w_gate, w_up):
 def gated_ff_workspace_bytes(N: int, D: int, F: int, dtype=torch.bfloat16, *, backward: bool = False,
                              aligned: bool = True) -> int:
     """Workspace of a forward (or backward) pass.  aligned: rows of x and the weights start at multiples of 16 bytes."""
-    return _bytes("dla_gated_ff_workspace_size", _FF.pack(N, D, F, _dtype_code(dtype)), int(backward), int(aligned))
+    return _bytes("dla_gated_ff_workspace_size", _FF.pack(N, D, F, _code(dtype)), int(backward), int(aligned))
 
 
 def gated_ff(x, w_gate, w_up, *, out=None, want_parts: bool = False, workspace=None):
@@ -359,7 +363,7 @@ def gated_ff(x, w_gate, w_up, *, out=None, want_parts: bool = False, workspace=N
     rows = _ff_rows(x, (N, D), x, "x"), _ff_rows(w_gate, (F, D), x, "w_gate"), _ff_rows(w_up, (F, D), x, "w_up")
     need = gated_ff_workspace_bytes(N, D, F, x.dtype, aligned=_aligned(x, w_gate, w_up))
     workspace, size = _work(workspace, need, dev)
-    _call("dla_gated_ff", dev, _FF.pack(N, D, F, _dtype_code(x.dtype)), *rows, y,
+    _call("dla_gated_ff", dev, _FF.pack(N, D, F, _code(x.dtype)), *rows, y,
           *(map(new, parts) if want_parts else (None, None)), _ptr(workspace), size)
     return out, parts
 
@@ -374,7 +378,7 @@ def gated_ff_backward(x, w_gate, w_up, parts, dy, *, workspace=None):
     dx, dwg, dwu = x.new_empty((N, D)), x.new_empty((F, D)), x.new_empty((F, D))
     need = gated_ff_workspace_bytes(N, D, F, x.dtype, backward=True, aligned=_aligned(x, w_gate, w_up))
     workspace, size = _work(workspace, need, dev)
-    _call("dla_gated_ff_backward", dev, _FF.pack(N, D, F, _dtype_code(x.dtype)), *rows,
+    _call("dla_gated_ff_backward", dev, _FF.pack(N, D, F, _code(x.dtype)), *rows,
           _ROWS.pack(parts.data_ptr(), F), _ROWS.pack(parts.data_ptr() + 4 * N * F, F), _ff_rows(dy, (N, F), x, "dy"),
           _ff_rows(dx, (N, D), x, "dx"), _ff_rows(dwg, (F, D), x, "dw_gate"), _ff_rows(dwu, (F, D), x, "dw_up"),
           _ptr(workspace), size)
