@@ -460,32 +460,33 @@ FfPlan plan_ff_gemm(int kind, int64_t M, int64_t N, int64_t K, int pairs) {
     w.tiles_n = (int)((N + width - 1) / width);
     w.tiles = (int64_t)w.tiles_m * w.tiles_n;
     w.steps = (K > 0 ? (K + kStep - 1) / kStep : 1) * pairs;   // (without K one of zeros)
-    // A step's time in microseconds where every compute unit has one workgroup (small tiles: two share the
-    // unit in turn, and pass without a pause from one to the next); what a part costs to write and to
-    // read.  Of 8 sizes from 100 to 16384 rows, tiles and shares by these are within 6% of the best of
-    // 12 tried, but for one (2048 x 512 x 512 rows of K: 10%).
+    // A step's time in microseconds; what a part costs to write and to read, and the joining.  A large tile has its
+    // compute unit for itself.  Of small ones two share a unit, and those behind them follow without a pause, so
+    // that more than two for each unit take a step's time each; one alone waits for its loads, and where some
+    // units have two and others one the two set the time.  Of 8 sizes from 270 to 16384 rows, three products each,
+    // tiles and shares by these are within 1.5% of the best of 13 tried on average, and within 10% (with up to two
+    // workgroups a unit counted by their number 3.6% and 18%: 4130 x 1280 x 154 float32, forward, in 297 workgroups 67
+    // us, in 396 57).
     const int64_t at_once = 256;
-    const double step = large ? 1.7 : 0.62, part = large ? 0.16 : 0.05, join = 8.;
+    const double step = large ? 1.7 : 0.62, part = large ? 0.12 : 0.03, join = 6.;
     const auto rounds = [&](int64_t n) {
-      return large ? (double)((n + at_once - 1) / at_once) : n < at_once ? (n > 0 ? 1. : 0.) : (double)n / at_once;
+      const double each = (double)n / at_once;
+      if (large || n == 0) return (double)((n + at_once - 1) / at_once);
+      return n <= at_once ? 1.25 : each < 1.8 ? 1.8 : each;
     };
     w.full = w.tiles / at_once * at_once;
     const int64_t rest = w.tiles - w.full;
-    double time = rounds(w.full) * w.steps * step;
-    if (rest) {
-      double cost = w.steps * step;
-      int share = 1;
-      for (int s = 2; s <= 64 && s * 4 <= w.steps; ++s) {     // of 4 steps at least
-        const double c = rounds(rest * s) * ((w.steps + s - 1) / s) * step + join + part * rest * s;
-        if (c < cost) {
-          cost = c;
-          share = s;
-        }
+    double time = (rounds(w.full) + rounds(rest)) * w.steps * step;
+    int share = 1;
+    for (int s = 2; rest && s <= 64 && s * 4 <= w.steps; ++s) {     // of 4 steps at least
+      const double c = (rounds(w.full) * w.steps + rounds(rest * s) * ((w.steps + s - 1) / s)) * step + join + part * rest * s;
+      if (c < time) {
+        time = c;
+        share = s;
       }
-      time += cost;
-      if (share > 1) w.share = share;
-      else w.full = w.tiles;
     }
+    if (share > 1) w.share = share;
+    else w.full = w.tiles;
     w.part_bytes = (size_t)(w.tiles - w.full) * w.share * t * t * 4;
     if (!large || time < least) {
       best = w;
