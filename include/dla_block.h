@@ -11,8 +11,9 @@
  * aligned, hold nothing between calls, and must not be used by another call until the
  * stream has passed the one they were given to.  Every result is the same from call to
  * call: no sum's order depends on timing.  Outputs do not overlap inputs, or each other,
- * but where a call says that they may be the same array.  Arrays need the alignment of
- * their type only; rows that start at multiples of 16 bytes are faster.
+ * but where a call says that they may be the same array: the same address with the same
+ * strides (the calls do not check it; the Python binding does).  Arrays need the alignment
+ * of their type only; rows that start at multiples of 16 bytes are faster.
  */
 #ifndef DLA_BLOCK_H
 #define DLA_BLOCK_H

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import struct
 from typing import Optional
 
@@ -82,10 +83,37 @@ def _last(t, name):
         raise ValueError(f"{name}: the last axis must be contiguous")
 
 
-def _apart(out, *inputs):
-    """An output that is not where an input is, which is still read when the first results are written."""
-    if out.numel() and any(out.data_ptr() == t.data_ptr() for t in inputs):
-        raise ValueError("out: the array of an input")
+def _place(t):
+    """Where a tensor lies, in bytes: its begin and end, and what its elements repeat: runs so long, at distances that
+    are multiples of a step (0: one run)."""
+    e, run, step, last = t.element_size(), 1, 0, 0
+    for n, distance in zip(reversed(t.shape), reversed(t.stride())):
+        if n > 1:
+            last += (n - 1) * distance
+            if distance == run and not step:
+                run *= n
+            else:
+                step = math.gcd(step, distance)
+    at = t.data_ptr()
+    return at, at + (last + 1) * e, run * e, step * e
+
+
+def _apart(name, out, *inputs):
+    """An output whose elements are no input's: those are still read when the first results are written.  Columns of one
+    wider array are apart."""
+    if not out.numel():
+        return
+    at, end, run, step = _place(out)
+    for t in inputs:
+        if t is None or not t.numel():
+            continue
+        t_at, t_end, t_run, t_step = _place(t)
+        if t_end <= at or end <= t_at:
+            continue
+        both = math.gcd(step, t_step)
+        off = (t_at - at) % both if both else 0
+        if off < run or off + t_run > both:
+            raise ValueError(f"{name}: lies over the array of an input")
 
 
 def _weight(t, shape, like, name, code=None):
@@ -137,21 +165,31 @@ def short_conv(x, weight, bias=None, *, activation: Optional[str] = "silu", stat
     """z_t = bias + sum_j weight[:, j] x_{t - (W - 1) + j} per channel, and its SiLU (dla_short_conv).
     x: [B, T, C], last axis contiguous; weight [C, W], W 2 to 4; state [B, W - 1, C], the inputs before
     the call, or None; lengths int32 [B]; starts [B, T], bool or uint8, where documents start.  state_out
-    may be state.  Returns (out, state_out); out is contiguous unless given."""
+    may be state; otherwise state_out and out are apart from the inputs and each other.  Returns (out, state_out);
+    out is contiguous unless given."""
     desc = _conv_desc(x, weight, bias, activation, state, lengths, starts)
     B, T, C = x.shape
+    _last(x, "x")
+    at, (b, t, _) = x.data_ptr(), x.stride()
+    given = out
     if out is None:
         out = _new(x)
         rows = _CONV_ROWS.pack(out.data_ptr(), T * C, C)
     else:
-        _apart(out, x)
         rows = _conv_rows(out, x, "out")
+        _apart("out", out, x, weight, bias, state, lengths, starts)
     if state_out is not None:
         if state_out is not state:
             _like(state_out, (B, weight.shape[1] - 1, C), x.dtype, x.device, "state_out", True)
+            same = state is not None and state.data_ptr() == state_out.data_ptr()
+            _apart("state_out", state_out, weight, bias, lengths, starts, given, None if same else state)
+        # (mostly told by their ends)
+        e, s = x.element_size(), state_out.data_ptr()
+        if at < s + state_out.numel() * e and s < at + ((B - 1) * b + (T - 1) * t + C) * e:
+            _apart("state_out", state_out, x)
     elif want_state:
         state_out = x.new_empty((B, weight.shape[1] - 1, C))
-    _call("dla_short_conv", x.device, desc, _conv_rows(x, x, "x"), weight.data_ptr(), _ptr(bias), _ptr(state), rows,
+    _call("dla_short_conv", x.device, desc, _CONV_ROWS.pack(at, b, t), weight.data_ptr(), _ptr(bias), _ptr(state), rows,
           _ptr(state_out))
     return out, state_out
 
@@ -302,7 +340,7 @@ def _logprobs_bytes(N, V, top, dtype):
 def token_logprobs_backward(logits, tokens, logprob, lse, dlogprob=None, *, entropy=None, dentropy=None, dlse=None,
                             dlogits=None):
     """The gradient of the logits from those of `token_logprobs`' outputs (None: zero) and the outputs themselves
-    (dla_token_logprobs_backward).  dlogits may be the logits."""
+    (dla_token_logprobs_backward).  dlogits may be the logits, and is otherwise apart from the inputs."""
     desc, dev, f32 = _logits(logits, tokens, 0), logits.device, torch.float32
     N = logits.shape[0]
     for name, t in (("logprob", logprob), ("lse", lse), ("entropy", entropy), ("dlogprob", dlogprob),
@@ -312,6 +350,8 @@ def token_logprobs_backward(logits, tokens, logprob, lse, dlogprob=None, *, entr
         dlogits = _new(logits)
     else:
         _like(dlogits, logits.shape, logits.dtype, dev, "dlogits")
+        same = dlogits.data_ptr() == logits.data_ptr() and (N <= 1 or dlogits.stride(0) == logits.stride(0))
+        _apart("dlogits", dlogits, None if same else logits, tokens, logprob, lse, entropy, dlogprob, dentropy, dlse)
     _call("dla_token_logprobs_backward", dev, desc, _logit_rows(logits, "logits"), _ptr(tokens), _ptr(logprob),
           _ptr(lse), _ptr(entropy), _ptr(dlogprob), _ptr(dentropy), _ptr(dlse), _logit_rows(dlogits, "dlogits"))
     return dlogits
@@ -348,8 +388,8 @@ def gated_ff_workspace_bytes(N: int, D: int, F: int, dtype=torch.bfloat16, *, ba
 
 
 def gated_ff(x, w_gate, w_up, *, out=None, want_parts: bool = False, workspace=None):
-    """y = silu(x w_gate^T) * (x w_up^T) (dla_gated_ff).  x: [N, D], w_gate and w_up [F, D], last axes contiguous.
-    Returns (y, parts): the products [2, N, F], float32, that gated_ff_backward needs, or None."""
+    """y = silu(x w_gate^T) * (x w_up^T) (dla_gated_ff).  x: [N, D], w_gate and w_up [F, D], last axes contiguous; out
+    is apart from them.  Returns (y, parts): the products [2, N, F], float32, that gated_ff_backward needs, or None."""
     N, D, F = _ff_sizes(x, w_gate, w_up)
     dev = x.device
     new = lambda t: _ROWS.pack(t.data_ptr(), F)  # noqa: E731
@@ -357,8 +397,8 @@ def gated_ff(x, w_gate, w_up, *, out=None, want_parts: bool = False, workspace=N
         out = x.new_empty((N, F))
         y = new(out)
     else:
-        _apart(out, x, w_gate, w_up)
         y = _ff_rows(out, (N, F), x, "out")
+        _apart("out", out, x, w_gate, w_up)
     parts = x.new_empty((2, N, F), dtype=torch.float32) if want_parts else None
     rows = _ff_rows(x, (N, D), x, "x"), _ff_rows(w_gate, (F, D), x, "w_gate"), _ff_rows(w_up, (F, D), x, "w_up")
     need = gated_ff_workspace_bytes(N, D, F, x.dtype, aligned=_aligned(x, w_gate, w_up))

@@ -1,0 +1,150 @@
+"""Outputs that a caller gives to the operators around the recurrence: apart from the inputs and each other, or refused
+before the library is called."""
+import pytest
+import torch
+
+from paper_2606_10650_amd import block
+
+REFUSED = pytest.raises(ValueError, match="array of an input")
+
+
+def _flat(n=4096, dtype=torch.float32):
+    return torch.zeros(n, dtype=dtype)
+
+
+def test_place():
+    """Begin, end, run and step against the elements' addresses themselves."""
+    for shape, strides in (((2, 5, 8), (40, 8, 1)), ((2, 5, 8), (60, 12, 1)), ((2, 5, 8), (8, 16, 1)), ((3, 1, 4), (30, 7, 1)), ((4, 6), (0, 1)),
+                           ((4, 6), (1, 10)), ((7,), (3,)), ((1, 1), (9, 9)), ((2, 3, 4), (5, 10, 1)), ((3, 4, 2), (4, 5, 1))):
+        t = _flat().as_strided(shape, strides, 11)
+        at, end, run, step = block._place(t)
+        have = torch.zeros(1, dtype=torch.int64)
+        for n, d in zip(shape, strides):
+            have = (have[:, None] + torch.arange(n) * d * 4).flatten()
+        assert at == t.data_ptr() and end - at == have.max().item() + 4
+        # every element lies in a run that begins at a multiple of the step
+        assert run <= end - at and all((h % step if step else h) < run for h in have.tolist())
+
+
+def test_apart_against_elements():
+    """Refused wherever an element is shared; taken for what a caller does: blocks behind each other, columns of one array."""
+    flat = _flat()
+    views = [flat.as_strided(shape, strides, at) for at in (0, 1, 5, 8, 12, 40, 79, 80, 200)
+             for shape, strides in (((2, 5, 8), (40, 8, 1)), ((2, 5, 4), (80, 16, 1)), ((10, 8), (16, 1)), ((10, 8), (24, 1)), ((5, 3), (16, 2)), ((1, 7), (7, 1)))]
+
+    def elements(t):
+        i = torch.arange(flat.numel()).as_strided(t.shape, t.stride(), t.storage_offset())
+        return set(i.flatten().tolist())
+
+    taken = 0
+    for a in views:
+        for b in views:
+            try:
+                block._apart("out", a, b)
+                taken += 1
+                assert not elements(a) & elements(b), (a.shape, a.stride(), a.storage_offset(), b.shape, b.stride(), b.storage_offset())
+            except ValueError:
+                pass
+    assert taken
+    wide = torch.zeros(6, 5, 40)
+    for a, b in ((wide[..., :16], wide[..., 16:32]), (wide[..., 24:], wide[..., :24]), (wide[:3], wide[3:]), (wide[:, :2], wide[:, 2:]),
+                 (wide[..., :8].transpose(0, 1), wide[..., 8:])):
+        block._apart("out", a, b)
+        block._apart("out", b, a)
+    block._apart("out", wide[:0], wide)
+    block._apart("out", wide, wide[:0], None)
+
+
+@pytest.mark.parametrize("shift", [1, 3, 8, 16, 40, 127])
+def test_conv_shifted(shift):
+    """An output a few elements or tokens into the input, before it and behind it."""
+    B, T, C = 2, 8, 16
+    flat, w = _flat(), torch.zeros(C, 4)
+    at = lambda n: flat[n:n + B * T * C].view(B, T, C)  # noqa: E731
+    for x, out in ((at(0), at(shift)), (at(shift), at(0))):
+        with REFUSED:
+            block.short_conv(x, w, out=out)
+    wide = torch.zeros(B, T + 1, C)
+    with REFUSED:
+        block.short_conv(wide[:, :-1], w, out=wide[:, 1:])
+    with REFUSED:
+        block.short_conv(wide[:, 1:], w, out=wide[:, :-1])
+
+
+def test_conv_states():
+    """The last state over the input, over a part of the given state, over the output; the output over the state."""
+    B, T, C = 3, 8, 16
+    w, x, S = torch.zeros(C, 4), torch.zeros(B, T, C), torch.zeros(B + 1, 3, C)
+    for state, state_out in ((S[:B], S[1:]), (S[1:], S[:B]), (None, x.view(-1)[:B * 3 * C].view(B, 3, C)), (S[:B], x.view(-1)[-B * 3 * C:].view(B, 3, C))):
+        with REFUSED:
+            block.short_conv(x, w, state=state, state_out=state_out)
+    same = x.view(-1)[16:16 + B * 3 * C].view(B, 3, C)
+    with REFUSED:
+        block.short_conv(x, w, state=same, state_out=same)
+    both = _flat()
+    out = both[:B * T * C].view(B, T, C)
+    for at in (0, 5, B * T * C - 1):
+        inside = both[at:at + B * 3 * C].view(B, 3, C)
+        with REFUSED:
+            block.short_conv(x, w, out=out, state_out=inside)
+        with REFUSED:
+            block.short_conv(x, w, out=out, state=inside)
+        with REFUSED:
+            block.short_conv(x, w, out=out, state=inside, state_out=inside)
+    with REFUSED:
+        block.short_conv(x, out.view(-1)[:C * 4].view(C, 4), out=out)
+
+
+@pytest.mark.parametrize("shift", [1, 8, 16, 48])
+def test_ff_shifted(shift):
+    N, D, F = 6, 16, 16
+    flat, g, u = _flat(), torch.zeros(F, D), torch.zeros(F, D)
+    at = lambda n: flat[n:n + N * D].view(N, D)  # noqa: E731
+    for x, out in ((at(0), at(shift)), (at(shift), at(0))):
+        with REFUSED:
+            block.gated_ff(x, g, u, out=out)
+        with REFUSED:
+            block.gated_ff(torch.zeros(N, D), flat[:F * D].view(F, D), u, out=out)
+    wide = torch.zeros(N + 1, D + 8)
+    with REFUSED:
+        block.gated_ff(wide[:-1, :D], g, u, out=wide[1:, 4:4 + D])
+
+
+def test_dlogits_shifted():
+    """The logits' place is taken with the logits' strides alone."""
+    N, V = 4, 10
+    flat, tok, f = _flat(), torch.zeros(N, dtype=torch.int64), [torch.zeros(N) for _ in range(3)]
+    rows = lambda at, stride: flat.as_strided((N, V), (stride, 1), at)  # noqa: E731
+    for logits, dlogits in ((rows(0, 10), rows(0, 12)), (rows(0, 12), rows(0, 10)), (rows(0, 10), rows(1, 10)), (rows(0, 10), rows(10, 10)),
+                            (rows(10, 16), rows(0, 16)), (rows(5, 0), rows(0, 10))):
+        with REFUSED:
+            block.token_logprobs_backward(logits, tok, *f, dlogits=dlogits)
+    with REFUSED:
+        block.token_logprobs_backward(rows(0, 10), tok, f[0], flat[80:84], f[2], dlogits=rows(50, 10))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_columns_of_one_array(dtype):
+    """Inputs and outputs side by side in the rows of one array, and gradients over the logits: as in arrays of their own."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda").to(dtype)  # noqa: E731
+    wide, w = rnd(2, 70, 100), rnd(48, 4)
+    want = block.short_conv(wide[..., :48].contiguous(), w)[0]
+    block.short_conv(wide[..., :48], w, out=wide[..., 50:98])
+    assert torch.equal(wide[..., 50:98], want)
+    for N in (9, 150):
+        wide, g, u = rnd(N, 100), rnd(48, 40), rnd(48, 40)
+        want = block.gated_ff(wide[:, :40].contiguous(), g, u)[0]
+        block.gated_ff(wide[:, :40], g, u, out=wide[:, 41:89])
+        assert torch.equal(wide[:, 41:89], want)
+    S, x = rnd(2, 3, 48), rnd(2, 5, 48)
+    want, last = block.short_conv(x, w, state=S, want_state=True)
+    got, over = block.short_conv(x, w, state=S, state_out=S.view(2, 3, 48))       # another view of the same state
+    assert torch.equal(got, want) and torch.equal(S, last) and over.data_ptr() == S.data_ptr()
+    l, tok = rnd(7, 300), torch.randint(0, 300, (7,), generator=gen, device="cuda")
+    lp, lse, *_ = block.token_logprobs(l, tok)
+    want = block.token_logprobs_backward(l, tok, lp, lse, lp)
+    assert torch.equal(block.token_logprobs_backward(l, tok, lp, lse, lp, dlogits=l), want) and torch.equal(l, want)
