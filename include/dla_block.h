@@ -189,8 +189,11 @@ dla_status dla_token_logprobs_backward(const dla_logprobs_desc* desc, const dla_
  * product is exact; y is formed from unrounded g and u.  float32 inputs are taken as sums of
  * three bfloat16 terms, the largest first, and products of terms below 2^-24 of the whole are
  * left out: results are float32's to about 2^-22 of the sum of the products' magnitudes.  Of
- * float32, magnitudes from 2^-100 to 2^126 are taken to that precision; an infinity may come out
- * as NaN.
+ * float32, magnitudes from 2^-100 to 2^126 are taken to that precision.  Terms do not hold an
+ * infinity (its first is one, and times another's zero term NaN): what it reaches is infinite or
+ * NaN, which of the two is not defined, and so with what is larger than 2^126.  A forward pass of
+ * up to 64 rows multiplies float32 values themselves, without these limits: there an infinity
+ * gives what float32's own sums give.
  */
 typedef struct {
   int64_t rows;

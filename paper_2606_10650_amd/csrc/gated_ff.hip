@@ -106,8 +106,9 @@ __global__ __launch_bounds__(512) void ff_step_kernel(int rows, int D, int F, Ff
   }
 }
 
-// Three bfloat16 terms of a value, whose sum it is to float32's last digit; a value that is not
-// finite is its first term.
+// Three bfloat16 terms of a value, whose sum it is to float32's last digit.  A value that is not finite, or
+// rounds to an infinity, is its first term: it makes every sum that it is in infinite or, by the other operand's
+// terms of zero or other sign, NaN.
 __device__ __forceinline__ void terms(float v, __bf16 (&t)[3]) {
   t[0] = (__bf16)v;
   float rest = v - (float)t[0];
@@ -115,7 +116,6 @@ __device__ __forceinline__ void terms(float v, __bf16 (&t)[3]) {
   t[1] = (__bf16)rest;
   t[2] = (__bf16)(rest - (float)t[1]);
 }
-
 
 // A piece of values to the planes.
 template <typename T, int N>
