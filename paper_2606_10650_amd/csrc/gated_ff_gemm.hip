@@ -126,12 +126,13 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
   const int l32 = lane & 31, half = lane >> 5;
   // A wave's columns of C, of one of the outputs, through LDS in rows of kLine bytes (so that eight lanes' pieces
   // have other banks), so that memory is written 16 bytes a lane.
-  auto out = [&](auto kind, const FfRows& r, int64_t rows, int64_t m, int64_t c, auto value) {
+  auto out = [&](auto kind, const FfRows& r, int64_t rows, int64_t m, int64_t c, auto value, auto for_later) {
     using T = decltype(kind);
-    constexpr bool f32 = sizeof(T) == 4, later = f32 && KIND == 0;
-    // value(e): element e of the lane; its row is m + l32, its columns c + out_row(e, lane); g and u,
+    constexpr bool f32 = sizeof(T) == 4, later = decltype(for_later)::value;
+    // value(e): element e of the lane; its row is m + l32, its columns c + out_row(e, lane); later: g and u,
     // which only the backward pass reads, are not to take the operands' place in the caches (with both in
-    // bfloat16 675 us became 655)
+    // bfloat16 675 us became 655); y, which the next product reads, may (float32, 8192 x 768 x 2048 with
+    // that product behind it, 486 us, and 487 with y past the caches too)
     if (!r.p) return;
     const bool pieces = ((uintptr_t)r.p & 15) == 0 && r.st % (f32 ? 4 : 8) == 0;
     if (!pieces) {
@@ -174,6 +175,8 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
     }
   };
   const typename std::conditional<F32, float, __bf16>::type type{};
+  const std::false_type soon;
+  const std::true_type later;
 #pragma unroll
   for (int i = 0; i < SM; ++i) {
     const int64_t m = mw + 32 * i;
@@ -181,9 +184,9 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
 #pragma unroll
       for (int j = 0; j < SN; j += 2) {
         const int64_t c = nw + 16 * j;
-        out(type, p.c, p.M, m, c, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; });
-        out(0.f, p.g, p.M, m, c, [&](int e) { return acc[i][j][e]; });
-        out(0.f, p.u, p.M, m, c, [&](int e) { return acc[i][j + 1][e]; });
+        out(type, p.c, p.M, m, c, [&](int e) { return silu(acc[i][j][e]) * acc[i][j + 1][e]; }, soon);
+        out(0.f, p.g, p.M, m, c, [&](int e) { return acc[i][j][e]; }, later);
+        out(0.f, p.u, p.M, m, c, [&](int e) { return acc[i][j + 1][e]; }, later);
       }
     } else {
       // of kind 2 a tile's 32 rows may belong to both halves, where these are not multiples of 32 long
@@ -191,10 +194,10 @@ __device__ __forceinline__ void ff_store(const FfGemm& p, const f32x16 (&acc)[TM
       for (int j = 0; j < SN; ++j) {
         auto value = [&](int e) { return acc[i][j][e]; };
         if constexpr (KIND == 1) {
-          out(type, p.c, p.M, m, nw + 32 * j, value);
+          out(type, p.c, p.M, m, nw + 32 * j, value, soon);
         } else {
-          if (m < p.half) out(type, p.c, p.rows, m, nw + 32 * j, value);
-          if (m + 32 > p.half) out(type, p.c2, p.rows, m - p.half, nw + 32 * j, value);
+          if (m < p.half) out(type, p.c, p.rows, m, nw + 32 * j, value, soon);
+          if (m + 32 > p.half) out(type, p.c2, p.rows, m - p.half, nw + 32 * j, value, soon);
         }
       }
     }
