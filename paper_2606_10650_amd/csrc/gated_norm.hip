@@ -375,8 +375,10 @@ hipError_t pick(const GatedNormArgs& a, bool back, hipStream_t st) {
       case 512: return backward<T, 512, 1>(a, st);
       default:
         if (pieces <= 1024) return backward<T, 1024, 1>(a, st);
-        if (pieces <= 2048) return backward<T, 1024, 2>(a, st);
-        return backward<T, 1024, 4>(a, st);
+        // (16384 bfloat16 values are 2048 pieces)
+        if constexpr (sizeof(T) == 4)
+          if (pieces > 2048) return backward<T, 1024, 4>(a, st);
+        return backward<T, 1024, 2>(a, st);
     }
   }
   switch (nt) {
@@ -391,8 +393,9 @@ hipError_t pick(const GatedNormArgs& a, bool back, hipStream_t st) {
       if (pieces <= 512) return forward<T, 256, 2>(a, st);
       return forward<T, 256, 4>(a, st);
     default:
-      if (pieces <= 2048) return forward<T, 1024, 2>(a, st);
-      return forward<T, 1024, 4>(a, st);
+      if constexpr (sizeof(T) == 4)
+        if (pieces > 2048) return forward<T, 1024, 4>(a, st);
+      return forward<T, 1024, 2>(a, st);
   }
 }
 
