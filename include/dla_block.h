@@ -220,7 +220,8 @@ dla_status dla_gated_ff(const dla_ff_desc* desc, const dla_norm_rows* x,
  *   dg = dy u (s + g s (1 - s)),  du = dy g s,  s = 1 / (1 + exp(-g)),
  * formed in float32 and rounded once to dtype:
  *   dx = dg w_gate + du w_up,  dw_gate = dg^T x,  dw_up = du^T x,
- * sums in float32, each rounded once to dtype.  dx, dw_gate and dw_up may be NULL: not wanted. */
+ * sums in float32, each rounded once to dtype.  (Of bfloat16, errors of dg's and du's rounding reach
+ * the gradients as large as those of their own.)  dx, dw_gate and dw_up may be NULL: not wanted. */
 dla_status dla_gated_ff_backward(const dla_ff_desc* desc, const dla_norm_rows* x,
                                  const dla_norm_rows* w_gate, const dla_norm_rows* w_up,
                                  const dla_norm_rows* g, const dla_norm_rows* u,

@@ -155,6 +155,10 @@ __global__ __launch_bounds__(256) void ff_pack_kernel(FfPacks sets) {
   }
 }
 
+// dg and du, formed in float32 and rounded once.  Of bfloat16 inputs they become bfloat16, which is what the matrix
+// units multiply: an error of 2^-8 of each at most, that adds to the gradients' own rounding (16384 rows, 2048 to 5504:
+// off by 0.0023 of the gradients' size against float64, of which rounding the results alone is 0.0017).  A second
+// bfloat16 term of each gives 0.0017, by twice the products: forward and backward 3380 us in place of 2140.
 template <typename T>
 __global__ __launch_bounds__(256) void ff_parts_kernel(int64_t rows, int F, int ld, FfRows g, FfRows u, FfRows dy,
                                                        uint16_t* to) {
