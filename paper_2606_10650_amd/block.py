@@ -84,36 +84,48 @@ def _last(t, name):
 
 
 def _place(t):
-    """Where a tensor lies, in bytes: its begin and end, and what its elements repeat: runs so long, at distances that
-    are multiples of a step (0: one run)."""
-    e, run, step, last = t.element_size(), 1, 0, 0
-    for n, distance in zip(reversed(t.shape), reversed(t.stride())):
-        if n > 1:
-            last += (n - 1) * distance
-            if distance == run and not step:
-                run *= n
-            else:
-                step = math.gcd(step, distance)
-    at = t.data_ptr()
-    return at, at + (last + 1) * e, run * e, step * e
+    """Where a tensor's elements lie: the first byte, and counts and distances in bytes of what repeats, the furthest
+    apart first; the last is a run of bytes."""
+    e, run, more = t.element_size(), 1, []
+    for distance, n in sorted(zip(t.stride(), t.shape)):
+        if distance == run and not more:
+            run *= n
+        elif n > 1 and distance:
+            more.append((n, distance * e))
+    return t.data_ptr(), (*reversed(more), (run * e, 1))
+
+
+def _meet(off, a, b):
+    """Whether a byte is both what lies as `a` and what lies as `b` and begins `off` bytes behind it; also where that is not
+    told by their distances."""
+    ends = [sum((n - 1) * s for n, s in t) + 1 for t in (a, b)]
+    if off >= ends[0] or off + ends[1] <= 0:
+        return False
+    (n, s), (m, t) = a[0], b[0]
+    if s == t == 1:
+        return True
+    if s == t:
+        # rows of one distance: those near each other
+        each = [end - (k - 1) * s for end, k in zip(ends, (n, m))]
+        low, high = max(1 - n, (-each[1] - off) // s + 1), min(m - 1, (each[0] - off - 1) // s)
+        if high - low < 8:
+            return any(_meet(off + k * s, a[1:], b[1:]) for k in range(low, high + 1))
+    # runs at multiples of a common step
+    step = functools.reduce(math.gcd, [s for _, s in (*a[:-1], *b[:-1])])
+    return off % step < a[-1][0] or off % step + b[-1][0] > step
 
 
 def _apart(name, out, *inputs):
-    """An output whose elements are no input's: those are still read when the first results are written.  Columns of one
-    wider array are apart."""
+    """An output whose elements are no input's: those are still read when the first results are written.  Columns or
+    tokens of one wider array are apart."""
     if not out.numel():
         return
-    at, end, run, step = _place(out)
+    at, own = _place(out)
     for t in inputs:
-        if t is None or not t.numel():
-            continue
-        t_at, t_end, t_run, t_step = _place(t)
-        if t_end <= at or end <= t_at:
-            continue
-        both = math.gcd(step, t_step)
-        off = (t_at - at) % both if both else 0
-        if off < run or off + t_run > both:
-            raise ValueError(f"{name}: lies over the array of an input")
+        if t is not None and t.numel():
+            t_at, t_own = _place(t)
+            if _meet(t_at - at, own, t_own):
+                raise ValueError(f"{name}: lies over the array of an input")
 
 
 def _weight(t, shape, like, name, code=None):

@@ -13,17 +13,19 @@ def _flat(n=4096, dtype=torch.float32):
 
 
 def test_place():
-    """Begin, end, run and step against the elements' addresses themselves."""
+    """A tensor's first byte and what repeats from there, against its elements' addresses."""
     for shape, strides in (((2, 5, 8), (40, 8, 1)), ((2, 5, 8), (60, 12, 1)), ((2, 5, 8), (8, 16, 1)), ((3, 1, 4), (30, 7, 1)), ((4, 6), (0, 1)),
-                           ((4, 6), (1, 10)), ((7,), (3,)), ((1, 1), (9, 9)), ((2, 3, 4), (5, 10, 1)), ((3, 4, 2), (4, 5, 1))):
+                           ((4, 6), (1, 10)), ((7,), (3,)), ((1, 1), (9, 9)), ((2, 3, 4), (5, 10, 1)), ((3, 4, 2), (4, 5, 1)), ((2, 1, 3), (1, 1, 2)),
+                           ((1, 5), (1, 1)), ((3, 3), (1, 1))):
         t = _flat().as_strided(shape, strides, 11)
-        at, end, run, step = block._place(t)
-        have = torch.zeros(1, dtype=torch.int64)
+        have, told = torch.zeros(1, dtype=torch.int64), torch.zeros(1, dtype=torch.int64)
         for n, d in zip(shape, strides):
             have = (have[:, None] + torch.arange(n) * d * 4).flatten()
-        assert at == t.data_ptr() and end - at == have.max().item() + 4
-        # every element lies in a run that begins at a multiple of the step
-        assert run <= end - at and all((h % step if step else h) < run for h in have.tolist())
+        have = (have[:, None] + torch.arange(4)).flatten()
+        at, own = block._place(t)
+        for n, d in own:
+            told = (told[:, None] + torch.arange(n) * d).flatten()
+        assert at == t.data_ptr() and set(have.tolist()) == set(told.tolist()) and own[-1][1] == 1
 
 
 def test_apart_against_elements():
@@ -36,7 +38,7 @@ def test_apart_against_elements():
         i = torch.arange(flat.numel()).as_strided(t.shape, t.stride(), t.storage_offset())
         return set(i.flatten().tolist())
 
-    taken = 0
+    taken = closer = 0
     for a in views:
         for b in views:
             try:
@@ -44,11 +46,13 @@ def test_apart_against_elements():
                 taken += 1
                 assert not elements(a) & elements(b), (a.shape, a.stride(), a.storage_offset(), b.shape, b.stride(), b.storage_offset())
             except ValueError:
-                pass
-    assert taken
+                closer += not elements(a) & elements(b)
+    # (few are apart without being told so)
+    assert taken and closer < 0.1 * taken
     wide = torch.zeros(6, 5, 40)
     for a, b in ((wide[..., :16], wide[..., 16:32]), (wide[..., 24:], wide[..., :24]), (wide[:3], wide[3:]), (wide[:, :2], wide[:, 2:]),
-                 (wide[..., :8].transpose(0, 1), wide[..., 8:])):
+                 (wide[..., :8].transpose(0, 1), wide[..., 8:]), (wide[:, ::2], wide[:, 1::2]), (wide[::3], wide[1::3]),
+                 (wide[:, 1:2, 5:], wide[:, 2:]), (wide[:, 0, :7], wide[:, 0, 7:]), (wide[:1, 0], wide[0, 1:])):
         block._apart("out", a, b)
         block._apart("out", b, a)
     block._apart("out", wide[:0], wide)
